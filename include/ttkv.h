@@ -321,6 +321,84 @@ ttkv_status ttkv_select_blocks(ttkv_handle h, const ttkv_cache *c, const void *q
                                int32_t *sel_blocks, int32_t *sel_count, int32_t sel_stride, void *scratch,
                                size_t scratch_bytes, void *stream);
 
+/* ---------------------------------------------------------------- from the projections to the cache */
+
+/* A strided view of heads of 128 channels, [sequence][token][head][128] (for instance the queries' part of a packed
+ * projection).  Strides count elements; those of dimensions of one entry are not looked at.  Every row starts at a multiple of
+ * 16 bytes.  Views that are read may repeat rows (stride 0); rows of views that are written do not overlap. */
+typedef struct ttkv_heads {
+  void *data;       /* [device] */
+  int32_t fmt;      /* TTKV_F16, TTKV_BF16 or TTKV_F32 */
+  int32_t n_heads;
+  int64_t seq_stride, token_stride, head_stride;
+} ttkv_heads;
+
+/* Norm and position rotation of queries and keys (keys reach the cache position-encoded, Alg. 1's k_t):
+ *   y = x / sqrt(mean(x^2) + eps) * weight        over a head's 128 channels, where `norm` says so
+ *   (a, b) -> magnitude (a cos - b sin, b cos + a sin), angle = position x freq[i], for pair i of the first rotary_dim
+ *   channels: channels (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved; the channels behind pass.
+ * Angles are reduced in 64 bits (any position up to 2^53); the rest is fp32, rounded once to the destination's type. */
+typedef struct ttkv_rope {
+  int32_t rotary_dim;       /* 0 .. 128, a multiple of 16 (UNSUPPORTED otherwise) */
+  int32_t interleaved;
+  int32_t norm;             /* bit 0: queries, bit 1: keys */
+  float eps, magnitude;     /* magnitude: 1 in the usual case */
+  const double *freq;       /* [host] rotary_dim / 2 radians per token, |freq| < 1e6 */
+  const float *q_weight, *k_weight; /* [device] fp32 [128], 16-byte aligned, or NULL: ones */
+} ttkv_rope;
+
+#define TTKV_MAX_ROPE_HEADS 65536
+#define TTKV_MAX_ROPE_TOKENS (1 << 28)
+
+/* Norm and rotation of queries and / or keys in one pass (q with q_out, k with k_out, or either pair NULL).  n_seq <=
+ * TTKV_MAX_BATCH sequences of n_tokens.  All inputs have one type, all outputs one; an output may be its own input
+ * (same type and strides), other overlaps are not allowed.  Positions: positions [device] int64 [n_seq][n_tokens], or NULL:
+ * first_pos[b] + i with first_pos [host] [n_seq], or NULL: i. */
+ttkv_status ttkv_norm_rope(ttkv_handle h, const ttkv_rope *r, const ttkv_heads *q, const ttkv_heads *q_out, const ttkv_heads *k,
+                           const ttkv_heads *k_out, int32_t n_seq, int64_t n_tokens, const int64_t *first_pos,
+                           const int64_t *positions, void *stream);
+
+/* Append to an fp16 / bf16 device tier (Sec. 4.1 "newly generated tokens are appended to the fast tier") with the norm and the
+ * rotation on the way: keys normed and rotated, values as they are, both rounded to the tier's type; the queries (nullable
+ * pair) normed and rotated to q_out, of the tier's type, in the same launch.
+ *   seq     -1: every sequence (views and arrays below have batch entries); >= 0: that sequence only (one entry).
+ *   n_each  [host] tokens of each sequence, 0 .. n_tokens, or NULL: n_tokens each (a padded batch: tokens behind a
+ *           sequence's own are neither read nor written, their rows of q_out stay as they were).
+ *   positions as in ttkv_norm_rope (rows of n_tokens); first_pos NULL: behind the tokens that all tiers hold of the sequence.
+ * Other tiers, and tiers that keep mean keys: UNSUPPORTED (ttkv_norm_rope, then ttkv_quantize_append).  CAPACITY if a ring would
+ * overflow.  Updates len[]. */
+ttkv_status ttkv_rope_append(ttkv_handle h, ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_rope *r, const ttkv_heads *q,
+                             const ttkv_heads *q_out, const ttkv_heads *k, const ttkv_heads *v, int64_t n_tokens,
+                             const int64_t *n_each, const int64_t *first_pos, const int64_t *positions, void *stream);
+
+/* ---------------------------------------------------------------- a prefix that a batch shares */
+
+/* Attention of n_seq sequences' queries over ONE cached prefix, whose bytes are read once for all of them (Alg. 1's Attn on
+ * a block, for many queries).  `prefix` is a cache of batch 1, its tiers fp16 / bf16 and in device memory (UNSUPPORTED
+ * otherwise); every token is attended.
+ *   q    [device] [n_seq][n_q_heads][128], 16-byte aligned, q_fmt as in ttkv_decode_attn; n_seq up to TTKV_MAX_SHARED_SEQS,
+ *        n_seq x n_q_heads < 2^22 (UNSUPPORTED beyond)
+ *   out  [device] [n_seq][n_q_heads][128] fp32;  lse [device] [n_seq][n_q_heads] fp32 or NULL; an empty prefix gives 0 and -inf
+ *   workspace [device], ttkv_shared_workspace_bytes: the partials of the prefix's parts.
+ * out and lse of several such calls, or of one and an attention over the sequences' own tokens, are joined by
+ * ttkv_merge_partials with m = lse, l = 1, acc = out. */
+#define TTKV_MAX_SHARED_SEQS 65536
+ttkv_status ttkv_shared_attn(ttkv_handle h, const ttkv_cache *prefix, const void *q, int32_t q_fmt, int32_t n_seq, float *out,
+                             float *lse, void *workspace, size_t ws_bytes, void *stream);
+size_t ttkv_shared_workspace_bytes(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);   /* 0: invalid, or nothing needed */
+/* Parts per row that a prefix adds for n_seq sequences that take part, or -1: a workspace of ttkv_decode_step_shared holds
+ * ttkv_count_parts (of the own cache) + ttkv_prefix_parts parts (ttkv_workspace_bytes). */
+int32_t ttkv_prefix_parts(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);
+
+/* ttkv_decode_step for a batch whose sequences share a prefix: each attends the prefix, its own cache and the step's token.
+ * The prefix has the cache's head counts and softmax_scale (INVALID_ARG otherwise).  member [host] [batch]: the sequences with
+ * a non-zero entry take part, NULL: all; the others attend their own tokens alone.  k_new, v_new both NULL: attend only; with
+ * a token, tier 0 must be an fp16 / bf16 device tier of format new_fmt without mean keys (UNSUPPORTED otherwise).  Every live
+ * block is attended, host tiers in place; one stream.  Same refusals otherwise. */
+ttkv_status ttkv_decode_step_shared(ttkv_handle h, ttkv_cache *c, const ttkv_cache *prefix, const int32_t *member, const void *q,
+                                    int32_t q_fmt, const void *k_new, const void *v_new, int32_t new_fmt, float *out, float *lse,
+                                    void *workspace, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -44,6 +44,16 @@ class ttkv_stats(C.Structure):
     ]
 
 
+class ttkv_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("fmt", C.c_int32), ("n_heads", C.c_int32),
+                ("seq_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class ttkv_rope(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("norm", C.c_int32), ("eps", C.c_float), ("magnitude", C.c_float),
+                ("freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
 EXPORTS = [
     "ttkv_create", "ttkv_destroy", "ttkv_get_stats", "ttkv_reset_stats", "ttkv_status_string", "ttkv_record_bytes",
     "ttkv_locate", "ttkv_workspace_bytes", "ttkv_demote_workspace_bytes", "ttkv_append_host_workspace_bytes",
@@ -51,6 +61,8 @@ EXPORTS = [
     "ttkv_decode_attn",
     "ttkv_decode_step", "ttkv_decode_step_topk", "ttkv_decode_attn_noalloc",
     "ttkv_merge_partials", "ttkv_select_blocks", "ttkv_set_split", "ttkv_set_table_check",
+    "ttkv_norm_rope", "ttkv_rope_append", "ttkv_shared_attn", "ttkv_shared_workspace_bytes", "ttkv_prefix_parts",
+    "ttkv_decode_step_shared",
 ]
 # include/ttkv_bench.h: measurement and inspection aids, not part of the boundary
 BENCH_EXPORTS = ["ttkv_time_attn", "ttkv_time_attn_repeat", "ttkv_read_attn_timing", "ttkv_stream_read", "ttkv_staged_schedule"]
@@ -111,6 +123,14 @@ def lib():
         L.ttkv_decode_step_topk.argtypes = [p, cp, p, i32, p, p, i32, p, p, i32, p, p, i32, p, sz, p, sz, p]
         L.ttkv_merge_partials.argtypes = [p, p, p, p, i32, i32, p, i32, p, p, p]
         L.ttkv_select_blocks.argtypes = [p, cp, p, i32, i32, p, p, i32, p, sz, p]
+        hp, rp = C.POINTER(ttkv_heads), C.POINTER(ttkv_rope)
+        L.ttkv_norm_rope.argtypes = [p, rp, hp, hp, hp, hp, i32, i64, p, p, p]
+        L.ttkv_rope_append.argtypes = [p, cp, i32, i32, rp, hp, hp, hp, hp, i64, p, p, p, p]
+        L.ttkv_shared_attn.argtypes = [p, cp, p, i32, i32, p, p, p, sz, p]
+        L.ttkv_shared_workspace_bytes.argtypes = [p, cp, i32]
+        L.ttkv_shared_workspace_bytes.restype = sz
+        L.ttkv_prefix_parts.argtypes = [p, cp, i32]
+        L.ttkv_decode_step_shared.argtypes = [p, cp, cp, p, p, i32, p, p, i32, p, p, p, sz, p]
         L.ttkv_time_attn.argtypes = [p, i32]
         L.ttkv_time_attn_repeat.argtypes = [p, i32]
         L.ttkv_stream_read.argtypes = [p, p, sz, p, p]
@@ -120,7 +140,7 @@ def lib():
             f = getattr(L, name)
             if name not in ("ttkv_get_stats", "ttkv_reset_stats", "ttkv_status_string", "ttkv_record_bytes",
                             "ttkv_workspace_bytes", "ttkv_demote_workspace_bytes",
-                            "ttkv_append_host_workspace_bytes", "ttkv_count_parts"):
+                            "ttkv_append_host_workspace_bytes", "ttkv_shared_workspace_bytes", "ttkv_count_parts"):
                 f.restype = i32
         _lib = L
     return _lib
@@ -253,6 +273,39 @@ def ttkv_merge_partials(h, m, l, acc, n_parts, part_stride, n_parts_row, rows, o
 def ttkv_select_blocks(h, cache, q, q_fmt, k, sel_blocks, sel_count, sel_stride, scratch, scratch_bytes, stream):
     _check(lib().ttkv_select_blocks(h, C.byref(cache), _p(q), q_fmt, k, _p(sel_blocks), _p(sel_count), sel_stride,
                                     _p(scratch), scratch_bytes, _p(stream)), "ttkv_select_blocks")
+
+
+def _ref(s):
+    """A structure by reference, or None."""
+    return None if s is None else C.byref(s)
+
+
+def ttkv_norm_rope(h, rope, q, q_out, k, k_out, n_seq, n_tokens, first_pos, positions, stream):
+    _check(lib().ttkv_norm_rope(h, C.byref(rope), _ref(q), _ref(q_out), _ref(k), _ref(k_out), n_seq, n_tokens, _p(first_pos),
+                                _p(positions), _p(stream)), "ttkv_norm_rope")
+
+
+def ttkv_rope_append(h, cache, tier, seq, rope, q, q_out, k, v, n_tokens, n_each, first_pos, positions, stream):
+    _check(lib().ttkv_rope_append(h, C.byref(cache), tier, seq, C.byref(rope), _ref(q), _ref(q_out), _ref(k), _ref(v), n_tokens,
+                                  _p(n_each), _p(first_pos), _p(positions), _p(stream)), "ttkv_rope_append")
+
+
+def ttkv_shared_attn(h, prefix, q, q_fmt, n_seq, out, lse, workspace, ws_bytes, stream):
+    _check(lib().ttkv_shared_attn(h, C.byref(prefix), _p(q), q_fmt, n_seq, _p(out), _p(lse), _p(workspace), ws_bytes, _p(stream)),
+           "ttkv_shared_attn")
+
+
+def ttkv_shared_workspace_bytes(h, prefix, n_seq):
+    return lib().ttkv_shared_workspace_bytes(h, C.byref(prefix), n_seq)
+
+
+def ttkv_prefix_parts(h, prefix, n_seq):
+    return lib().ttkv_prefix_parts(h, C.byref(prefix), n_seq)
+
+
+def ttkv_decode_step_shared(h, cache, prefix, member, q, q_fmt, k_new, v_new, new_fmt, out, lse, workspace, ws_bytes, stream):
+    _check(lib().ttkv_decode_step_shared(h, C.byref(cache), C.byref(prefix), _p(member), _p(q), q_fmt, _p(k_new), _p(v_new), new_fmt,
+                                         _p(out), _p(lse), _p(workspace), ws_bytes, _p(stream)), "ttkv_decode_step_shared")
 
 
 def ttkv_time_attn(h, max_samples):

@@ -16,6 +16,8 @@ SOURCES = {
     "ttkv_attn.hip": [],
     "ttkv_attn_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],   # MFMA results feed vector code: keep them out of the AGPRs
     "ttkv_select.hip": ["-ffp-contract=off"],
+    "ttkv_rope.hip": [],
+    "ttkv_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_probe.hip": [],
 }
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

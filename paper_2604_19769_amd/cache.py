@@ -3,6 +3,7 @@
 forwards to the C ABI.  No arithmetic of the method lives here; every step of
 the hot path runs in the library's kernels."""
 import ctypes as C
+import functools
 from dataclasses import dataclass
 
 import numpy as np
@@ -31,8 +32,103 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _SECTION_BYTES = {"f16": (256, 0), "bf16": (256, 0), "i8": (128, 8), "i4": (64, 8), "i4t": (64, 4), "i4c": (64, 8)}
 
 
+def _on_own_device(method):
+    """The call runs with the object's device current (the default stream's handle means the current device's)."""
+    @functools.wraps(method)
+    def call(self, *args, **kw):
+        index = self.device.index
+        if index is None or torch.cuda.current_device() == index:
+            return method(self, *args, **kw)
+        with torch.cuda.device(index):
+            return method(self, *args, **kw)
+    return call
+
+
+def _stream_of(device):
+    if _raw_stream is None or device.index is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device.index)
+
+
+def _heads(x, device):
+    """A tensor [sequence][token][head][128] as the library's strided view."""
+    assert x.dim() == 4 and x.shape[3] == 128 and x.stride(3) == 1 and x.device == device, (x.shape, x.stride(), x.device)
+    return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], x.shape[2], *x.stride()[:3])
+
+
+def _host_int64(x, n):
+    """None, or n host integers as (array to keep, address)."""
+    if x is None:
+        return None, None
+    a = np.ascontiguousarray(x, np.int64)
+    assert a.shape == (n,), a.shape
+    return a, a.ctypes.data
+
+
+def _device_positions(x, n_seq, n_tokens, device):
+    if x is not None:
+        assert x.dtype == torch.int64 and x.shape == (n_seq, n_tokens) and x.is_contiguous() and x.device == device
+    return x
+
+
+class Rotary:
+    """Norm per head and position rotation of queries and keys (ttkv_norm_rope; in TieredCache.append_rotated).
+    freq: radians per token of each pair (64-bit; its length is half the number of channels that turn, a multiple of 8 up to
+    64); interleaved: pairs (2 i, 2 i + 1) instead of (i, i + len(freq)); norm: RMS norm of both queries and keys, or a pair of
+    truth values for each; q_weight, k_weight: the norms' weights [128] (None: ones)."""
+
+    def __init__(self, freq, interleaved=False, magnitude=1.0, norm=False, q_weight=None, k_weight=None, eps=1e-6, device="cuda:0"):
+        self.device = torch.device(device)
+        self.freq = np.ascontiguousarray(freq, np.float64)
+        assert self.freq.ndim == 1
+        weights = []
+        for w in (q_weight, k_weight):
+            if w is not None:
+                assert w.shape == (128,), w.shape
+                w = w.detach().to(self.device, torch.float32).contiguous().clone()
+            weights.append(w)
+        self.q_weight, self.k_weight = weights
+        norm_q, norm_k = norm if isinstance(norm, (tuple, list)) else (norm, norm)
+        self.r = B.ttkv_rope(2 * len(self.freq), int(interleaved), int(bool(norm_q)) + 2 * int(bool(norm_k)), eps, magnitude,
+                             self.freq.ctypes.data, B._p(weights[0]), B._p(weights[1]))
+        self.h = B.ttkv_create()
+
+    @staticmethod
+    def frequencies(rotary_dim=128, base=10000.0):
+        return base ** (-np.arange(0, rotary_dim, 2, dtype=np.float64) / rotary_dim)
+
+    def close(self):
+        if self.h is not None:
+            torch.cuda.synchronize(self.device)
+            B.ttkv_destroy(self.h)
+            self.h = None
+
+    @_on_own_device
+    def apply(self, q=None, k=None, first_pos=None, positions=None, q_out=None, k_out=None, dtype=None):
+        """q [B][T][Hq][128] and / or k [B][T][Hkv][128], any strides but the last, f16 / bf16 / f32 -> (q_out, k_out), new tensors
+        of `dtype` (None: the input's) unless given (an output may be its own input).  Token i of sequence b is at
+        positions[b][i] (int64 on the device), or first_pos[b] + i (host integers; None: i)."""
+        views, out = [], []
+        shape = (q if q is not None else k).shape[:2]
+        for x, y in ((q, q_out), (k, k_out)):
+            if x is not None:
+                assert x.shape[:2] == shape
+                if y is None:
+                    y = torch.empty(x.shape, dtype=dtype or x.dtype, device=self.device)
+                assert y.shape == x.shape
+                views += [_heads(x, self.device), _heads(y, self.device)]
+                out.append(y)
+            else:
+                views += [None, None]
+                out.append(None)
+        keep, first = _host_int64(first_pos, shape[0])
+        B.ttkv_norm_rope(self.h, self.r, *views, shape[0], shape[1], first, _device_positions(positions, *shape, self.device),
+                         _stream_of(self.device))
+        return tuple(out)
+
+
 class TieredCache:
-    def __init__(self, batch, n_q_heads, n_kv_heads, tiers, device="cuda:0", softmax_scale=None, n_slots=0):
+    def __init__(self, batch, n_q_heads, n_kv_heads, tiers, device="cuda:0", softmax_scale=None, n_slots=0, prefix=None, members=None):
         self.B, self.Hq, self.Hkv = batch, n_q_heads, n_kv_heads
         self.cfg = list(tiers)
         self.device = torch.device(device)
@@ -96,6 +192,22 @@ class TieredCache:
         self.sel_blocks = self.sel_count = self.sel_scratch = None
         self.out = torch.empty(batch, n_q_heads, 128, dtype=torch.float32, device=self.device)
         self.lse = torch.empty(batch, n_q_heads, dtype=torch.float32, device=self.device)
+        self.shared_out = self.shared_lse = self.shared_ws = None
+        self.prefix = self.members = None
+        if prefix is not None:
+            self.share(prefix, members)
+
+    def share(self, prefix, members=None):
+        """Attend the tokens of `prefix`, a TieredCache of batch 1 with fp16 / bf16 tiers in HBM, in front of every sequence's own
+        from now on (members: truth values, the sequences that do; None: all).  prefix None: no longer."""
+        if prefix is not None:
+            assert prefix.B == 1 and (prefix.Hq, prefix.Hkv, prefix.device) == (self.Hq, self.Hkv, self.device)
+            assert self.n_slots == 0, "a prefix goes with host tiers read in place"
+        if members is not None:
+            members = np.ascontiguousarray(np.asarray(members, bool), np.int32)
+            assert members.shape == (self.B,)
+        self.prefix, self.members = prefix, members
+        self._parts_age = None
 
     def close(self):
         if self.h is not None:
@@ -105,9 +217,7 @@ class TieredCache:
 
     # ------------------------------------------------------------------ streams
     def _compute(self):
-        if _raw_stream is None or self.device.index is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
-        return _raw_stream(self.device.index)
+        return _stream_of(self.device)
 
     def _copy(self, overlap=True):
         return self.copy_stream.cuda_stream if overlap else self._compute()
@@ -140,6 +250,33 @@ class TieredCache:
         else:
             B.ttkv_quantize_append(self.h, self.c, tier, seq, k, v, fmt, n, int(through_tiers), self._compute())
 
+    @_on_own_device
+    def append_rotated(self, rotary, k, v, q=None, q_out=None, counts=None, first_pos=None, positions=None, tier=0, seq=-1):
+        """Keys normed and rotated on their way into an fp16 / bf16 tier, values beside them, the queries normed and rotated in the
+        same launch (ttkv_rope_append).  k, v [B][T][Hkv][128], q [B][T][Hq][128], any strides but the last, f16 / bf16 / f32;
+        seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
+        Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given)."""
+        n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
+        assert k.shape == v.shape == (n, T, self.Hkv, 128)
+        dev = self.device
+        qv = qo = None
+        if q is not None:
+            assert q.shape == (n, T, self.Hq, 128)
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=torch.bfloat16 if self.cfg[tier].k_fmt == "bf16" else torch.float16, device=dev)
+            assert q_out.shape == q.shape
+            qv, qo = _heads(q, dev), _heads(q_out, dev)
+        if first_pos is None and positions is None and self.prefix is not None:
+            first_pos = sum(self.len) + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
+            first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
+        keep_n, n_each = _host_int64(counts, n)
+        keep_p, first = _host_int64(first_pos, n)
+        B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, dev), _heads(v, dev), T, n_each, first,
+                           _device_positions(positions, n, T, dev), self._compute())
+        self._parts_age = None            # lengths jump: count the parts again at the next step
+        self._until_evict = 0
+        return q_out
+
     def demote(self, overlap=True):
         """Cascade eviction through all tiers (Alg. 1, last lines)."""
         if self._demote_need is None:
@@ -161,6 +298,9 @@ class TieredCache:
     def decode(self, q, selected=None, overlap=True, new=None):
         """q [B][Hq][128] f16/bf16 on the device.  selected: None or (sel_blocks, sel_count) pinned int32 tensors.
         new: None, or (k_new, v_new) [B][Hkv][1][128] of the step's token, appended to tier 0 by the same call."""
+        if self.prefix is not None:
+            assert selected is None, "blocks are not selected behind a prefix"
+            return self._decode_shared(q, new)
         q_fmt = _Q_FMT[q.dtype]
         assert q.is_contiguous() and q.shape == (self.B, self.Hq, 128)
         sb = sc = None
@@ -203,6 +343,63 @@ class TieredCache:
                                self._compute(), self._copy(overlap))
         return self.out, self.lse
 
+    @_on_own_device
+    def _decode_shared(self, q, new):
+        """decode() of a cache with a prefix (ttkv_decode_step_shared)."""
+        q_fmt = _Q_FMT[q.dtype]
+        assert q.is_contiguous() and q.shape == (self.B, self.Hq, 128)
+        k_new, v_new = new if new is not None else (None, None)
+        fmt = q_fmt
+        if new is not None:
+            fmt = _Q_FMT[k_new.dtype]
+            assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype == v_new.dtype
+            assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128)
+        # parts per row: counted anew every 64 steps, as in decode(), or when the library finds the workspace too small
+        if new is None or self.ws is None or self._parts_age is None or self._parts_age >= 64:
+            self._count_shared(new is not None)
+            self._parts_age = 0 if new is not None else None
+        else:
+            self._parts_age += 1
+        members = None if self.members is None else self.members.ctypes.data
+        while True:
+            try:
+                B.ttkv_decode_step_shared(self.h, self.c, self.prefix.c, members, q, q_fmt, k_new, v_new, fmt, self.out, self.lse, self.ws,
+                                          self.ws.numel(), self._compute())
+                return self.out, self.lse
+            except B.TTKVError as e:
+                if e.status != B.ERR_WORKSPACE or self._parts_age in (None, 0):
+                    raise
+                self._count_shared(new is not None)
+                self._parts_age = 0
+
+    def _count_shared(self, with_token):
+        if with_token:
+            self.len[0] += 1            # size the workspace for the lengths the attention may see
+        own = B.ttkv_count_parts(self.h, self.c, None, None, 0, 0)
+        if with_token:
+            self.len[0] -= 1
+        lead = B.ttkv_prefix_parts(self.h, self.prefix.c, self.B if self.members is None else int(self.members.sum()))
+        if own < 0 or lead < 0:
+            raise B.TTKVError(B.ERR_INVALID_ARG, "ttkv_count_parts" if own < 0 else "ttkv_prefix_parts")
+        self._workspace(max(own, self._few_parts) + lead)
+
+    @_on_own_device
+    def attend_shared(self, q):
+        """Queries of any number of sequences over this cache of batch 1 as their shared prefix: q [n][Hq][128] f16 / bf16 ->
+        out [n][Hq][128], lse [n][Hq] fp32 (ttkv_shared_attn; kept for the next call, like those of decode())."""
+        q_fmt = _Q_FMT[q.dtype]
+        n = q.shape[0]
+        assert q.is_contiguous() and q.shape == (n, self.Hq, 128) and q.device == self.device
+        if self.shared_out is None or self.shared_out.shape[0] != n:
+            self.shared_out = torch.empty(n, self.Hq, 128, dtype=torch.float32, device=self.device)
+            self.shared_lse = torch.empty(n, self.Hq, dtype=torch.float32, device=self.device)
+        need = B.ttkv_shared_workspace_bytes(self.h, self.c, n)
+        if self.shared_ws is None or self.shared_ws.numel() < need:
+            self.shared_ws = torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
+        B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
+                           self._compute())
+        return self.shared_out, self.shared_lse
+
     def select(self, q, k):
         q_fmt = _Q_FMT[q.dtype]
         stride = self._select_buffers(k)
@@ -220,6 +417,7 @@ class TieredCache:
 
     def step_topk(self, q, k_new, v_new, k):
         """append -> identify + top-k + attend with the chosen ids left on the device (no host round trip)."""
+        assert self.prefix is None, "blocks are not selected behind a prefix"
         q_fmt = _Q_FMT[q.dtype]
         fmt = _Q_FMT[k_new.dtype]
         assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
@@ -269,6 +467,16 @@ class TieredCache:
         else:
             sel = self.select(q, select_k) if select_k is not None else None
             out, lse = self.decode(q, sel, overlap, new=(k_new, v_new))
+        self._evict_if_due(overlap)
+        return out, lse
+
+    def step_rotated(self, rotary, q, k, v, first_pos=None, positions=None, overlap=True):
+        """One decode step from the projections: norm and rotation -> append -> attend (the prefix too) -> evict.  q [B][1][Hq][128],
+        k, v [B][1][Hkv][128] and the positions as in append_rotated."""
+        until = self._until_evict
+        rotated = self.append_rotated(rotary, k, v, q=q, first_pos=first_pos, positions=positions)
+        self._until_evict = until         # one token per sequence: nothing jumped
+        out, lse = self.decode(rotated.view(self.B, self.Hq, 128), None, overlap)
         self._evict_if_due(overlap)
         return out, lse
 

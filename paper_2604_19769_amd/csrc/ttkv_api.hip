@@ -4,6 +4,7 @@
 #include "ttkv_internal.h"
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -1091,6 +1092,67 @@ struct TraceChain : Chain {
   hipError_t merge(const MergeArgs &) override { put(TTKV_OP_MERGE, 0, -1, -1, -1, 0); return hipSuccess; }
 };
 
+// A prefix that a batch shares: a cache of one sequence, attended by the queries of every sequence that takes part.
+struct SharedPrefix {
+  const ttkv_cache *c;
+  const int32_t *member;       // host, nullable: which sequences take part (non-zero)
+  int n_seq;                   // sequences that take part
+  int chunk[TTKV_MAX_TIERS];   // tokens per part of each tier
+  int parts;                   // per row, all tiers
+};
+static int split_of(int64_t len, int chunk) { return (int)((len + chunk - 1) / chunk); }
+// Checks a prefix for queries of type q_fmt and counts its parts; nothing is enqueued.
+static ttkv_status plan_prefix(const ttkv_cache *c, bool check_tables, int32_t q_fmt, int n_seq, SharedPrefix &P) {
+  ttkv_status st = validate_cache(c, check_tables);
+  if (st != TTKV_OK) return st;
+  if (c->batch != 1) return TTKV_ERR_INVALID_ARG;
+  P.c = c;
+  P.n_seq = n_seq;
+  P.parts = 0;
+  for (int t = 0; t < c->n_tiers; ++t) {
+    const ttkv_tier &T = c->tier[t];
+    if (T.mem != TTKV_MEM_DEVICE || !is_fp(T.k_fmt) || T.k_fmt != T.v_fmt) return TTKV_ERR_UNSUPPORTED;
+    if (T.k_fmt == TTKV_BF16 && q_fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
+    P.chunk[t] = 0;
+    if (n_seq == 0 || T.len[0] == 0) continue;
+    P.chunk[t] = shared_chunk(n_seq * (c->n_q_heads / c->n_kv_heads), c->n_kv_heads, T.len[0]);
+    P.parts += split_of(T.len[0], P.chunk[t]);
+  }
+  return TTKV_OK;
+}
+static hipError_t launch_prefix(const SharedPrefix &P, const void *q, int32_t q_fmt, float *pm, float *pl, float *pacc, int64_t part_stride,
+                                const uint8_t *member, hipStream_t s, int *nk) {
+  const ttkv_cache *c = P.c;
+  int base = 0;
+  for (int t = 0; t < c->n_tiers; ++t) {
+    if (!P.chunk[t]) continue;
+    const ttkv_tier &T = c->tier[t];
+    SharedArgs a{};
+    a.q = q;
+    a.q_fmt = q_fmt;
+    a.Hq = c->n_q_heads;
+    a.Hkv = c->n_kv_heads;
+    a.G = a.Hq / a.Hkv;
+    a.rows = P.n_seq * a.G;
+    a.chunk = P.chunk[t];
+    a.n_split = split_of(T.len[0], a.chunk);
+    a.first_tok = (int32_t)(T.start[0] % ring_tokens(T));
+    a.len = (int32_t)T.len[0];
+    a.part_base = base;
+    a.part_stride = part_stride;
+    a.scale = c->softmax_scale;
+    a.pm = pm; a.pl = pl; a.pacc = pacc;
+    a.tv = make_view(T, make_layout(T, c->n_kv_heads));
+    a.listed = member != nullptr;
+    if (member) std::copy(member, member + P.n_seq, a.member);
+    const hipError_t e = launch_shared(a, s);
+    if (e != hipSuccess) return e;
+    ++*nk;
+    base += a.n_split;
+  }
+  return hipSuccess;
+}
+
 // Attention over the cached tokens and the merge.  k_new non-null: the step's new token as well, which the merge
 // kernel adds and stores at the tail of tier 0 (an fp device tier of format new_fmt with room for it: the caller
 // has checked); len[] of tier 0 then grows by one.
@@ -1098,7 +1160,8 @@ static ttkv_status decode_impl(Handle *h, const ttkv_cache *c, const void *q, in
                                const int32_t *sel_blocks, const int32_t *sel_count, int32_t sel_stride, void *workspace,
                                size_t ws_bytes, int32_t n_slots, void *compute_, void *copy_, const void *k_new,
                                const void *v_new, int32_t new_fmt, bool check_only = false, const DevSel *ds = nullptr,
-                               Chain *trace = nullptr, bool fixed_ws = false) {
+                               Chain *trace = nullptr, bool fixed_ws = false, const SharedPrefix *prefix = nullptr) {
+  // prefix: attended too by the sequences that take part (its parts come first in their rows)
   // fixed_ws: the caller cannot bring a larger workspace; a coarser split than the default one is taken where that fits
   ttkv_status st = validate_cache(c, h ? h->check_tables : true);
   if (st != TTKV_OK) return st;
@@ -1124,13 +1187,16 @@ static ttkv_status decode_impl(Handle *h, const ttkv_cache *c, const void *q, in
   const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
   if (ws_bytes < mis + slots_bytes) return TTKV_ERR_WORKSPACE;
   const int64_t stride = (int64_t)((ws_bytes - mis - slots_bytes) / (rows * 130 * sizeof(float)));
+  // the parts of the sequences that share a prefix stand behind its own
+  const int lead = prefix ? prefix->parts : 0;
+  auto leads = [&](int b) { return prefix && (!prefix->member || prefix->member[b]) ? lead : 0; };
   // Items of 128 tokens are twice as many partials.  A cache one token longer may be beyond them, so a workspace sized for
   // the longer one holds the plan of 256-token items and not always this one.
-  if (P.few && P.max_parts > stride) build_plan(c, sel_blocks, sel_count, sel_stride, staged, 0, &P, ds, false);
+  if (P.few && P.max_parts + lead > stride) build_plan(c, sel_blocks, sel_count, sel_stride, staged, 0, &P, ds, false);
   if (fixed_ws && h->target_items == 0)
     for (int target = P.resident_items; P.max_parts > stride && target > 0; target /= 2)
       build_plan(c, sel_blocks, sel_count, sel_stride, staged, target, &P, ds);
-  if (stride < std::max(1, P.max_parts) || P.max_parts > TTKV_MAX_PARTS) return TTKV_ERR_WORKSPACE;
+  if (stride < std::max(1, P.max_parts + lead) || P.max_parts + lead > TTKV_MAX_PARTS) return TTKV_ERR_WORKSPACE;
   const int32_t part_stride = (int32_t)std::min<int64_t>(stride, TTKV_MAX_PARTS);
   if (check_only) return TTKV_OK;   // nothing enqueued so far
   if (!trace && !P.fetch.empty() && copy != compute && (st = ensure_events(h)) != TTKV_OK) return st;
@@ -1142,6 +1208,13 @@ static ttkv_status decode_impl(Handle *h, const ttkv_cache *c, const void *q, in
   float *pacc = pl + rows * part_stride;
 
   int nk = 0, nm = 0;
+  if (lead) {
+    uint8_t member[TTKV_MAX_BATCH];
+    int n = 0;
+    for (int b = 0; b < c->batch; ++b)
+      if (leads(b)) member[n++] = (uint8_t)b;
+    TTKV_HIP(h, launch_prefix(*prefix, q, q_fmt, pm, pl, pacc, part_stride, n < c->batch ? member : nullptr, compute, &nk));
+  }
   FusedArgs a{};
   a.q = q;
   a.q_fmt = q_fmt;
@@ -1205,7 +1278,7 @@ static ttkv_status decode_impl(Handle *h, const ttkv_cache *c, const void *q, in
     int items = 0;
     for (size_t i = r0; i < r1; ++i) {
       const Run &r = *order[i];
-      a.e[i - r0] = make_entry(r.tier, r.b, r.part_base, (r.no_table ? kEntryNoTable : 0) | (r.selected ? kEntrySelected : 0),
+      a.e[i - r0] = make_entry(r.tier, r.b, r.part_base + leads(r.b), (r.no_table ? kEntryNoTable : 0) | (r.selected ? kEntrySelected : 0),
                                r.no_table ? r.rec_base : r.first_tok, r.len);
       a.start[i - r0] = items;
       items += r.n_chunks;
@@ -1260,12 +1333,12 @@ static ttkv_status decode_impl(Handle *h, const ttkv_cache *c, const void *q, in
   }
   MergeArgs m{};
   m.m = pm; m.l = pl; m.acc = pacc;
-  m.n_parts = P.max_parts;
+  m.n_parts = P.max_parts + lead;
   m.part_stride = part_stride;
   m.rows = (int32_t)rows;
   m.n_parts_row = nullptr;
   m.rows_per_seq = c->n_q_heads;
-  for (int b = 0; b < c->batch; ++b) m.cnt[b] = P.parts[b];
+  for (int b = 0; b < c->batch; ++b) m.cnt[b] = P.parts[b] + leads(b);
   m.out = out;
   m.lse = lse;
   if (k_new) {
@@ -1382,6 +1455,201 @@ ttkv_status ttkv_decode_step(ttkv_handle hh, ttkv_cache *c, const void *q, int32
   if (st != TTKV_OK) return st;
   return decode_impl(h, c, q, q_fmt, out, lse, sel_blocks, sel_count, sel_stride, workspace, ws_bytes, n_slots, compute,
                      copy, nullptr, nullptr, 0);
+}
+
+int32_t ttkv_prefix_parts(ttkv_handle hh, const ttkv_cache *prefix, int32_t n_seq) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  SharedPrefix P{};
+  if (!h || n_seq < 0 || n_seq > TTKV_MAX_SHARED_SEQS || plan_prefix(prefix, h->check_tables, TTKV_BF16, n_seq, P) != TTKV_OK) return -1;
+  return P.parts;
+}
+
+size_t ttkv_shared_workspace_bytes(ttkv_handle hh, const ttkv_cache *prefix, int32_t n_seq) {
+  const int32_t parts = ttkv_prefix_parts(hh, prefix, n_seq);
+  if (parts < 0) return 0;
+  return align256((size_t)n_seq * prefix->n_q_heads * parts * 130 * sizeof(float)) + 256;
+}
+
+ttkv_status ttkv_shared_attn(ttkv_handle hh, const ttkv_cache *prefix, const void *q, int32_t q_fmt, int32_t n_seq, float *out,
+                             float *lse, void *workspace, size_t ws_bytes, void *stream_) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || (n_seq > 0 && (!q || !out)) || n_seq < 0 || n_seq > TTKV_MAX_SHARED_SEQS || (q_fmt != TTKV_F16 && q_fmt != TTKV_BF16)) return TTKV_ERR_INVALID_ARG;
+  SharedPrefix P{};
+  const ttkv_status st = plan_prefix(prefix, h->check_tables, q_fmt, n_seq, P);
+  if (st != TTKV_OK) return st;
+  if ((uintptr_t)q & 15) return TTKV_ERR_INVALID_ARG;
+  if (n_seq == 0) return TTKV_OK;
+  if ((int64_t)n_seq * prefix->n_q_heads >= 1 << 22) return TTKV_ERR_UNSUPPORTED;
+  const int64_t rows = (int64_t)n_seq * prefix->n_q_heads, stride = std::max(1, P.parts);
+  const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
+  if (P.parts && (!workspace || ws_bytes < mis + (size_t)rows * stride * 130 * sizeof(float))) return TTKV_ERR_WORKSPACE;
+  hipStream_t stream = (hipStream_t)stream_;
+  float *pm = (float *)((uint8_t *)workspace + mis), *pl = pm + rows * stride, *pacc = pl + rows * stride;
+  int nk = 0;
+  TTKV_HIP(h, launch_prefix(P, q, q_fmt, pm, pl, pacc, stride, nullptr, stream, &nk));
+  MergeArgs m{};
+  m.m = pm; m.l = pl; m.acc = pacc;
+  m.n_parts = m.cnt[0] = P.parts;
+  m.part_stride = (int32_t)stride;
+  m.rows = (int32_t)rows;
+  m.out = out;
+  m.lse = lse;
+  TTKV_HIP(h, launch_merge(m, stream));
+  h->stats.kernels += nk + 1;
+  return TTKV_OK;
+}
+
+ttkv_status ttkv_decode_step_shared(ttkv_handle hh, ttkv_cache *c, const ttkv_cache *prefix, const int32_t *member, const void *q,
+                                    int32_t q_fmt, const void *k_new, const void *v_new, int32_t new_fmt, float *out, float *lse,
+                                    void *workspace, size_t ws_bytes, void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || (k_new == nullptr) != (v_new == nullptr)) return TTKV_ERR_INVALID_ARG;
+  ttkv_status st = validate_cache(c, h->check_tables);
+  if (st != TTKV_OK) return st;
+  if (!q || ((uintptr_t)q & 15) || (q_fmt != TTKV_F16 && q_fmt != TTKV_BF16)) return TTKV_ERR_INVALID_ARG;
+  SharedPrefix P{};
+  P.member = member;
+  int n_seq = 0;
+  for (int b = 0; b < c->batch; ++b) n_seq += !member || member[b];
+  st = plan_prefix(prefix, h->check_tables, q_fmt, n_seq, P);
+  if (st != TTKV_OK) return st;
+  if (prefix->n_q_heads != c->n_q_heads || prefix->n_kv_heads != c->n_kv_heads || prefix->softmax_scale != c->softmax_scale)
+    return TTKV_ERR_INVALID_ARG;
+  if (k_new) {
+    if (new_fmt != TTKV_F16 && new_fmt != TTKV_BF16) return TTKV_ERR_INVALID_ARG;
+    const ttkv_tier &T0 = c->tier[0];
+    for (int b = 0; b < c->batch; ++b)
+      if (T0.len[b] + 1 > ring_tokens(T0)) return TTKV_ERR_CAPACITY;
+    if (T0.mem != TTKV_MEM_DEVICE || T0.k_fmt != new_fmt || T0.v_fmt != new_fmt || T0.k_sum) return TTKV_ERR_UNSUPPORTED;
+  }
+  return decode_impl(h, c, q, q_fmt, out, lse, nullptr, nullptr, 0, workspace, ws_bytes, 0, stream, stream, k_new, v_new, new_fmt, false,
+                     nullptr, nullptr, false, &P);
+}
+
+// ---------------------------------------------------------------- norm, rotation, append
+namespace {
+size_t elem_of(int32_t fmt) { return fmt == TTKV_F32 ? 4 : 2; }
+bool is_value_fmt(int32_t fmt) { return fmt == TTKV_F16 || fmt == TTKV_BF16 || fmt == TTKV_F32; }
+// A view's address and strides in bytes; the strides of dimensions of one entry do not matter.
+ttkv_status read_heads(const ttkv_heads *v, int64_t n_seq, int64_t n_tokens, bool written, int64_t out[3], uint8_t **data) {
+  if ((!v->data && n_seq * n_tokens > 0) || !is_value_fmt(v->fmt) || v->n_heads < 1 || v->n_heads > TTKV_MAX_ROPE_HEADS) return TTKV_ERR_INVALID_ARG;
+  const int64_t n[3] = {n_seq, n_tokens, v->n_heads}, s[3] = {v->seq_stride, v->token_stride, v->head_stride};
+  if ((uintptr_t)v->data & 15) return TTKV_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i) {
+    out[i] = 0;
+    if (n[i] <= 1) continue;
+    if (s[i] < (written ? TTKV_HEAD_DIM : 0) || s[i] > ((int64_t)1 << 58)) return TTKV_ERR_INVALID_ARG;   // rows do not overlap where they are written
+    out[i] = s[i] * (int64_t)elem_of(v->fmt);
+    if (out[i] & 15) return TTKV_ERR_INVALID_ARG;
+  }
+  *data = (uint8_t *)v->data;
+  return TTKV_OK;
+}
+ttkv_status read_side(RopeSide &s, const ttkv_heads *in, const ttkv_heads *out, int64_t n_seq, int64_t n_tokens) {
+  int64_t st[3];
+  uint8_t *data;
+  ttkv_status e = read_heads(in, n_seq, n_tokens, false, st, &data);
+  if (e != TTKV_OK) return e;
+  s.src = data; s.src_seq = st[0]; s.src_token = st[1]; s.src_head = st[2];
+  s.n_heads = in->n_heads;
+  if (!out) return TTKV_OK;
+  e = read_heads(out, n_seq, n_tokens, true, st, &data);
+  if (e != TTKV_OK) return e;
+  if (out->n_heads != in->n_heads) return TTKV_ERR_INVALID_ARG;
+  s.dst = data; s.dst_seq = st[0]; s.dst_token = st[1]; s.dst_head = st[2];
+  return TTKV_OK;
+}
+ttkv_status read_rope(RopeArgs &a, const ttkv_rope *r) {
+  if (!r || r->rotary_dim < 0 || r->rotary_dim > TTKV_HEAD_DIM || (r->rotary_dim && !r->freq)) return TTKV_ERR_INVALID_ARG;
+  if (r->rotary_dim % 16) return TTKV_ERR_UNSUPPORTED;
+  if (!(r->eps >= 0.0f) || (r->norm & ~3)) return TTKV_ERR_INVALID_ARG;
+  if (((uintptr_t)r->q_weight | (uintptr_t)r->k_weight) & 15) return TTKV_ERR_INVALID_ARG;
+  a.turning = r->rotary_dim / 16;
+  a.interleaved = r->interleaved != 0;
+  a.magnitude = r->magnitude;
+  a.eps = r->eps;
+  for (int i = 0; i < r->rotary_dim / 2; ++i) {
+    if (!(std::fabs(r->freq[i]) < 1e6)) return TTKV_ERR_INVALID_ARG;   // NaN and infinities too
+    // times 1 / (2 pi), both in two numbers: turns of far positions are exact to 2^-100 of themselves
+    const double hi = r->freq[i] * 0.15915494309189535;
+    a.turns[i] = hi;
+    a.turns_rest[i] = std::fma(r->freq[i], 0.15915494309189535, -hi) + r->freq[i] * -9.839338337591243e-18;
+  }
+  a.side[0].norm = r->norm & 1;
+  a.side[1].norm = r->norm >> 1 & 1;
+  a.side[0].weight = r->q_weight;
+  a.side[1].weight = r->k_weight;
+  return TTKV_OK;
+}
+}  // namespace
+
+ttkv_status ttkv_norm_rope(ttkv_handle hh, const ttkv_rope *r, const ttkv_heads *q, const ttkv_heads *q_out, const ttkv_heads *k,
+                           const ttkv_heads *k_out, int32_t n_seq, int64_t n_tokens, const int64_t *first_pos, const int64_t *positions,
+                           void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || (!q && !k) || !q != !q_out || !k != !k_out) return TTKV_ERR_INVALID_ARG;
+  if (n_seq < 0 || n_seq > TTKV_MAX_BATCH || n_tokens < 0 || n_tokens > TTKV_MAX_ROPE_TOKENS) return TTKV_ERR_INVALID_ARG;
+  RopeArgs a{};
+  ttkv_status st = read_rope(a, r);
+  if (st != TTKV_OK) return st;
+  if (q && (st = read_side(a.side[0], q, q_out, n_seq, n_tokens)) != TTKV_OK) return st;
+  if (k && (st = read_side(a.side[1], k, k_out, n_seq, n_tokens)) != TTKV_OK) return st;
+  if (q && k && (q->fmt != k->fmt || q_out->fmt != k_out->fmt)) return TTKV_ERR_UNSUPPORTED;
+  if (n_seq == 0 || n_tokens == 0) return TTKV_OK;
+  a.positions = positions;
+  a.pos_stride = n_tokens;
+  for (int j = 0; j < n_seq; ++j) {
+    a.first_pos[j] = first_pos ? first_pos[j] : 0;
+    a.count[j] = (int32_t)n_tokens;
+  }
+  TTKV_HIP(h, launch_rope(a, n_seq, n_tokens, q ? q->fmt : k->fmt, q ? q_out->fmt : k_out->fmt, (hipStream_t)stream));
+  h->stats.kernels += 1;
+  return TTKV_OK;
+}
+
+ttkv_status ttkv_rope_append(ttkv_handle hh, ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_rope *r, const ttkv_heads *q,
+                             const ttkv_heads *q_out, const ttkv_heads *k, const ttkv_heads *v, int64_t n_tokens, const int64_t *n_each,
+                             const int64_t *first_pos, const int64_t *positions, void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h) return TTKV_ERR_INVALID_ARG;
+  ttkv_status st = validate_cache(c, h->check_tables);
+  if (st != TTKV_OK) return st;
+  if (tier < 0 || tier >= c->n_tiers || seq < -1 || seq >= c->batch || !k || !v || !q != !q_out) return TTKV_ERR_INVALID_ARG;
+  if (n_tokens < 0 || n_tokens > TTKV_MAX_ROPE_TOKENS) return TTKV_ERR_INVALID_ARG;
+  ttkv_tier &T = c->tier[tier];
+  if (T.mem != TTKV_MEM_DEVICE || !is_fp(T.k_fmt) || T.k_fmt != T.v_fmt || T.k_sum) return TTKV_ERR_UNSUPPORTED;
+  const int b0 = seq < 0 ? 0 : seq, n_seq = seq < 0 ? c->batch : 1;
+  RopeArgs a{};
+  if ((st = read_rope(a, r)) != TTKV_OK) return st;
+  if (q && (st = read_side(a.side[0], q, q_out, n_seq, n_tokens)) != TTKV_OK) return st;
+  if ((st = read_side(a.side[1], k, nullptr, n_seq, n_tokens)) != TTKV_OK) return st;
+  if ((st = read_side(a.side[2], v, nullptr, n_seq, n_tokens)) != TTKV_OK) return st;
+  if (k->n_heads != c->n_kv_heads || v->n_heads != c->n_kv_heads) return TTKV_ERR_INVALID_ARG;
+  if (k->fmt != v->fmt || (q && (q->fmt != k->fmt || q_out->fmt != T.k_fmt))) return TTKV_ERR_UNSUPPORTED;
+  const Layout L = make_layout(T, c->n_kv_heads);
+  a.in_tier = 1;
+  a.tier = make_view(T, L);
+  a.positions = positions;
+  a.pos_stride = n_tokens;
+  int64_t most = 0;
+  for (int j = 0; j < n_seq; ++j) {
+    const int b = b0 + j;
+    const int64_t n = n_each ? n_each[j] : n_tokens;
+    if (n < 0 || n > n_tokens) return TTKV_ERR_INVALID_ARG;
+    if (T.len[b] + n > ring_tokens(T)) return TTKV_ERR_CAPACITY;
+    most = std::max(most, n);
+    int64_t held = 0;
+    for (int t = 0; t < c->n_tiers; ++t) held += c->tier[t].len[b];
+    a.first_pos[j] = first_pos ? first_pos[j] : held;
+    a.count[j] = (int32_t)n;
+    a.seq_id[j] = b;
+    a.dst_first_tok[j] = (int32_t)((T.start[b] + T.len[b]) % ring_tokens(T));
+  }
+  if (most == 0) return TTKV_OK;
+  TTKV_HIP(h, launch_rope(a, n_seq, most, k->fmt, T.k_fmt, (hipStream_t)stream));
+  h->stats.kernels += 1;
+  for (int j = 0; j < n_seq; ++j) T.len[b0 + j] += a.count[j];
+  return TTKV_OK;
 }
 
 ttkv_status ttkv_merge_partials(ttkv_handle hh, const float *m, const float *l, const float *acc, int32_t n_parts,

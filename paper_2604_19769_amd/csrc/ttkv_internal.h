@@ -317,6 +317,50 @@ struct SelectArgs {
 };
 hipError_t launch_select(const SelectArgs &a, hipStream_t s);
 
+// Norm, rotation and append in one pass (rope_kernel).  Strides in bytes.
+struct RopeSide {   // queries, keys, values
+  const uint8_t *src;
+  uint8_t *dst;     // unused by keys and values that go to a tier
+  int64_t src_seq, src_token, src_head, dst_seq, dst_token, dst_head;
+  const float *weight;   // [128], nullable: ones
+  int32_t n_heads, norm;
+};
+struct RopeArgs {
+  RopeSide side[3];
+  int32_t first_batch[3], n_batches;   // batches of eight heads of a token
+  int32_t wave_shift;                  // log2 of the waves that share a token's batches
+  int32_t turning, interleaved;        // channels that turn / 16
+  int32_t in_tier;
+  float magnitude, eps;
+  const int64_t *positions;            // device, nullable: first_pos[entry] + token
+  int64_t pos_stride;
+  TierView tier;
+  int64_t first_pos[TTKV_MAX_BATCH];
+  int32_t count[TTKV_MAX_BATCH], seq_id[TTKV_MAX_BATCH], dst_first_tok[TTKV_MAX_BATCH];   // tokens, sequence and first ring token per entry
+  double turns[64], turns_rest[64];    // frequency of pair i in turns per token, and what the first number leaves out
+};
+static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments are passed by value");
+hipError_t launch_rope(RopeArgs &a, int n_seq, int64_t n_tokens, int src_fmt, int dst_fmt, hipStream_t s);
+
+// Attention of many query rows over one run of tokens of one fp tier (shared_kernel).
+struct SharedArgs {
+  const void *q;                 // [sequence][Hq][128]
+  int32_t q_fmt, Hq, Hkv, G;
+  int32_t rows;                  // query rows per KV head: sequences that take part x G
+  int32_t row_tiles, n_split, chunk;   // workgroups along the rows and the tokens; tokens of one
+  int32_t first_tok, len;        // ring token and length of the run
+  int32_t part_base;
+  int64_t part_stride;
+  float scale;
+  int32_t listed;                // the taking part are member[0 .. ), else sequences 0, 1, ..
+  float *pm, *pl, *pacc;
+  TierView tv;
+  uint8_t member[TTKV_MAX_BATCH];
+};
+// How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part (a multiple of 128).
+int shared_chunk(int rows, int n_kv_heads, int64_t len);
+hipError_t launch_shared(SharedArgs &a, hipStream_t s);
+
 // Load-only kernel over `bytes` (rounded down to 64 KiB) of device memory; sink: 4 writable bytes.
 hipError_t launch_stream_read(const void *src, int64_t bytes, uint32_t *sink, hipStream_t s);
 

@@ -1,0 +1,228 @@
+// Between the projections and the cache: RMS norm of queries and keys per head, position rotation, and the rows' way into
+// a tier, in one pass over them.
+//
+//   y = x rsqrt(mean(x^2) + eps) w         over one head's 128 channels (optional per side)
+//   angle_i = pos freq_i;  c_i = magnitude cos, s_i = magnitude sin
+//   (a, b) -> (a c - b s, b c + a s)       for the pairs (i, i + R/2), or (2 i, 2 i + 1); channels from R on pass
+//
+// A wave takes one token and eight heads at a time, eight lanes per head.  Lane j of a head holds the two 16-byte pieces that
+// contain pairs 8 j .. 8 j + 7: pieces j and j + R/16 of the row's sixteen (pairs half a rotation apart), or 2 j and 2 j + 1 (side
+// by side), so a rotation needs no exchange between lanes; lanes from R/16 on hold pieces that pass.  The wave's 64 lanes work
+// out one angle each and hand them to the eight heads through LDS.  Angles are counted in turns: pos x (freq / 2 pi)
+// with the factor in two 64-bit numbers and the product's rounding taken back, so what is left after the whole turns is right at any
+// position (one 64-bit product alone would be 1e-4 off at 2^40); everything else is fp32, rounded once to the destination's type.
+#include "ttkv_internal.h"
+
+#include <hip/hip_fp16.h>
+
+#include <algorithm>
+
+namespace ttkv {
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+
+template <int F>
+constexpr int elem_bytes() { return F == TTKV_F32 ? 4 : 2; }
+
+// Eight channels as they lie.
+template <int F>
+struct Piece {
+  u32x4 w[F == TTKV_F32 ? 2 : 1];
+};
+template <int F>
+__device__ __forceinline__ Piece<F> load_piece(const uint8_t *row, int piece) {
+  Piece<F> p;
+  const u32x4 *s = (const u32x4 *)(row + piece * 8 * elem_bytes<F>());
+#pragma unroll
+  for (int i = 0; i < elem_bytes<F>() / 2; ++i) p.w[i] = s[i];
+  return p;
+}
+template <int F>
+__device__ __forceinline__ void expand(const Piece<F> &p, float (&x)[8]) {
+  if constexpr (F == TTKV_F32) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(p.w[i / 4][i % 4]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = p.w[0][i];
+      if constexpr (F == TTKV_F16) {
+        const h2 v = __builtin_bit_cast(h2, u);
+        x[2 * i] = (float)v.x;
+        x[2 * i + 1] = (float)v.y;
+      } else {
+        x[2 * i] = __uint_as_float(u << 16);
+        x[2 * i + 1] = __uint_as_float(u & 0xffff0000u);
+      }
+    }
+  }
+}
+template <int F>
+__device__ __forceinline__ void store_piece(uint8_t *row, int piece, const float (&x)[8]) {
+  u32x4 *d = (u32x4 *)(row + piece * 8 * elem_bytes<F>());
+  if constexpr (F == TTKV_F32) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      d[i] = u32x4{__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3])};
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {   // nearest even
+      const f2 v = {x[2 * i], x[2 * i + 1]};
+      if constexpr (F == TTKV_F16) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
+      else w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
+    }
+    d[0] = u32x4{w[0], w[1], w[2], w[3]};
+  }
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum_of_eight_lanes(float v) {
+  v += dpp<0xB1>(v);            // quad_perm [1,0,3,2]
+  v += dpp<0x4E>(v);            // quad_perm [2,3,0,1]
+  return v + dpp<0x141>(v);     // row_half_mirror
+}
+
+template <int SRC, int DST>
+__global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
+  __shared__ f2 s_turn[4][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int j = blockIdx.y;
+  const int64_t w = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t token = w >> a.wave_shift;
+  const int part = (int)(w - (token << a.wave_shift)), parts = 1 << a.wave_shift;
+  if (token >= a.count[j]) return;    // whole waves leave together; no barriers
+
+  if (lane < 8 * a.turning) {
+#pragma clang fp contract(off)
+    const int64_t pos = a.positions ? a.positions[(int64_t)j * a.pos_stride + token] : a.first_pos[j] + token;
+    const double x = (double)pos, turns = x * a.turns[lane];
+    const float r = (float)((turns - __builtin_rint(turns)) + (__builtin_fma(x, a.turns[lane], -turns) + x * a.turns_rest[lane]));
+    float s, c;
+    sincospif(2.0f * r, &s, &c);
+    s_turn[wave][lane] = f2{c * a.magnitude, s * a.magnitude};
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int l8 = lane & 7, slot = lane >> 3;
+  const bool turns_here = l8 < a.turning;
+  f2 cs[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) cs[i] = turns_here ? s_turn[wave][8 * l8 + i] : f2{1.0f, 0.0f};
+  const bool side_by_side = a.interleaved || !turns_here;
+  const int p0 = side_by_side ? 2 * l8 : l8, p1 = side_by_side ? 2 * l8 + 1 : l8 + a.turning;
+
+  uint8_t *head0 = nullptr;   // the token's place in the tier
+  int64_t head_step = 0;
+  int64_t v_off = 0;
+  if (a.in_tier) {
+    const TierView &tv = a.tier;
+    int64_t tok = a.dst_first_tok[j] + token;
+    const int64_t ring = (int64_t)tv.ring_blocks * tv.bt;
+    if (tok >= ring) tok -= ring;
+    const int r = div_bt((int)tok, tv.bt, tv.bt_magic), row = (int)tok - r * tv.bt;
+    const int64_t at = (int64_t)a.seq_id[j] * tv.ring_blocks + r;
+    const int64_t rec = tv.table ? (int64_t)tv.table[at] : at;
+    head0 = tv.base + rec * tv.rec_bytes + row * 256;
+    head_step = tv.head_bytes;
+    v_off = tv.v_off;
+  }
+
+  for (int b = part; b < a.n_batches; b += parts) {
+    const int side = b >= a.first_batch[2] ? 2 : b >= a.first_batch[1] ? 1 : 0;   // queries, keys, values
+    const RopeSide &s = a.side[side];
+    const int h = (b - a.first_batch[side]) * 8 + slot;
+    const bool live = h < s.n_heads;
+    const uint8_t *src = s.src + j * s.src_seq + token * s.src_token + (live ? h : 0) * s.src_head;
+    const Piece<SRC> w0 = load_piece<SRC>(src, p0), w1 = load_piece<SRC>(src, p1);
+    float x[8], y[8];
+    expand<SRC>(w0, x);
+    expand<SRC>(w1, y);
+    if (side < 2) {
+      if (s.norm) {
+        float sq = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+        const float inv = 1.0f / sqrtf(sum_of_eight_lanes(sq) * (1.0f / 128.0f) + a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x[i] *= inv;
+          y[i] *= inv;
+        }
+        if (s.weight) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] *= s.weight[8 * p0 + i];
+            y[i] *= s.weight[8 * p1 + i];
+          }
+        }
+      }
+      if (turns_here) {
+        if (a.interleaved) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
+            x[2 * i] = x0 * cs[i].x - x1 * cs[i].y;
+            x[2 * i + 1] = x1 * cs[i].x + x0 * cs[i].y;
+            y[2 * i] = y0 * cs[4 + i].x - y1 * cs[4 + i].y;
+            y[2 * i + 1] = y1 * cs[4 + i].x + y0 * cs[4 + i].y;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float u = x[i], v = y[i];
+            x[i] = u * cs[i].x - v * cs[i].y;
+            y[i] = v * cs[i].x + u * cs[i].y;
+          }
+        }
+      }
+    }
+    if (!live) continue;
+    uint8_t *dst = a.in_tier && side ? head0 + h * head_step + (side == 2 ? v_off : 0)
+                                     : s.dst + j * s.dst_seq + token * s.dst_token + h * s.dst_head;
+    store_piece<DST>(dst, p0, x);
+    store_piece<DST>(dst, p1, y);
+  }
+}
+
+template <int SRC>
+void launch_from(const RopeArgs &a, int dst, dim3 grid, hipStream_t s) {
+  switch (dst) {
+    case TTKV_F16: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_F16>), grid, dim3(256), 0, s, a); break;
+    case TTKV_BF16: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_BF16>), grid, dim3(256), 0, s, a); break;
+    default: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_F32>), grid, dim3(256), 0, s, a); break;
+  }
+}
+
+}  // namespace
+
+// a.count: tokens per entry, at most n_tokens.
+hipError_t launch_rope(RopeArgs &a, int n_seq, int64_t n_tokens, int src_fmt, int dst_fmt, hipStream_t s) {
+  int n = 0;
+  for (int i = 0; i < 3; ++i) {
+    a.first_batch[i] = n;
+    n += (a.side[i].n_heads + 7) / 8;
+  }
+  a.n_batches = n;
+  // A wave works its angles out once for all its heads; where there are too few tokens to fill the chip (eight waves per
+  // CU's four SIMDs) they are shared out over more waves.
+  a.wave_shift = 0;
+  while ((1 << a.wave_shift) < n && ((n_tokens * n_seq) << a.wave_shift) < 8192) ++a.wave_shift;
+  const dim3 grid((unsigned)(((n_tokens << a.wave_shift) + 3) / 4), n_seq);
+  switch (src_fmt) {
+    case TTKV_F16: launch_from<TTKV_F16>(a, dst_fmt, grid, s); break;
+    case TTKV_BF16: launch_from<TTKV_BF16>(a, dst_fmt, grid, s); break;
+    default: launch_from<TTKV_F32>(a, dst_fmt, grid, s); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ttkv

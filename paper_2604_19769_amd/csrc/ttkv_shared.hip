@@ -12,14 +12,14 @@
 // (ds_read_b64_tr_b16: four tokens of one channel per lane).
 //
 // A workgroup's four waves are RW along the rows (32 each) times TW along the tokens of a tile; K and V tiles go global ->
-// registers -> LDS, the next tile's loads in flight while one is computed.  LDS rows keep their sixteen 16-byte pieces in the
-// order p ^ swz(row), which spreads both products' reads over the banks.
+// registers -> LDS, the next tile's loads in flight while one is computed.
 //
-// The weights p carry 2^14 and meet fp16 values as an fp16 number and its remainder (22 bits), bf16 values as three bf16
+// The weights p meet fp16 values as an fp16 number and its remainder (22 bits), bf16 values as three bf16
 // numbers (24 bits): the outputs are fp32.
 #include "ttkv_attn_dev.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace ttkv {
 
@@ -51,215 +51,144 @@ __device__ __forceinline__ f2 unpack2(uint32_t w) {
   if constexpr (BF) return f2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
   else return f2{(float)as_h2(w).x, (float)as_h2(w).y};
 }
-// Sixteen rows that differ in their low four bits keep a piece in sixteen places; rows 4 r .. 4 r + 3 in four pairs of places.
-__device__ __forceinline__ int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1) | (row & 8); }
+// x - the lower (upper) half of w
+__device__ __forceinline__ float minus_low(uint32_t w, float x) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(x));
+  return r;
+}
+__device__ __forceinline__ float minus_high(uint32_t w, float x) {
+  float r;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(x));
+  return r;
+}
+// LDS rows: eight rows' 16-byte pieces of one column fall into different banks (keys, 4 banks apart), and so do four rows' 32
+// bytes (values, 8 banks apart); every address is one register and a constant.
+constexpr int kRowK = 272, kRowV = 288;
 
+// The weights carry 2^kUnit, and the reference moves only when a score is kRoom (in powers of two) above it: the weights stay below
+// 2^15, and a wave of 32 rows, some of whose maxima would grow in nearly every step, hardly ever rescales its outputs.
+constexpr float kUnit = 8.0f, kRoom = 7.0f;
+template <bool BF>
+constexpr int parts_of() { return BF ? 3 : 2; }   // numbers that hold a weight
 constexpr int kTile(int tw) { return tw == 4 ? 128 : 64; }   // tokens in LDS at a time
 
-template <bool BF, int RW, int TW>
-__global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
-  static_assert(RW * TW == 4, "four waves");
-  constexpr int TILE = kTile(TW), SUB = TILE / (32 * TW), NL = TILE / 16;   // 32-token steps of a wave per tile; 16-byte loads of K (V) per thread
-  constexpr int NP = BF ? 3 : 2;                                            // numbers that hold a weight
-  __shared__ __align__(16) char s_tile[2 * TILE * 256];   // K rows, V rows; at the end partial outputs, 16 KiB per row block
-  char *const s_k = s_tile, *const s_v = s_tile + TILE * 256;
-  static_assert(2 * TILE * 256 >= RW * 64 * 64 * 4 || TW == 1, "room for the partial outputs");
-  __shared__ float s_m[4][32], s_l[4][32];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rw = wave % RW, tw = wave / RW;
-  const int c = lane & 31, hh = lane >> 5;
-  // workgroups that read the same tokens of a KV head lie on one XCD, one behind the other
-  const int x8 = blockIdx.x >> 3, unit = x8 / a.row_tiles * 8 + (blockIdx.x & 7), rt = x8 % a.row_tiles;
-  if (unit >= a.n_split * a.Hkv) return;
-  const int split = unit / a.Hkv, hkv = unit - split * a.Hkv;
-  const int t_begin = split * a.chunk, n_tok = min(a.chunk, a.len - t_begin);   // at least 1
-
-  // ---- queries: the lane's row, channels 16 kb + 8 hh .. + 7 per step
-  const int row = (rt * RW + rw) * 32 + c;
-  const bool row_on = row < a.rows;
-  const int row_in = min(row, a.rows - 1);
-  const int n = row_in / a.G, seq = a.listed ? a.member[n] : n, hq = hkv * a.G + row_in - n * a.G;
-  u32x4 qf[8];
-  {
-    const u32x4 *qp = (const u32x4 *)((const uint16_t *)a.q + ((int64_t)seq * a.Hq + hq) * 128);
+// What a wave keeps of its 32 query rows beside the outputs: lane -> row lane % 32, both halves alike but for l.
+struct Rows {
+  float cs, inv_cs;                        // scores are kept in the log2 domain
+  float m, l, mcs, f, far;                 // a token's weight: exp2(score cs + mcs) = 2^f e^(score - m); a score beyond `far` moves m
+  int seq, hq;
+  bool on;
+};
+// Row `row` of the KV head's rows (the last one again behind them) and its channels 16 kb + 8 hh .. + 7 in qf[kb].
+template <bool BF>
+__device__ __forceinline__ Rows begin_rows(const SharedArgs &a, int row, int hkv, int hh, u32x4 (&qf)[8]) {
+  Rows r;
+  r.on = row < a.rows;
+  row = min(row, a.rows - 1);
+  const int n = row / a.G;
+  r.seq = a.listed ? a.member[n] : n;
+  r.hq = hkv * a.G + row - n * a.G;
+  const u32x4 *qp = (const u32x4 *)((const uint16_t *)a.q + ((int64_t)r.seq * a.Hq + r.hq) * 128);
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) qf[kb] = qp[2 * kb + hh];
-    if (!BF && a.q_fmt == TTKV_BF16) {   // bf16 -> fp16 (exact inside the fp16 normal range, clamped outside)
+  for (int kb = 0; kb < 8; ++kb) qf[kb] = qp[2 * kb + hh];
+  if (!BF && a.q_fmt == TTKV_BF16) {   // bf16 -> fp16 (exact inside the fp16 normal range, clamped outside)
 #pragma unroll
-      for (int kb = 0; kb < 8; ++kb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f2 v = unpack2<true>(qf[kb][i]);
-          qf[kb][i] = pack2<false>(fminf(fmaxf(v.x, -65504.0f), 65504.0f), fminf(fmaxf(v.y, -65504.0f), 65504.0f));
-        }
-    }
-  }
-  const float cs = a.scale * kLog2e;   // scores are kept in the log2 domain
-
-  f16v o[4];
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  float m = -INFINITY, l = 0.0f, mcs = 0.0f, f = 0.0f;   // a token's weight: exp2(score cs + mcs) = 2^f e^(score - m)
-
-  // ---- tiles: thread -> row (threadIdx / 16) + 16 i, piece threadIdx % 16
-  const int ring = a.tv.ring_blocks * a.tv.bt, lr = threadIdx.x >> 4, lp = threadIdx.x & 15;
-  u32x4 kr[NL], vr[NL];
-  auto load = [&](int t0) {   // tokens t0 .. of the item; rows behind its end repeat its last one
-#pragma unroll
-    for (int g = 0; g < TILE / 64; ++g) {
-      const int live0 = (n_tok - 1) & ~63;
-      const int at = min(t0 + 64 * g, live0);
-      const int last = n_tok - 1 - at;
-      int tok = a.first_tok + t_begin + at;
-      if (tok >= ring) tok -= ring;
-      const int rb = div_bt(tok, a.tv.bt, a.tv.bt_magic), row0 = tok - rb * a.tv.bt;
-      const int64_t rec = a.tv.table ? (int64_t)a.tv.table[rb] : (int64_t)rb;
-      const uint8_t *head = a.tv.base + rec * a.tv.rec_bytes + (int64_t)hkv * a.tv.head_bytes + row0 * 256;
+    for (int kb = 0; kb < 8; ++kb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = min(lr + 16 * i, last);
-        const uint8_t *p = head + r * 256 + lp * 16;
-        kr[4 * g + i] = *(const u32x4 *)p;
-        vr[4 * g + i] = *(const u32x4 *)(p + a.tv.v_off);
+        const f2 v = unpack2<true>(qf[kb][i]);
+        qf[kb][i] = pack2<false>(fminf(fmaxf(v.x, -65504.0f), 65504.0f), fminf(fmaxf(v.y, -65504.0f), 65504.0f));
       }
-    }
-  };
-  const int n_tiles = (n_tok + TILE - 1) / TILE;
-  load(0);
-  for (int t = 0; t < n_tiles; ++t) {
-    __syncthreads();
+  }
+  r.cs = a.scale * kLog2e;
+  r.inv_cs = 1.0f / r.cs;
+  r.m = r.far = -INFINITY;
+  r.l = r.mcs = r.f = 0.0f;
+  return r;
+}
+// The largest of a step's scores, in both halves.
+__device__ __forceinline__ float step_max(const f16v &sc) {
+  float mt = sc[0];
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int r = lr + 16 * i, at = r * 256 + ((lp ^ swz(r)) << 4);
-      *(u32x4 *)(s_k + at) = kr[i];
-      *(u32x4 *)(s_v + at) = vr[i];
-    }
-    __syncthreads();
-    if (t + 1 < n_tiles) load((t + 1) * TILE);
+  for (int i = 1; i < 16; ++i) mt = fmaxf(mt, sc[i]);
+  const f2 both = both32(mt);
+  return fmaxf(both.x, both.y);
+}
+__device__ __forceinline__ void rescale(f16v (&o)[4], float by) {
 #pragma unroll
-    for (int s = 0; s < SUB; ++s) {
-      const int t0 = (tw * SUB + s) * 32;                 // the step's first token in the tile
-      const int left = n_tok - t * TILE - t0;             // live tokens from it on
-      if (left <= 0) break;                               // (wave-uniform)
-      f16v sc;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[i] = 0.0f;
-#pragma unroll
-      for (int kb = 0; kb < 8; ++kb) {
-        const int r = t0 + c;
-        sc = mma<BF>(*(const u32x4 *)(s_k + r * 256 + (((2 * kb + hh) ^ swz(r)) << 4)), qf[kb], sc);
-      }
-      if (left < 32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (8 * (i / 4) + 4 * hh + i % 4 >= left) sc[i] = -INFINITY;
-      }
-      float mt = sc[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mt = fmaxf(mt, sc[i]);
-      const f2 both = both32(mt);
-      mt = fmaxf(both.x, both.y);
-      if (__any(mt > m)) {
+  for (int d = 0; d < 4; ++d) o[d] *= by;
+}
+// The reference moves up to the largest score so far.
+__device__ __forceinline__ void move_reference(Rows &r, float mt, f16v (&o)[4]) {
 #pragma clang fp contract(off)
-        const float mn = fmaxf(m, mt), r = mn * cs, was = mcs;
-        f = fabsf(r) < 4194304.0f ? 14.0f : 0.0f;   // beyond, f - mcs would not be exact
-        mcs = mn == -INFINITY ? 0.0f : f - r;
-        const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mcs - was);
-        l *= alpha;
+  const float mn = fmaxf(r.m, mt), at = mn * r.cs, was = r.mcs;
+  r.f = fabsf(at) < 4194304.0f ? kUnit : 0.0f;   // beyond, f - mcs would not be exact
+  r.mcs = mn == -INFINITY ? 0.0f : r.f - at;
+  const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.mcs - was);
+  r.l *= alpha;
+  rescale(o, alpha);
+  r.m = mn;
+  r.far = r.f == 0.0f ? mn : (at + kRoom) * r.inv_cs;
+}
+// Scores of tokens from `left` on count nothing.
+__device__ __forceinline__ void mask_step(f16v &sc, int left, int hh) {
 #pragma unroll
-        for (int d = 0; d < 4; ++d) o[d] *= alpha;
-        m = mn;
-      }
-      u32x4 p[NP][2];   // [part of the weight][16 tokens]
+  for (int i = 0; i < 16; ++i) {
+    if (8 * (i / 4) + 4 * hh + i % 4 >= left) sc[i] = -INFINITY;
+    asm volatile("" : "+v"(sc[i]));   // stays a branch, not sixteen selects in every step
+  }
+}
+// Weights 2 i and 2 i + 1 of a step as NP packed numbers each.
+template <bool BF>
+__device__ __forceinline__ void weigh(Rows &r, const f16v &sc, int i, u32x4 (&p)[parts_of<BF>()][2]) {
+  float w0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], r.cs, r.mcs)), w1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], r.cs, r.mcs));
+  r.l += w0 + w1;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float w0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], cs, mcs)), w1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], cs, mcs));
-        l += w0 + w1;
-#pragma unroll
-        for (int u = 0; u < NP; ++u) {
-          const uint32_t w = pack2<BF>(w0, w1);
-          p[u][i / 4][i % 4] = w;
-          const f2 x = unpack2<BF>(w);
-          w0 -= x.x;
-          w1 -= x.y;
-        }
-      }
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          u32x4 va;
-#pragma unroll
-          for (int jb = 0; jb < 2; ++jb) {
-            const int r = t0 + 16 * b + 8 * jb + 4 * hh + ((lane & 15) >> 2);
-            const int piece = 4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-            const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((las_s4)(s_v + r * 256 + ((piece ^ swz(r)) << 4) + (lane & 1) * 8));
-            const u32x2 y = __builtin_bit_cast(u32x2, x);
-            va[2 * jb] = y.x;
-            va[2 * jb + 1] = y.y;
-          }
-#pragma unroll
-          for (int u = 0; u < NP; ++u) o[d] = mma<BF>(va, p[u][b], o[d]);
-        }
+  for (int u = 0; u < parts_of<BF>(); ++u) {
+    const uint32_t w = pack2<BF>(w0, w1);
+    p[u][i / 4][i % 4] = w;
+    if constexpr (BF) {
+      const f2 x = unpack2<true>(w);
+      w0 -= x.x;
+      w1 -= x.y;
+    } else {
+      w0 = minus_low(w, w0);
+      w1 = minus_high(w, w1);
     }
   }
-  {   // the halves' sums, without the power of two
-    const f2 both = both32(l);
-    const float unit = f == 0.0f ? 1.0f : 0x1p-14f;
-    l = (both.x + both.y) * unit;
+}
+// Value operand: channels 32 d .. + 31 (rows), tokens of half b in the order of the scores' registers.
+__device__ __forceinline__ u32x4 value_operand(const char *v_at, int d, int b) {
+  u32x4 va;
 #pragma unroll
-    for (int d = 0; d < 4; ++d) o[d] *= unit;
+  for (int jb = 0; jb < 2; ++jb) {
+    const s4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((las_s4)(v_at + (16 * b + 8 * jb) * kRowV + 64 * d));
+    const u32x2 y = __builtin_bit_cast(u32x2, x);
+    va[2 * jb] = y.x;
+    va[2 * jb + 1] = y.y;
   }
-
-  // ---- the waves of one row block join
-  float ref = m == -INFINITY ? -INFINITY : f - mcs;   // the weights are exp2(score cs - ref) ...
-  if constexpr (TW > 1) {
-    float *const s_o = (float *)s_tile;   // [row block][channel register][lane]
-    __syncthreads();
-    if (hh == 0) {
-      s_m[wave][c] = ref;
-      s_l[wave][c] = l;
-    }
-    __syncthreads();
-    float top = -INFINITY;
+  return va;
+}
+template <bool BF>
+__device__ __forceinline__ void add_values(f16v &o, const u32x4 &va, const u32x4 (&p)[parts_of<BF>()][2], int b) {
 #pragma unroll
-    for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
-    const float mine = ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top);
-    float sum = 0.0f;
-#pragma unroll
-    for (int u = 0; u < TW; ++u) {
-      const float mu = s_m[u * RW + rw][c];
-      sum += mu == -INFINITY ? 0.0f : s_l[u * RW + rw][c] * __builtin_amdgcn_exp2f(mu - top);
-    }
-    l = sum;
-    ref = top;
-#pragma unroll
-    for (int d = 0; d < 4; ++d) o[d] *= mine;
-    for (int u = 1; u < TW; ++u) {
-      __syncthreads();
-      if (tw == u) {
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s_o[(rw * 64 + d * 16 + i) * 64 + lane] = o[d][i];
-      }
-      __syncthreads();
-      if (tw == 0) {
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] += s_o[(rw * 64 + d * 16 + i) * 64 + lane];
-      }
-    }
-    if (tw > 0) return;
-  }
-  if (!row_on) return;
-  const int64_t at = ((int64_t)seq * a.Hq + hq) * a.part_stride + a.part_base + split;
+  for (int u = 0; u < parts_of<BF>(); ++u) o = mma<BF>(va, p[u][b], o);
+}
+// Reference of the wave's sums (in log2: weights are exp2(score cs - reference)); l over both halves, l and o without 2^f.
+__device__ __forceinline__ float end_rows(Rows &r, f16v (&o)[4]) {
+  const f2 both = both32(r.l);
+  const float unit = r.f == 0.0f ? 1.0f : 0x1p-8f;
+  r.l = (both.x + both.y) * unit;
+  rescale(o, unit);
+  return r.m == -INFINITY ? -INFINITY : r.f - r.mcs;
+}
+__device__ __forceinline__ void store_part(const SharedArgs &a, const Rows &r, float ref, const f16v (&o)[4], int split, int hh) {
+  if (!r.on) return;
+  const int64_t at = ((int64_t)r.seq * a.Hq + r.hq) * a.part_stride + a.part_base + split;
   if (hh == 0) {
-    a.pm[at] = ref * kLn2;          // ... = e^(score scale - ref ln 2)
-    a.pl[at] = l;
+    a.pm[at] = ref * kLn2;
+    a.pl[at] = r.l;
   }
   float *po = a.pacc + at * 128;
 #pragma unroll
@@ -267,38 +196,343 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) po[32 * d + 8 * (i / 4) + 4 * hh + i % 4] = o[d][i];
 }
+// A place in the run: the KV head's part of a ring block and a row of it.  Everything a step further needs is kept in scalar
+// registers, and the block table is read once per block: a scalar load in every step would be waited for together with the
+// LDS reads that are in flight.
+// Addresses are numbers until a load: a pointer that has been through a register constraint is loaded by flat instructions,
+// which the LDS waits wait for as well.
+typedef const __attribute__((address_space(1))) u32x4 *gas_u32x4;
+typedef const __attribute__((address_space(4))) int32_t *const_i32;
+struct Cursor {
+  uint64_t base, head;   // the KV head's part of record 0, and of the block's
+  uint64_t table;        // written before the launch: read through the constant address space
+  int64_t rec_bytes;
+  int bt, ring_blocks, block, row;
+  __device__ __forceinline__ void find() { head = base + (table ? (int64_t)((const_i32)table)[block] : (int64_t)block) * rec_bytes; }
+  __device__ __forceinline__ Cursor(const SharedArgs &a, int hkv, int token) {   // a multiple of 32
+    bt = a.tv.bt;
+    ring_blocks = a.tv.ring_blocks;
+    rec_bytes = a.tv.rec_bytes;
+    table = (uint64_t)a.tv.table;
+    base = (uint64_t)a.tv.base + (int64_t)hkv * a.tv.head_bytes;
+    int tok = a.first_tok + token;
+    if (tok >= ring_blocks * bt) tok -= ring_blocks * bt;
+    block = div_bt(tok, bt, a.tv.bt_magic);
+    row = tok - block * bt;
+    asm volatile("" : "+s"(bt), "+s"(ring_blocks), "+s"(rec_bytes), "+s"(table), "+s"(base));
+    find();
+  }
+  __device__ __forceinline__ void advance(int rows) {   // up to the next block
+    row += rows;
+    if (row < bt) return;
+    row = 0;
+    block = block + 1 == ring_blocks ? 0 : block + 1;
+    find();
+  }
+  __device__ __forceinline__ uint64_t rows() const { return head + row * 256; }
+};
+// workgroups that read the same tokens of a KV head lie on one XCD, one behind the other
+struct Item {
+  int row_tile, split, hkv, begin, n_tok;
+};
+__device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it) {
+  const int x8 = blockIdx.x >> 3, unit = x8 / a.row_tiles * 8 + (blockIdx.x & 7);
+  it.row_tile = x8 % a.row_tiles;
+  it.split = unit / a.Hkv;
+  it.hkv = unit - it.split * a.Hkv;
+  it.begin = it.split * a.chunk;
+  it.n_tok = min(a.chunk, a.len - it.begin);   // at least 1
+  return unit < a.n_split * a.Hkv;
+}
+// the lane's place in a step's keys and values
+__device__ __forceinline__ int k_lane(int lane) { return (lane & 31) * kRowK + 16 * (lane >> 5); }
+__device__ __forceinline__ int v_lane(int lane) { return (4 * (lane >> 5) + ((lane & 15) >> 2)) * kRowV + 32 * ((lane >> 4) & 1) + 8 * (lane & 3); }
 
+// The TW waves of one row block add up in the first of them: returns the common reference.  s_o: RW x 16 KiB; all waves of the
+// workgroup take part.
+template <int RW, int TW>
+__device__ __forceinline__ float join(Rows &r, float ref, f16v (&o)[4], int rw, int tw, int lane, float *s_o, float (*s_m)[32], float (*s_l)[32]) {
+  const int c = lane & 31, wave = tw * RW + rw;
+  __syncthreads();   // everybody is done with the tiles
+  if (lane < 32) {
+    s_m[wave][c] = ref;
+    s_l[wave][c] = r.l;
+  }
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
+  float sum = 0.0f;
+#pragma unroll
+  for (int u = 0; u < TW; ++u) {
+    const float mu = s_m[u * RW + rw][c];
+    sum += mu == -INFINITY ? 0.0f : s_l[u * RW + rw][c] * __builtin_amdgcn_exp2f(mu - top);
+  }
+  r.l = sum;
+  rescale(o, ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top));
+  for (int u = 1; u < TW; ++u) {
+    if (u > 1) __syncthreads();
+    if (tw == u) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s_o[(rw * 64 + d * 16 + i) * 64 + lane] = o[d][i];
+    }
+    __syncthreads();
+    if (tw == 0) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] += s_o[(rw * 64 + d * 16 + i) * 64 + lane];
+    }
+  }
+  return top;
+}
+
+// ---------------------------------------------------------------- up to 64 rows per KV head
+template <bool BF, int RW, int TW>
+__global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
+  static_assert(RW * TW == 4 && TW > 1, "four waves");
+  constexpr int TILE = kTile(TW), SUB = TILE / (32 * TW), NL = TILE / 16;   // 32-token steps of a wave per tile; 16-byte loads of K (V) per thread
+  static_assert(SUB == 1, "one step per tile and wave");
+  constexpr int kBuffer = TILE * (kRowK + kRowV), NBUF = TW == 4 ? 1 : 2;   // two workgroups per CU either way
+  __shared__ __align__(16) char s_tile[NBUF * kBuffer];   // K rows, V rows per buffer; at the end partial outputs, 16 KiB per row block
+  static_assert(NBUF * kBuffer >= RW * 64 * 64 * 4, "room for the partial outputs");
+  __shared__ float s_m[4][32], s_l[4][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rw = wave % RW, tw = wave / RW;
+  const int c = lane & 31, hh = lane >> 5;
+  Item it;
+  if (!item_of(a, it)) return;
+  u32x4 qf[8];
+  Rows r = begin_rows<BF>(a, (it.row_tile * RW + rw) * 32 + c, it.hkv, hh, qf);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+
+  // ---- tiles: thread -> row (threadIdx / 16) + 16 i, piece threadIdx % 16
+  const int lr = threadIdx.x >> 4, lp = threadIdx.x & 15;
+  u32x4 kr[NL], vr[NL];
+  Cursor at(a, it.hkv, it.begin);
+  int to_load = it.n_tok;     // tokens from the cursor on
+  const int v_off = a.tv.v_off;
+  auto load = [&]() {   // the next tile; rows behind the item's end repeat its last one
+#pragma unroll
+    for (int g = 0; g < TILE / 64; ++g) {
+      const uint64_t head = at.rows();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t p = head + (uint32_t)(min(lr + 16 * i, to_load - 1) * 256 + lp * 16);
+        kr[4 * g + i] = __builtin_nontemporal_load((gas_u32x4)p);   // read once
+        vr[4 * g + i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
+      }
+      if (to_load > 64) {
+        to_load -= 64;
+        at.advance(64);
+      }
+    }
+  };
+  const int n_tiles = (it.n_tok + TILE - 1) / TILE, first = tw * 32;   // the wave's first token in a tile
+  const char *const k_at = s_tile + first * kRowK + k_lane(lane), *const v_at = s_tile + TILE * kRowK + first * kRowV + v_lane(lane);
+  char *const k_put = s_tile + lr * kRowK + lp * 16, *const v_put = s_tile + TILE * kRowK + lr * kRowV + lp * 16;
+  auto put = [&](int buffer) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      *(u32x4 *)(k_put + buffer + i * 16 * kRowK) = kr[i];
+      *(u32x4 *)(v_put + buffer + i * 16 * kRowV) = vr[i];
+    }
+  };
+  load();
+  put(0);
+  int buffer = 0;
+  for (int t = 0; t < n_tiles; ++t) {
+    if (NBUF == 2) __syncthreads();     // tile t is in its buffer; everybody is done with the other one
+    if (t + 1 < n_tiles) load();
+    if (NBUF == 1) __syncthreads();
+    const int left = it.n_tok - t * TILE - first;
+    if (left > 0) {   // (wave-uniform)
+      f16v sc = {};
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb) sc = mma<BF>(*(const u32x4 *)(k_at + buffer + 32 * kb), qf[kb], sc);
+      if (left < 32) mask_step(sc, left, hh);
+      const float mt = step_max(sc);
+      if (__any(mt > r.far)) move_reference(r, mt, o);
+      u32x4 p[parts_of<BF>()][2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) weigh<BF>(r, sc, i, p);
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + buffer, d, b), p, b);
+    }
+    if (NBUF == 1) __syncthreads();
+    if (t + 1 < n_tiles) {
+      if (NBUF == 2) buffer = kBuffer - buffer;
+      put(buffer);
+    }
+  }
+  const float ref = end_rows(r, o);
+  const float top = join<RW, TW>(r, ref, o, rw, tw, lane, (float *)s_tile, s_m, s_l);
+  if (tw == 0) store_part(a, r, top, o, it.split, hh);
+}
+
+// ---------------------------------------------------------------- more rows: 128 per workgroup
+// Bound: the matrix cores.  The steps of 32 tokens overlap inside a wave: while the softmax of step s runs on the vector unit, the
+// matrix cores work on the values of step s - 1 and the scores of step s + 1, none of which depends on it.  LDS holds two
+// steps' keys and values each (s + 1 and s + 2; s - 1 and s), one barrier per step.
+template <bool BF>
+__global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a) {
+  constexpr int NP = parts_of<BF>(), kKeys = 32 * kRowK, kValues = 32 * kRowV, kHalf = 2 * (kKeys + kValues);
+  __shared__ __align__(16) char s_tile[2 * kHalf];   // per half: keys of even and odd steps, values of even and odd steps
+  static_assert(2 * kHalf >= 4 * 64 * 64 * 4, "room for the partial outputs");
+  __shared__ float s_m[8][32], s_l[8][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = lane & 31, hh = lane >> 5, rw = wave & 3, half = wave >> 2;
+  Item it;
+  if (!item_of(a, it)) return;
+  // Four waves take the item's first half, four the second; one without tokens looks at a live one that counts nothing.
+  const int n_half = a.chunk / 2, n_steps = ((min(it.n_tok, n_half) + 31) / 32 + 1) & ~1;   // in pairs: the last ones may have no live token
+  const int n_tok = half ? max(it.n_tok - n_half, 0) : min(it.n_tok, n_half);
+  if (half && n_tok) it.begin += n_half;
+  const int lr = threadIdx.x >> 4 & 15, lp = threadIdx.x & 15;
+  char *const s_half = s_tile + half * kHalf;
+  const char *const k_at = s_half + k_lane(lane), *const v_at = s_half + 2 * kKeys + v_lane(lane);
+  char *const k_put = s_half + lr * kRowK + lp * 16, *const v_put = s_half + 2 * kKeys + lr * kRowV + lp * 16;
+  u32x4 kr[2], vr[2];
+  // rows lr and lr + 16 of the next step; behind the item's end rows of its last one again
+  Cursor keys(a, it.hkv, it.begin), values = keys;
+  values.base += a.tv.v_off;
+  values.head += a.tv.v_off;
+  int k_left = max(n_tok, 1), v_left = k_left;   // tokens from the cursors on
+  auto load = [&](Cursor &at, int &left, u32x4 (&x)[2]) __attribute__((always_inline)) {
+    const uint64_t head = at.rows();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = *(gas_u32x4)(head + (uint32_t)(min(lr + 16 * i, left - 1) * 256 + lp * 16));
+    if (left > 32) {
+      left -= 32;
+      at.advance(32);
+    }
+  };
+  auto load_keys = [&]() __attribute__((always_inline)) { load(keys, k_left, kr); };
+  auto load_values = [&]() __attribute__((always_inline)) { load(values, v_left, vr); };
+  auto put_keys = [&](int odd) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(u32x4 *)(k_put + odd * kKeys + i * 16 * kRowK) = kr[i];
+  };
+  auto put_values = [&](int odd) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(u32x4 *)(v_put + odd * kValues + i * 16 * kRowV) = vr[i];
+  };
+  // everything that the first steps need is asked for at once
+  u32x4 first[2][2];
+  load(keys, k_left, first[0]);
+  load(keys, k_left, first[1]);
+  load_keys();
+  load_values();
+  u32x4 qf[8];
+  Rows r = begin_rows<BF>(a, (it.row_tile * 4 + rw) * 32 + c, it.hkv, hh, qf);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+  // Step s (of parity ODD): sc its scores, p the weights of step s - 1; next, pn receive the scores of s + 1 and its own weights.
+  auto body = [&](int s, auto odd_tag, f16v &sc, f16v &next, u32x4 (&p)[NP][2], u32x4 (&pn)[NP][2]) __attribute__((always_inline)) {
+    constexpr int ODD = decltype(odd_tag)::value;
+    __syncthreads();   // keys of s + 1 and values of s - 1 are there; everybody is done with those of s and s - 2
+    const char *const v_old = v_at + (1 - ODD) * kValues, *const k_next = k_at + (1 - ODD) * kKeys;
+    const float mt = step_max(sc);
+    if (__any(mt > r.far)) {   // the outputs take the weights of the old reference first; what is added below is then nothing
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_old, d, b), p, b);
+      move_reference(r, mt, o);
+#pragma unroll
+      for (int u = 0; u < NP; ++u) p[u][0] = p[u][1] = u32x4{0, 0, 0, 0};
+    }
+    put_keys(ODD);       // of s + 2
+    put_values(ODD);     // of s
+    load_keys();         // of s + 3
+    load_values();       // of s + 1
+    f16v nx = {};
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {   // a product of the scores, two or three of the values, an eighth of the softmax
+      add_values<BF>(o[g / 2], value_operand(v_old, g / 2, g % 2), p, g % 2);
+      nx = mma<BF>(*(const u32x4 *)(k_next + 32 * g), qf[g], nx);
+      weigh<BF>(r, sc, g, pn);
+    }
+    const int left = n_tok - 32 * (s + 1);
+    if (left < 32) mask_step(nx, left, hh);
+    next = nx;
+  };
+  u32x4 p0[NP][2], p1[NP][2];
+#pragma unroll
+  for (int u = 0; u < NP; ++u) p0[u][0] = p0[u][1] = u32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int odd = 0; odd < 2; ++odd)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      *(u32x4 *)(k_put + odd * kKeys + i * 16 * kRowK) = first[odd][i];
+      if (odd) *(u32x4 *)(v_put + kValues + i * 16 * kRowV) = u32x4{0, 0, 0, 0};   // there is no step before the first: weights of zero meet zeros
+    }
+  __syncthreads();
+  f16v s0 = {}, s1;
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) s0 = mma<BF>(*(const u32x4 *)(k_at + 32 * kb), qf[kb], s0);
+  if (n_tok < 32) mask_step(s0, n_tok, hh);
+  for (int s = 0; s < n_steps; s += 2) {
+    body(s, std::integral_constant<int, 0>{}, s0, s1, p0, p1);
+    body(s + 1, std::integral_constant<int, 1>{}, s1, s0, p1, p0);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + kValues, d, b), p0, b);
+  const float ref = end_rows(r, o), top = join<4, 2>(r, ref, o, rw, half, lane, (float *)s_tile, s_m, s_l);
+  if (half == 0) store_part(a, r, top, o, it.split, hh);
+}
+
+// Query rows per workgroup, workgroups along the rows.
 struct Shape {
-  int rw, row_tiles;
+  int rows, row_tiles, resident;   // resident: workgroups on the chip at once
 };
 Shape shape_of(int rows) {
-  if (rows <= 32) return Shape{1, 1};
-  if (rows <= 64) return Shape{2, 1};
-  return Shape{4, (rows + 127) / 128};
+  if (rows <= 32) return Shape{32, 1, 512};
+  if (rows <= 64) return Shape{64, 1, 512};
+  return Shape{128, (rows + 127) / 128, 256};
 }
 
 }  // namespace
 
 int shared_chunk(int rows, int n_kv_heads, int64_t len) {
   const Shape s = shape_of(rows);
-  const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
+  const int64_t want = std::max<int64_t>(1, s.resident / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
   return (int)(((len + want - 1) / want + 127) / 128 * 128);
 }
 
 hipError_t launch_shared(SharedArgs &a, hipStream_t s) {
   const Shape sh = shape_of(a.rows);
   a.row_tiles = sh.row_tiles;
-  const dim3 grid((unsigned)(((int64_t)a.n_split * a.Hkv + 7) / 8 * 8 * sh.row_tiles));
+  const dim3 grid((unsigned)(((int64_t)a.n_split * a.Hkv + 7) / 8 * 8 * sh.row_tiles)), block(256);
   const bool bf = a.tv.k_fmt == TTKV_BF16;
-#define TTKV_SHARED(RW, TW)                                                                          \
-  if (bf) hipLaunchKernelGGL((shared_kernel<true, RW, TW>), grid, dim3(256), 0, s, a);              \
-  else hipLaunchKernelGGL((shared_kernel<false, RW, TW>), grid, dim3(256), 0, s, a)
-  switch (sh.rw) {
-    case 1: TTKV_SHARED(1, 4); break;
-    case 2: TTKV_SHARED(2, 2); break;
-    default: TTKV_SHARED(4, 1); break;
+  switch (sh.rows) {
+    case 32:
+      if (bf) hipLaunchKernelGGL((shared_kernel<true, 1, 4>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((shared_kernel<false, 1, 4>), grid, block, 0, s, a);
+      break;
+    case 64:
+      if (bf) hipLaunchKernelGGL((shared_kernel<true, 2, 2>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((shared_kernel<false, 2, 2>), grid, block, 0, s, a);
+      break;
+    default:
+      if (bf) hipLaunchKernelGGL(shared_rows_kernel<true>, grid, dim3(512), 0, s, a);
+      else hipLaunchKernelGGL(shared_rows_kernel<false>, grid, dim3(512), 0, s, a);
+      break;
   }
-#undef TTKV_SHARED
   return hipGetLastError();
 }
 

@@ -348,6 +348,7 @@ struct SharedArgs {
   int32_t q_fmt, Hq, Hkv, G;
   int32_t rows;                  // query rows per KV head: sequences that take part x G
   int32_t row_tiles, n_split, chunk;   // workgroups along the rows and the tokens; tokens of one
+  uint32_t g_magic, hkv_magic, tiles_magic;   // divisions by G, Hkv and row_tiles by a multiplication; 0: by a division
   int32_t first_tok, len;        // ring token and length of the run
   int32_t part_base;
   int64_t part_stride;
@@ -357,7 +358,7 @@ struct SharedArgs {
   TierView tv;
   uint8_t member[TTKV_MAX_BATCH];
 };
-// How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part (a multiple of 128).
+// How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part (a multiple of 64).
 int shared_chunk(int rows, int n_kv_heads, int64_t len);
 hipError_t launch_shared(SharedArgs &a, hipStream_t s);
 

@@ -32,6 +32,7 @@ typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) s4 *las_s4;
+typedef float float4_any __attribute__((ext_vector_type(4), aligned(4)));   // the partials may start at any float
 
 template <bool BF>
 __device__ __forceinline__ f16v mma(const u32x4 &a, const u32x4 &b, const f16v &c) {
@@ -86,7 +87,7 @@ __device__ __forceinline__ Rows begin_rows(const SharedArgs &a, int row, int hkv
   Rows r;
   r.on = row < a.rows;
   row = min(row, a.rows - 1);
-  const int n = row / a.G;
+  const int n = a.G == 1 ? row : a.g_magic ? (int)mul_high((uint32_t)row, a.g_magic) : row / a.G;
   r.seq = a.listed ? a.member[n] : n;
   r.hq = hkv * a.G + row - n * a.G;
   const u32x4 *qp = (const u32x4 *)((const uint16_t *)a.q + ((int64_t)r.seq * a.Hq + r.hq) * 128);
@@ -175,26 +176,9 @@ __device__ __forceinline__ void add_values(f16v &o, const u32x4 &va, const u32x4
 #pragma unroll
   for (int u = 0; u < parts_of<BF>(); ++u) o = mma<BF>(va, p[u][b], o);
 }
-// Reference of the wave's sums (in log2: weights are exp2(score cs - reference)); l over both halves, l and o without 2^f.
-__device__ __forceinline__ float end_rows(Rows &r, f16v (&o)[4]) {
+__device__ __forceinline__ void end_rows(Rows &r) {   // l over both halves
   const f2 both = both32(r.l);
-  const float unit = r.f == 0.0f ? 1.0f : 0x1p-8f;
-  r.l = (both.x + both.y) * unit;
-  rescale(o, unit);
-  return r.m == -INFINITY ? -INFINITY : r.f - r.mcs;
-}
-__device__ __forceinline__ void store_part(const SharedArgs &a, const Rows &r, float ref, const f16v (&o)[4], int split, int hh) {
-  if (!r.on) return;
-  const int64_t at = ((int64_t)r.seq * a.Hq + r.hq) * a.part_stride + a.part_base + split;
-  if (hh == 0) {
-    a.pm[at] = ref * kLn2;
-    a.pl[at] = r.l;
-  }
-  float *po = a.pacc + at * 128;
-#pragma unroll
-  for (int d = 0; d < 4; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) po[32 * d + 8 * (i / 4) + 4 * hh + i % 4] = o[d][i];
+  r.l = both.x + both.y;
 }
 // A place in the run: the KV head's part of a ring block and a row of it.  Everything a step further needs is kept in scalar
 // registers, and the block table is read once per block: a scalar load in every step would be waited for together with the
@@ -222,11 +206,13 @@ struct Cursor {
     asm volatile("" : "+s"(bt), "+s"(ring_blocks), "+s"(rec_bytes), "+s"(table), "+s"(base));
     find();
   }
-  __device__ __forceinline__ void advance(int rows) {   // up to the next block
+  __device__ __forceinline__ void advance(int rows) {   // up to two blocks on
     row += rows;
     if (row < bt) return;
-    row = 0;
-    block = block + 1 == ring_blocks ? 0 : block + 1;
+    do {
+      row -= bt;
+      block = block + 1 == ring_blocks ? 0 : block + 1;
+    } while (row >= bt);
     find();
   }
   __device__ __forceinline__ uint64_t rows() const { return head + row * 256; }
@@ -236,9 +222,14 @@ struct Item {
   int row_tile, split, hkv, begin, n_tok;
 };
 __device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it) {
-  const int x8 = blockIdx.x >> 3, unit = x8 / a.row_tiles * 8 + (blockIdx.x & 7);
-  it.row_tile = x8 % a.row_tiles;
-  it.split = unit / a.Hkv;
+  // all that the look-ups read, asked for at once: a launch's arguments are in no cache when its first workgroups start
+  asm volatile("" ::"s"(a.row_tiles), "s"(a.Hkv), "s"(a.chunk), "s"(a.len), "s"(a.first_tok), "s"(a.G), "s"(a.q), "s"(a.rows), "s"(a.tv.base),
+               "s"(a.tv.bt), "s"(a.part_stride), "s"(a.pm));
+  const int x8 = blockIdx.x >> 3;
+  const int x = a.row_tiles == 1 ? x8 : a.tiles_magic ? (int)mul_high((uint32_t)x8, a.tiles_magic) : x8 / a.row_tiles;
+  const int unit = 8 * x + (blockIdx.x & 7);
+  it.row_tile = x8 - x * a.row_tiles;
+  it.split = a.Hkv == 1 ? unit : a.hkv_magic ? (int)mul_high((uint32_t)unit, a.hkv_magic) : unit / a.Hkv;
   it.hkv = unit - it.split * a.Hkv;
   it.begin = it.split * a.chunk;
   it.n_tok = min(a.chunk, a.len - it.begin);   // at least 1
@@ -248,45 +239,73 @@ __device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it) {
 __device__ __forceinline__ int k_lane(int lane) { return (lane & 31) * kRowK + 16 * (lane >> 5); }
 __device__ __forceinline__ int v_lane(int lane) { return (4 * (lane >> 5) + ((lane & 15) >> 2)) * kRowV + 32 * ((lane >> 4) & 1) + 8 * (lane & 3); }
 
-// The TW waves of one row block add up in the first of them: returns the common reference.  s_o: RW x 16 KiB; all waves of the
-// workgroup take part.
+// The TW waves of one row block add up, each 128 / TW channels of the rows, and store them.  s_o: (4 - 4 / TW) x 4 KiB per wave; all
+// waves of the workgroup take part.  Weights of a wave are exp2(score cs + mcs).
 template <int RW, int TW>
-__device__ __forceinline__ float join(Rows &r, float ref, f16v (&o)[4], int rw, int tw, int lane, float *s_o, float (*s_m)[32], float (*s_l)[32]) {
-  const int c = lane & 31, wave = tw * RW + rw;
+__device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &r, const f16v (&o)[4], int rw, int tw, int lane, int split, char *s_o,
+                                               float (*s_m)[32], float (*s_l)[32]) {
+  constexpr int OWN = 4 / TW;   // blocks of 32 channels that a wave ends up with
+  const int c = lane & 31, hh = lane >> 5;
   __syncthreads();   // everybody is done with the tiles
-  if (lane < 32) {
-    s_m[wave][c] = ref;
-    s_l[wave][c] = r.l;
+  if (hh == 0) {
+    s_m[tw * RW + rw][c] = r.m == -INFINITY ? -INFINITY : -r.mcs;
+    s_l[tw * RW + rw][c] = r.l;
   }
+  // what the other waves of the row block need: [giver][taker, without the giver][block][quarter][lane]
+  auto place = [&](int giver, int taker, int e, int k) __attribute__((always_inline)) -> float4 * {
+    const int slot = taker - (taker > giver);
+    return (float4 *)(s_o + (((((giver * RW + rw) * (TW - 1) + slot) * OWN + e) * 4 + k) * 64 + lane) * 16);
+  };
+#pragma unroll
+  for (int t = 0; t < TW; ++t)
+    if (t != tw)
+#pragma unroll
+      for (int e = 0; e < OWN; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const f16v &x = o[t * OWN + e];
+          *place(tw, t, e, k) = float4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+        }
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
   for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
-  float sum = 0.0f;
+  // the reference without the weights' power of two (exact: top is that of some wave)
+  const float up = fabsf(top) < 4194304.0f ? kUnit : 0.0f;
+  float by[TW], l = 0.0f;
 #pragma unroll
   for (int u = 0; u < TW; ++u) {
     const float mu = s_m[u * RW + rw][c];
-    sum += mu == -INFINITY ? 0.0f : s_l[u * RW + rw][c] * __builtin_amdgcn_exp2f(mu - top);
+    by[u] = mu == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((mu - top) - up);
+    l = fmaf(s_l[u * RW + rw][c], by[u], l);
   }
-  r.l = sum;
-  rescale(o, ref == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref - top));
-  for (int u = 1; u < TW; ++u) {
-    if (u > 1) __syncthreads();
-    if (tw == u) {
+  const int64_t at = ((int64_t)r.seq * a.Hq + r.hq) * a.part_stride + a.part_base + split;
+  float *const po = a.pacc + at * 128 + 4 * hh;
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+  for (int w = 0; w < TW; ++w) {
+    if (w != tw) continue;   // (wave-uniform)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s_o[(rw * 64 + d * 16 + i) * 64 + lane] = o[d][i];
-    }
-    __syncthreads();
-    if (tw == 0) {
+    for (int e = 0; e < OWN; ++e)
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+      for (int k = 0; k < 4; ++k) {
+        const f16v &x = o[w * OWN + e];
+        float4 y = {x[4 * k] * by[w], x[4 * k + 1] * by[w], x[4 * k + 2] * by[w], x[4 * k + 3] * by[w]};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] += s_o[(rw * 64 + d * 16 + i) * 64 + lane];
-    }
+        for (int u = 0; u < TW; ++u) {
+          if (u == w) continue;
+          const float4 z = *place(u, w, e, k);
+          y.x = fmaf(z.x, by[u], y.x);
+          y.y = fmaf(z.y, by[u], y.y);
+          y.z = fmaf(z.z, by[u], y.z);
+          y.w = fmaf(z.w, by[u], y.w);
+        }
+        if (r.on) *(float4_any *)(po + 32 * (w * OWN + e) + 8 * k) = float4_any{y.x, y.y, y.z, y.w};
+      }
   }
-  return top;
+  if (r.on && hh == 0 && tw == 0) {
+    a.pm[at] = (top + up) * kLn2;   // the weights are e^(score scale - this)
+    a.pl[at] = l;
+  }
 }
 
 // ---------------------------------------------------------------- up to 64 rows per KV head
@@ -295,15 +314,52 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
   static_assert(RW * TW == 4 && TW > 1, "four waves");
   constexpr int TILE = kTile(TW), SUB = TILE / (32 * TW), NL = TILE / 16;   // 32-token steps of a wave per tile; 16-byte loads of K (V) per thread
   static_assert(SUB == 1, "one step per tile and wave");
+  constexpr bool ALONE = RW == 1;   // a wave's 32 tokens of a tile are its own: it loads and stores them itself, and waits for nobody
   constexpr int kBuffer = TILE * (kRowK + kRowV), NBUF = TW == 4 ? 1 : 2;   // two workgroups per CU either way
-  __shared__ __align__(16) char s_tile[NBUF * kBuffer];   // K rows, V rows per buffer; at the end partial outputs, 16 KiB per row block
-  static_assert(NBUF * kBuffer >= RW * 64 * 64 * 4, "room for the partial outputs");
+  __shared__ __align__(16) char s_tile[NBUF * kBuffer];   // K rows, V rows per buffer; at the end what the waves exchange
+  static_assert(NBUF * kBuffer >= 4 * (4 - 4 / TW) * 4096, "room for what the waves exchange");
   __shared__ float s_m[4][32], s_l[4][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = wave % RW, tw = wave / RW;
   const int c = lane & 31, hh = lane >> 5;
   Item it;
   if (!item_of(a, it)) return;
+  // ---- tiles: a thread's rows lr + LR i of the tile (of the wave's 32), piece lp
+  constexpr int LR = ALONE ? 4 : 16;
+  const int lr = (ALONE ? lane : (int)threadIdx.x) >> 4, lp = threadIdx.x & 15;
+  const int n_tiles = (it.n_tok + TILE - 1) / TILE, first = tw * 32;   // the wave's first token in a tile
+  const int mine = it.n_tok - first;                                   // tokens from the wave's first one on
+  u32x4 kr[NL], vr[NL];
+  Cursor at(a, it.hkv, it.begin + (ALONE && mine > 0 ? first : 0));
+  int to_load = ALONE ? max(mine, 1) : it.n_tok;     // tokens from the cursor on
+  const int v_off = a.tv.v_off;
+  auto load = [&]() __attribute__((always_inline)) {   // the next tile; rows behind the item's end repeat its last one
+    if constexpr (ALONE) {
+      const uint64_t head = at.rows();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint64_t p = head + (uint32_t)(min(lr + LR * i, to_load - 1) * 256 + lp * 16);
+        kr[i] = __builtin_nontemporal_load((gas_u32x4)p);   // read once
+        vr[i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
+      }
+      if (to_load > TILE) {
+        to_load -= TILE;
+        at.advance(TILE);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t p = at.rows() + (uint32_t)(min(lr + LR * i, to_load - 1) * 256 + lp * 16);
+        kr[i] = __builtin_nontemporal_load((gas_u32x4)p);
+        vr[i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
+      }
+      if (to_load > TILE) {
+        to_load -= TILE;
+        at.advance(TILE);
+      }
+    }
+  };
+  load();
   u32x4 qf[8];
   Rows r = begin_rows<BF>(a, (it.row_tile * RW + rw) * 32 + c, it.hkv, hh, qf);
   f16v o[4];
@@ -311,47 +367,25 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-
-  // ---- tiles: thread -> row (threadIdx / 16) + 16 i, piece threadIdx % 16
-  const int lr = threadIdx.x >> 4, lp = threadIdx.x & 15;
-  u32x4 kr[NL], vr[NL];
-  Cursor at(a, it.hkv, it.begin);
-  int to_load = it.n_tok;     // tokens from the cursor on
-  const int v_off = a.tv.v_off;
-  auto load = [&]() {   // the next tile; rows behind the item's end repeat its last one
-#pragma unroll
-    for (int g = 0; g < TILE / 64; ++g) {
-      const uint64_t head = at.rows();
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint64_t p = head + (uint32_t)(min(lr + 16 * i, to_load - 1) * 256 + lp * 16);
-        kr[4 * g + i] = __builtin_nontemporal_load((gas_u32x4)p);   // read once
-        vr[4 * g + i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
-      }
-      if (to_load > 64) {
-        to_load -= 64;
-        at.advance(64);
-      }
-    }
-  };
-  const int n_tiles = (it.n_tok + TILE - 1) / TILE, first = tw * 32;   // the wave's first token in a tile
   const char *const k_at = s_tile + first * kRowK + k_lane(lane), *const v_at = s_tile + TILE * kRowK + first * kRowV + v_lane(lane);
-  char *const k_put = s_tile + lr * kRowK + lp * 16, *const v_put = s_tile + TILE * kRowK + lr * kRowV + lp * 16;
-  auto put = [&](int buffer) {
+  const int put_row = lr + (ALONE ? first : 0);
+  char *const k_put = s_tile + put_row * kRowK + lp * 16, *const v_put = s_tile + TILE * kRowK + put_row * kRowV + lp * 16;
+  auto put = [&](int buffer) __attribute__((always_inline)) {
+    // (a wave that is alone: LDS takes its reads and stores in order, the compiler has to leave them so)
+    if constexpr (ALONE) asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      *(u32x4 *)(k_put + buffer + i * 16 * kRowK) = kr[i];
-      *(u32x4 *)(v_put + buffer + i * 16 * kRowV) = vr[i];
+      *(u32x4 *)(k_put + buffer + i * LR * kRowK) = kr[i];
+      *(u32x4 *)(v_put + buffer + i * LR * kRowV) = vr[i];
     }
+    if constexpr (ALONE) asm volatile("" ::: "memory");
   };
-  load();
   put(0);
   int buffer = 0;
   for (int t = 0; t < n_tiles; ++t) {
-    if (NBUF == 2) __syncthreads();     // tile t is in its buffer; everybody is done with the other one
+    if (!ALONE) __syncthreads();        // tile t is in its buffer; everybody is done with the other one
     if (t + 1 < n_tiles) load();
-    if (NBUF == 1) __syncthreads();
-    const int left = it.n_tok - t * TILE - first;
+    const int left = mine - t * TILE;
     if (left > 0) {   // (wave-uniform)
       f16v sc = {};
 #pragma unroll
@@ -367,15 +401,13 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
 #pragma unroll
         for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + buffer, d, b), p, b);
     }
-    if (NBUF == 1) __syncthreads();
     if (t + 1 < n_tiles) {
-      if (NBUF == 2) buffer = kBuffer - buffer;
+      if (!ALONE) buffer = kBuffer - buffer;
       put(buffer);
     }
   }
-  const float ref = end_rows(r, o);
-  const float top = join<RW, TW>(r, ref, o, rw, tw, lane, (float *)s_tile, s_m, s_l);
-  if (tw == 0) store_part(a, r, top, o, it.split, hh);
+  end_rows(r);
+  join_and_store<RW, TW>(a, r, o, rw, tw, lane, it.split, s_tile, s_m, s_l);
 }
 
 // ---------------------------------------------------------------- more rows: 128 per workgroup
@@ -386,7 +418,7 @@ template <bool BF>
 __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a) {
   constexpr int NP = parts_of<BF>(), kKeys = 32 * kRowK, kValues = 32 * kRowV, kHalf = 2 * (kKeys + kValues);
   __shared__ __align__(16) char s_tile[2 * kHalf];   // per half: keys of even and odd steps, values of even and odd steps
-  static_assert(2 * kHalf >= 4 * 64 * 64 * 4, "room for the partial outputs");
+  static_assert(2 * kHalf >= 8 * 8192, "room for what the waves exchange");
   __shared__ float s_m[8][32], s_l[8][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hh = lane >> 5, rw = wave & 3, half = wave >> 2;
@@ -492,18 +524,18 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + kValues, d, b), p0, b);
-  const float ref = end_rows(r, o), top = join<4, 2>(r, ref, o, rw, half, lane, (float *)s_tile, s_m, s_l);
-  if (half == 0) store_part(a, r, top, o, it.split, hh);
+  end_rows(r);
+  join_and_store<4, 2>(a, r, o, rw, half, lane, it.split, s_tile, s_m, s_l);
 }
 
 // Query rows per workgroup, workgroups along the rows.
 struct Shape {
-  int rows, row_tiles, resident;   // resident: workgroups on the chip at once
+  int rows, row_tiles, resident, tokens;   // resident: workgroups on the chip at once; tokens of an item: a multiple of this
 };
 Shape shape_of(int rows) {
-  if (rows <= 32) return Shape{32, 1, 512};
-  if (rows <= 64) return Shape{64, 1, 512};
-  return Shape{128, (rows + 127) / 128, 256};
+  if (rows <= 32) return Shape{32, 1, 512, 64};
+  if (rows <= 64) return Shape{64, 1, 512, 64};
+  return Shape{128, (rows + 127) / 128, 256, 128};
 }
 
 }  // namespace
@@ -511,13 +543,18 @@ Shape shape_of(int rows) {
 int shared_chunk(int rows, int n_kv_heads, int64_t len) {
   const Shape s = shape_of(rows);
   const int64_t want = std::max<int64_t>(1, s.resident / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
-  return (int)(((len + want - 1) / want + 127) / 128 * 128);
+  return (int)(((len + want - 1) / want + s.tokens - 1) / s.tokens * s.tokens);
 }
 
 hipError_t launch_shared(SharedArgs &a, hipStream_t s) {
   const Shape sh = shape_of(a.rows);
   a.row_tiles = sh.row_tiles;
-  const dim3 grid((unsigned)(((int64_t)a.n_split * a.Hkv + 7) / 8 * 8 * sh.row_tiles)), block(256);
+  const int64_t units = ((int64_t)a.n_split * a.Hkv + 7) / 8 * 8;
+  a.g_magic = a.rows < 1 << 20 ? magic_heads(1 << 20, a.G) : 0;
+  auto magic = [](int64_t most, int d) { return d > 1 && most * d < (1ll << 32) ? (uint32_t)(((1ll << 32) + d - 1) / d) : 0u; };
+  a.hkv_magic = magic(units, a.Hkv);
+  a.tiles_magic = magic(units / 8 * sh.row_tiles, sh.row_tiles);
+  const dim3 grid((unsigned)(units * sh.row_tiles)), block(256);
   const bool bf = a.tv.k_fmt == TTKV_BF16;
   switch (sh.rows) {
     case 32:

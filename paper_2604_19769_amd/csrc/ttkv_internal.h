@@ -358,7 +358,7 @@ struct SharedArgs {
   TierView tv;
   uint8_t member[TTKV_MAX_BATCH];
 };
-// How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part (a multiple of 64).
+// How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part.
 int shared_chunk(int rows, int n_kv_heads, int64_t len);
 hipError_t launch_shared(SharedArgs &a, hipStream_t s);
 

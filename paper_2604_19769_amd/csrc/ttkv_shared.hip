@@ -72,7 +72,6 @@ constexpr int kRowK = 272, kRowV = 288;
 constexpr float kUnit = 8.0f, kRoom = 7.0f;
 template <bool BF>
 constexpr int parts_of() { return BF ? 3 : 2; }   // numbers that hold a weight
-constexpr int kTile(int tw) { return tw == 4 ? 128 : 64; }   // tokens in LDS at a time
 
 // What a wave keeps of its 32 query rows beside the outputs: lane -> row lane % 32, both halves alike but for l.
 struct Rows {
@@ -193,7 +192,7 @@ struct Cursor {
   int64_t rec_bytes;
   int bt, ring_blocks, block, row;
   __device__ __forceinline__ void find() { head = base + (table ? (int64_t)((const_i32)table)[block] : (int64_t)block) * rec_bytes; }
-  __device__ __forceinline__ Cursor(const SharedArgs &a, int hkv, int token) {   // a multiple of 32
+  __device__ __forceinline__ Cursor(const SharedArgs &a, int hkv, int token) {
     bt = a.tv.bt;
     ring_blocks = a.tv.ring_blocks;
     rec_bytes = a.tv.rec_bytes;
@@ -206,7 +205,7 @@ struct Cursor {
     asm volatile("" : "+s"(bt), "+s"(ring_blocks), "+s"(rec_bytes), "+s"(table), "+s"(base));
     find();
   }
-  __device__ __forceinline__ void advance(int rows) {   // up to two blocks on
+  __device__ __forceinline__ void advance(int rows) {
     row += rows;
     if (row < bt) return;
     do {
@@ -239,33 +238,33 @@ __device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it) {
 __device__ __forceinline__ int k_lane(int lane) { return (lane & 31) * kRowK + 16 * (lane >> 5); }
 __device__ __forceinline__ int v_lane(int lane) { return (4 * (lane >> 5) + ((lane & 15) >> 2)) * kRowV + 32 * ((lane >> 4) & 1) + 8 * (lane & 3); }
 
-// The TW waves of one row block add up, each 128 / TW channels of the rows, and store them.  s_o: (4 - 4 / TW) x 4 KiB per wave; all
+// The TW waves of one row block add up, each 128 / TW channels of the rows, and store them.  s_o: (16 - 16 / TW) KiB per wave; all
 // waves of the workgroup take part.  Weights of a wave are exp2(score cs + mcs).
 template <int RW, int TW>
 __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &r, const f16v (&o)[4], int rw, int tw, int lane, int split, char *s_o,
                                                float (*s_m)[32], float (*s_l)[32]) {
-  constexpr int OWN = 4 / TW;   // blocks of 32 channels that a wave ends up with
+  constexpr int OWN = 16 / TW;   // pieces of 4 registers (channels 8 k + 4 hh .. + 3 of the block of 32) that a wave ends up with
   const int c = lane & 31, hh = lane >> 5;
   __syncthreads();   // everybody is done with the tiles
   if (hh == 0) {
     s_m[tw * RW + rw][c] = r.m == -INFINITY ? -INFINITY : -r.mcs;
     s_l[tw * RW + rw][c] = r.l;
   }
-  // what the other waves of the row block need: [giver][taker, without the giver][block][quarter][lane]
-  auto place = [&](int giver, int taker, int e, int k) __attribute__((always_inline)) -> float4 * {
+  // what the other waves of the row block need: [giver][taker, without the giver][piece][lane]
+  auto place = [&](int giver, int taker, int e) __attribute__((always_inline)) -> float4 * {
     const int slot = taker - (taker > giver);
-    return (float4 *)(s_o + (((((giver * RW + rw) * (TW - 1) + slot) * OWN + e) * 4 + k) * 64 + lane) * 16);
+    return (float4 *)(s_o + ((((giver * RW + rw) * (TW - 1) + slot) * OWN + e) * 64 + lane) * 16);
+  };
+  auto piece = [&](int q) __attribute__((always_inline)) -> float4 {
+    const f16v &x = o[q / 4];
+    const int k = 4 * (q % 4);
+    return float4{x[k], x[k + 1], x[k + 2], x[k + 3]};
   };
 #pragma unroll
   for (int t = 0; t < TW; ++t)
-    if (t != tw)
+    if (t != tw)   // (wave-uniform)
 #pragma unroll
-      for (int e = 0; e < OWN; ++e)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const f16v &x = o[t * OWN + e];
-          *place(tw, t, e, k) = float4{x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
-        }
+      for (int e = 0; e < OWN; ++e) *place(tw, t, e) = piece(t * OWN + e);
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
@@ -283,24 +282,23 @@ __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &
   float *const po = a.pacc + at * 128 + 4 * hh;
 #pragma unroll
   for (int w = 0; w < TW; ++w) {
-    if (w != tw) continue;   // (wave-uniform)
+    if (w != tw) continue;
 #pragma unroll
-    for (int e = 0; e < OWN; ++e)
+    for (int e = 0; e < OWN; ++e) {
+      const int q = w * OWN + e;
+      const float4 x = piece(q);
+      float4 y = {x.x * by[w], x.y * by[w], x.z * by[w], x.w * by[w]};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const f16v &x = o[w * OWN + e];
-        float4 y = {x[4 * k] * by[w], x[4 * k + 1] * by[w], x[4 * k + 2] * by[w], x[4 * k + 3] * by[w]};
-#pragma unroll
-        for (int u = 0; u < TW; ++u) {
-          if (u == w) continue;
-          const float4 z = *place(u, w, e, k);
-          y.x = fmaf(z.x, by[u], y.x);
-          y.y = fmaf(z.y, by[u], y.y);
-          y.z = fmaf(z.z, by[u], y.z);
-          y.w = fmaf(z.w, by[u], y.w);
-        }
-        if (r.on) *(float4_any *)(po + 32 * (w * OWN + e) + 8 * k) = float4_any{y.x, y.y, y.z, y.w};
+      for (int u = 0; u < TW; ++u) {
+        if (u == w) continue;
+        const float4 z = *place(u, w, e);
+        y.x = fmaf(z.x, by[u], y.x);
+        y.y = fmaf(z.y, by[u], y.y);
+        y.z = fmaf(z.z, by[u], y.z);
+        y.w = fmaf(z.w, by[u], y.w);
       }
+      if (r.on) *(float4_any *)(po + 8 * q) = float4_any{y.x, y.y, y.z, y.w};
+    }
   }
   if (r.on && hh == 0 && tw == 0) {
     a.pm[at] = (top + up) * kLn2;   // the weights are e^(score scale - this)
@@ -309,57 +307,53 @@ __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &
 }
 
 // ---------------------------------------------------------------- up to 64 rows per KV head
+// Bound: memory.  One workgroup of eight waves per CU: TW teams of RW waves (32 rows each) take the item's steps of 32 tokens
+// in turn (with a run of its own for each team, 2048 tokens of 256 items, the streams a power of two apart took 59.7 us instead of
+// 49.8).  A team loads its steps' rows itself and needs no other; K of one step and V of the step before
+// are always on their way, and leave their registers for LDS where the step before has been read.
 template <bool BF, int RW, int TW>
-__global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
-  static_assert(RW * TW == 4 && TW > 1, "four waves");
-  constexpr int TILE = kTile(TW), SUB = TILE / (32 * TW), NL = TILE / 16;   // 32-token steps of a wave per tile; 16-byte loads of K (V) per thread
-  static_assert(SUB == 1, "one step per tile and wave");
-  constexpr bool ALONE = RW == 1;   // a wave's 32 tokens of a tile are its own: it loads and stores them itself, and waits for nobody
-  constexpr int kBuffer = TILE * (kRowK + kRowV), NBUF = TW == 4 ? 1 : 2;   // two workgroups per CU either way
-  __shared__ __align__(16) char s_tile[NBUF * kBuffer];   // K rows, V rows per buffer; at the end what the waves exchange
-  static_assert(NBUF * kBuffer >= 4 * (4 - 4 / TW) * 4096, "room for what the waves exchange");
-  __shared__ float s_m[4][32], s_l[4][32];
+__global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
+  static_assert(RW * TW == 8 && (RW == 1 || RW == 2), "eight waves");
+  constexpr bool ALONE = RW == 1;   // a team of one waits for nobody: LDS takes a wave's stores and reads in order
+  constexpr int NL = 8 / RW, LR = 4 * RW;                        // 16-byte loads of K (V) per thread; rows apart
+  constexpr int kKeys = 32 * kRowK, kStep = 32 * (kRowK + kRowV), NBUF = ALONE ? 1 : 2;
+  __shared__ __align__(16) char s_tile[TW * NBUF * kStep];       // per team: keys and values of one step (two); at the end what the waves exchange
+  static_assert(TW * NBUF * kStep >= 8 * (16 - 16 / TW) * 1024, "room for what the waves exchange");
+  __shared__ float s_m[8][32], s_l[8][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int rw = wave % RW, tw = wave / RW;
+  const int tw = wave / RW, rw = wave % RW;
   const int c = lane & 31, hh = lane >> 5;
   Item it;
   if (!item_of(a, it)) return;
-  // ---- tiles: a thread's rows lr + LR i of the tile (of the wave's 32), piece lp
-  constexpr int LR = ALONE ? 4 : 16;
-  const int lr = (ALONE ? lane : (int)threadIdx.x) >> 4, lp = threadIdx.x & 15;
-  const int n_tiles = (it.n_tok + TILE - 1) / TILE, first = tw * 32;   // the wave's first token in a tile
-  const int mine = it.n_tok - first;                                   // tokens from the wave's first one on
+  const int mine = it.n_tok - 32 * tw;                           // tokens from the team's first step on; it takes every TW-th
+  Cursor keys(a, it.hkv, it.begin + (mine > 0 ? 32 * tw : 0)), values = keys;
+  values.base += a.tv.v_off;
+  values.head += a.tv.v_off;
+  int k_left = mine, v_left = mine;                              // tokens from the cursors on
+  const int lr = (threadIdx.x & (64 * RW - 1)) >> 4, lp = threadIdx.x & 15;
   u32x4 kr[NL], vr[NL];
-  Cursor at(a, it.hkv, it.begin + (ALONE && mine > 0 ? first : 0));
-  int to_load = ALONE ? max(mine, 1) : it.n_tok;     // tokens from the cursor on
-  const int v_off = a.tv.v_off;
-  auto load = [&]() __attribute__((always_inline)) {   // the next tile; rows behind the item's end repeat its last one
-    if constexpr (ALONE) {
-      const uint64_t head = at.rows();
+  auto load = [&](Cursor &at, int &left, u32x4 (&x)[NL]) __attribute__((always_inline)) {   // the team's next step, if there is one; rows behind the item's end: its last one
+    if (left <= 0) return;
+    const int len = min(left, 32);
+    const uint64_t head = at.rows();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint64_t p = head + (uint32_t)(min(lr + LR * i, to_load - 1) * 256 + lp * 16);
-        kr[i] = __builtin_nontemporal_load((gas_u32x4)p);   // read once
-        vr[i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
-      }
-      if (to_load > TILE) {
-        to_load -= TILE;
-        at.advance(TILE);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint64_t p = at.rows() + (uint32_t)(min(lr + LR * i, to_load - 1) * 256 + lp * 16);
-        kr[i] = __builtin_nontemporal_load((gas_u32x4)p);
-        vr[i] = __builtin_nontemporal_load((gas_u32x4)(p + v_off));
-      }
-      if (to_load > TILE) {
-        to_load -= TILE;
-        at.advance(TILE);
-      }
-    }
+    for (int i = 0; i < NL; ++i) x[i] = __builtin_nontemporal_load((gas_u32x4)(head + (uint32_t)(min(lr + LR * i, len - 1) * 256 + lp * 16)));
+    left -= 32 * TW;
+    if (left > 0) at.advance(32 * TW);
   };
-  load();
+  char *const team = s_tile + tw * NBUF * kStep;
+  const char *const k_at = team + k_lane(lane), *const v_at = team + kKeys + v_lane(lane);
+  char *const k_put = team + lr * kRowK + lp * 16, *const v_put = team + kKeys + lr * kRowV + lp * 16;
+  auto put = [&](char *to, int row_bytes, const u32x4 (&x)[NL]) __attribute__((always_inline)) {
+    if constexpr (ALONE) asm volatile("" ::: "memory");          // (the compiler has to leave the order as it is)
+#pragma unroll
+    for (int i = 0; i < NL; ++i) *(u32x4 *)(to + i * LR * row_bytes) = x[i];
+    if constexpr (ALONE) asm volatile("" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < NL; ++i) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+  load(keys, k_left, kr);
+  load(values, v_left, vr);
   u32x4 qf[8];
   Rows r = begin_rows<BF>(a, (it.row_tile * RW + rw) * 32 + c, it.hkv, hh, qf);
   f16v o[4];
@@ -367,30 +361,23 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  const char *const k_at = s_tile + first * kRowK + k_lane(lane), *const v_at = s_tile + TILE * kRowK + first * kRowV + v_lane(lane);
-  const int put_row = lr + (ALONE ? first : 0);
-  char *const k_put = s_tile + put_row * kRowK + lp * 16, *const v_put = s_tile + TILE * kRowK + put_row * kRowV + lp * 16;
-  auto put = [&](int buffer) __attribute__((always_inline)) {
-    // (a wave that is alone: LDS takes its reads and stores in order, the compiler has to leave them so)
-    if constexpr (ALONE) asm volatile("" ::: "memory");
+  put(k_put, kRowK, kr);
+  load(keys, k_left, kr);
+  put(v_put, kRowV, vr);
+  load(values, v_left, vr);
+  // (with barriers all teams take as many steps as the first)
+  const int n_steps = ((ALONE ? max(mine, 0) : it.n_tok) + 32 * TW - 1) / (32 * TW);
+  int now = 0;   // buffer of the step
+  for (int t = 0; t < n_steps; ++t) {
+    if (!ALONE) __syncthreads();   // the step is in its buffer; everybody is done with the other one
+    const int next = ALONE ? 0 : kStep - now, len = mine - 32 * TW * t;
+    f16v sc = {};
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      *(u32x4 *)(k_put + buffer + i * LR * kRowK) = kr[i];
-      *(u32x4 *)(v_put + buffer + i * LR * kRowV) = vr[i];
-    }
-    if constexpr (ALONE) asm volatile("" ::: "memory");
-  };
-  put(0);
-  int buffer = 0;
-  for (int t = 0; t < n_tiles; ++t) {
-    if (!ALONE) __syncthreads();        // tile t is in its buffer; everybody is done with the other one
-    if (t + 1 < n_tiles) load();
-    const int left = mine - t * TILE;
-    if (left > 0) {   // (wave-uniform)
-      f16v sc = {};
-#pragma unroll
-      for (int kb = 0; kb < 8; ++kb) sc = mma<BF>(*(const u32x4 *)(k_at + buffer + 32 * kb), qf[kb], sc);
-      if (left < 32) mask_step(sc, left, hh);
+    for (int kb = 0; kb < 8; ++kb) sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
+    put(k_put + next, kRowK, kr);
+    load(keys, k_left, kr);
+    if (len > 0) {   // (wave-uniform)
+      if (len < 32) mask_step(sc, len, hh);
       const float mt = step_max(sc);
       if (__any(mt > r.far)) move_reference(r, mt, o);
       u32x4 p[parts_of<BF>()][2];
@@ -399,12 +386,11 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const SharedArgs a) {
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + buffer, d, b), p, b);
+        for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + now, d, b), p, b);
     }
-    if (t + 1 < n_tiles) {
-      if (!ALONE) buffer = kBuffer - buffer;
-      put(buffer);
-    }
+    put(v_put + next, kRowV, vr);
+    load(values, v_left, vr);
+    now = next;
   }
   end_rows(r);
   join_and_store<RW, TW>(a, r, o, rw, tw, lane, it.split, s_tile, s_m, s_l);
@@ -418,7 +404,7 @@ template <bool BF>
 __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a) {
   constexpr int NP = parts_of<BF>(), kKeys = 32 * kRowK, kValues = 32 * kRowV, kHalf = 2 * (kKeys + kValues);
   __shared__ __align__(16) char s_tile[2 * kHalf];   // per half: keys of even and odd steps, values of even and odd steps
-  static_assert(2 * kHalf >= 8 * 8192, "room for what the waves exchange");
+  static_assert(2 * kHalf >= 8 * 8 * 1024, "room for what the waves exchange");
   __shared__ float s_m[8][32], s_l[8][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = lane & 31, hh = lane >> 5, rw = wave & 3, half = wave >> 2;
@@ -533,8 +519,8 @@ struct Shape {
   int rows, row_tiles, resident, tokens;   // resident: workgroups on the chip at once; tokens of an item: a multiple of this
 };
 Shape shape_of(int rows) {
-  if (rows <= 32) return Shape{32, 1, 512, 64};
-  if (rows <= 64) return Shape{64, 1, 512, 64};
+  if (rows <= 32) return Shape{32, 1, 256, 32};
+  if (rows <= 64) return Shape{64, 1, 256, 32};
   return Shape{128, (rows + 127) / 128, 256, 128};
 }
 
@@ -542,7 +528,8 @@ Shape shape_of(int rows) {
 
 int shared_chunk(int rows, int n_kv_heads, int64_t len) {
   const Shape s = shape_of(rows);
-  const int64_t want = std::max<int64_t>(1, s.resident / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
+  const int64_t most = std::max<int64_t>(1, s.resident / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
+  const int64_t want = std::min(most, (len + 63) / 64);
   return (int)(((len + want - 1) / want + s.tokens - 1) / s.tokens * s.tokens);
 }
 
@@ -554,20 +541,20 @@ hipError_t launch_shared(SharedArgs &a, hipStream_t s) {
   auto magic = [](int64_t most, int d) { return d > 1 && most * d < (1ll << 32) ? (uint32_t)(((1ll << 32) + d - 1) / d) : 0u; };
   a.hkv_magic = magic(units, a.Hkv);
   a.tiles_magic = magic(units / 8 * sh.row_tiles, sh.row_tiles);
-  const dim3 grid((unsigned)(units * sh.row_tiles)), block(256);
+  const dim3 grid((unsigned)(units * sh.row_tiles)), block(512);
   const bool bf = a.tv.k_fmt == TTKV_BF16;
   switch (sh.rows) {
     case 32:
-      if (bf) hipLaunchKernelGGL((shared_kernel<true, 1, 4>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((shared_kernel<false, 1, 4>), grid, block, 0, s, a);
+      if (bf) hipLaunchKernelGGL((shared_kernel<true, 1, 8>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((shared_kernel<false, 1, 8>), grid, block, 0, s, a);
       break;
     case 64:
-      if (bf) hipLaunchKernelGGL((shared_kernel<true, 2, 2>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((shared_kernel<false, 2, 2>), grid, block, 0, s, a);
+      if (bf) hipLaunchKernelGGL((shared_kernel<true, 2, 4>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((shared_kernel<false, 2, 4>), grid, block, 0, s, a);
       break;
     default:
-      if (bf) hipLaunchKernelGGL(shared_rows_kernel<true>, grid, dim3(512), 0, s, a);
-      else hipLaunchKernelGGL(shared_rows_kernel<false>, grid, dim3(512), 0, s, a);
+      if (bf) hipLaunchKernelGGL(shared_rows_kernel<true>, grid, block, 0, s, a);
+      else hipLaunchKernelGGL(shared_rows_kernel<false>, grid, block, 0, s, a);
       break;
   }
   return hipGetLastError();

@@ -156,8 +156,8 @@ def _check(status, what):
 
 
 def _p(x):
-    """Pointer of a torch tensor / int / None, as ctypes takes it for a void* argument."""
-    return x if x is None or isinstance(x, int) else x.data_ptr()
+    """Pointer of a torch tensor / int / ctypes array / None, as ctypes takes it for a void* argument."""
+    return x if x is None or isinstance(x, (int, C.Array)) else x.data_ptr()
 
 
 def ttkv_create():

@@ -28,6 +28,7 @@ _Q_FMT = {torch.float16: B.F16, torch.bfloat16: B.BF16}
 _SRC_FMT = {torch.float16: B.F16, torch.bfloat16: B.BF16, torch.float32: B.F32}
 # The current stream's handle without a torch.cuda.Stream object around it (2 us of a step's 14 on the host).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)   # (its users hold device tensors: the runtime is up)
 
 _SECTION_BYTES = {"f16": (256, 0), "bf16": (256, 0), "i8": (128, 8), "i4": (64, 8), "i4t": (64, 4), "i4c": (64, 8)}
 
@@ -37,7 +38,7 @@ def _on_own_device(method):
     @functools.wraps(method)
     def call(self, *args, **kw):
         index = self.device.index
-        if index is None or torch.cuda.current_device() == index:
+        if index is None or _current_device() == index:
             return method(self, *args, **kw)
         with torch.cuda.device(index):
             return method(self, *args, **kw)
@@ -52,17 +53,18 @@ def _stream_of(device):
 
 def _heads(x, device):
     """A tensor [sequence][token][head][128] as the library's strided view."""
-    assert x.dim() == 4 and x.shape[3] == 128 and x.stride(3) == 1 and x.device == device, (x.shape, x.stride(), x.device)
-    return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], x.shape[2], *x.stride()[:3])
+    n, s = x.shape, x.stride()
+    assert len(n) == 4 and n[3] == 128 and s[3] == 1 and x.device == device, (n, s, x.device)
+    return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], n[2], s[0], s[1], s[2])
 
 
 def _host_int64(x, n):
-    """None, or n host integers as (array to keep, address)."""
-    if x is None:
-        return None, None
+    """None, or n host integers as the library takes them."""
+    if x is None or n == 0:
+        return None
     a = np.ascontiguousarray(x, np.int64)
     assert a.shape == (n,), a.shape
-    return a, a.ctypes.data
+    return (C.c_int64 * n).from_buffer(a if a.flags.writeable else a.copy())   # (half the time of a.ctypes)
 
 
 def _device_positions(x, n_seq, n_tokens, device):
@@ -121,8 +123,7 @@ class Rotary:
             else:
                 views += [None, None]
                 out.append(None)
-        keep, first = _host_int64(first_pos, shape[0])
-        B.ttkv_norm_rope(self.h, self.r, *views, shape[0], shape[1], first, _device_positions(positions, *shape, self.device),
+        B.ttkv_norm_rope(self.h, self.r, *views, shape[0], shape[1], _host_int64(first_pos, shape[0]), _device_positions(positions, *shape, self.device),
                          _stream_of(self.device))
         return tuple(out)
 
@@ -269,10 +270,8 @@ class TieredCache:
         if first_pos is None and positions is None and self.prefix is not None:
             first_pos = sum(self.len) + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
-        keep_n, n_each = _host_int64(counts, n)
-        keep_p, first = _host_int64(first_pos, n)
-        B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, dev), _heads(v, dev), T, n_each, first,
-                           _device_positions(positions, n, T, dev), self._compute())
+        B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, dev), _heads(v, dev), T, _host_int64(counts, n),
+                           _host_int64(first_pos, n), _device_positions(positions, n, T, dev), self._compute())
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
         return q_out
@@ -393,12 +392,22 @@ class TieredCache:
         if self.shared_out is None or self.shared_out.shape[0] != n:
             self.shared_out = torch.empty(n, self.Hq, 128, dtype=torch.float32, device=self.device)
             self.shared_lse = torch.empty(n, self.Hq, dtype=torch.float32, device=self.device)
-        need = B.ttkv_shared_workspace_bytes(self.h, self.c, n)
-        if self.shared_ws is None or self.shared_ws.numel() < need:
-            self.shared_ws = torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
-        B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
-                           self._compute())
+        if self.shared_ws is None:
+            self._shared_workspace(n)
+        try:
+            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
+                               self._compute())
+        except B.TTKVError as e:
+            if e.status != B.ERR_WORKSPACE:
+                raise
+            self._shared_workspace(n)         # more sequences or parts than any call before: nothing was enqueued
+            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
+                               self._compute())
         return self.shared_out, self.shared_lse
+
+    def _shared_workspace(self, n):
+        need = B.ttkv_shared_workspace_bytes(self.h, self.c, n)
+        self.shared_ws = torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
 
     def select(self, q, k):
         q_fmt = _Q_FMT[q.dtype]

@@ -5,10 +5,11 @@
 //   angle_i = pos freq_i;  c_i = magnitude cos, s_i = magnitude sin
 //   (a, b) -> (a c - b s, b c + a s)       for the pairs (i, i + R/2), or (2 i, 2 i + 1); channels from R on pass
 //
-// A wave takes one token and eight heads at a time, eight lanes per head.  Lane j of a head holds the two 16-byte pieces that
-// contain pairs 8 j .. 8 j + 7: pieces j and j + R/16 of the row's sixteen (pairs half a rotation apart), or 2 j and 2 j + 1 (side
-// by side), so a rotation needs no exchange between lanes; lanes from R/16 on hold pieces that pass.  The wave's 64 lanes work
-// out one angle each and hand them to the eight heads through LDS.  Angles are counted in turns: pos x (freq / 2 pi)
+// A wave takes one token and eight heads at a time, eight lanes per head.  Lane j of a head holds two of the row's sixteen 16-byte pieces
+// (of 16-bit channels): j and j + 8, so that the lanes of one instruction cover whole lines, where pairs are side by side or all 128
+// channels turn; pieces j and j + R/16 where fewer turn half a rotation apart, lanes from R/16 on then hold pieces that pass.  Either way
+// a rotation needs no exchange between lanes.  The wave's 64 lanes work out one angle each and hand them to the eight heads
+// through LDS.  Angles are counted in turns: pos x (freq / 2 pi)
 // with the factor in two 64-bit numbers and the product's rounding taken back, so what is left after the whole turns is right at any
 // position (one 64-bit product alone would be 1e-4 off at 2^40); everything else is fp32, rounded once to the destination's type.
 #include "ttkv_internal.h"
@@ -62,7 +63,9 @@ __device__ __forceinline__ void expand(const Piece<F> &p, float (&x)[8]) {
     }
   }
 }
-template <int F>
+// STREAM: with the streaming hint, where the lanes of one instruction fill whole lines of 128 bytes (2 x 4096 tokens of 32 / 8 bf16 heads
+// 40.4 -> 33.9 us; where they fill half lines, 6000 tokens of 32 / 32 heads with 96 channels turning, 88 -> 110).
+template <int F, bool STREAM>
 __device__ __forceinline__ void store_piece(uint8_t *row, int piece, const float (&x)[8]) {
   u32x4 *d = (u32x4 *)(row + piece * 8 * elem_bytes<F>());
   if constexpr (F == TTKV_F32) {
@@ -77,7 +80,9 @@ __device__ __forceinline__ void store_piece(uint8_t *row, int piece, const float
       if constexpr (F == TTKV_F16) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
       else w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
     }
-    d[0] = u32x4{w[0], w[1], w[2], w[3]};
+    const u32x4 v = {w[0], w[1], w[2], w[3]};
+    if constexpr (STREAM) __builtin_nontemporal_store(v, d);
+    else d[0] = v;
   }
 }
 
@@ -91,7 +96,8 @@ __device__ __forceinline__ float sum_of_eight_lanes(float v) {
   return v + dpp<0x141>(v);     // row_half_mirror
 }
 
-template <int SRC, int DST>
+// WHOLE: pairs are side by side, or all channels turn, or none (see the pieces above).
+template <int SRC, int DST, bool WHOLE>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   __shared__ f2 s_turn[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -100,6 +106,27 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   const int64_t token = w >> a.wave_shift;
   const int part = (int)(w - (token << a.wave_shift)), parts = 1 << a.wave_shift;
   if (token >= a.count[j]) return;    // whole waves leave together; no barriers
+
+  const int l8 = lane & 7, slot = lane >> 3;
+  // The lane's two pieces and which of them turn.
+  const int p0 = !WHOLE && l8 >= a.turning ? 2 * l8 : l8, p1 = WHOLE ? l8 + 8 : l8 < a.turning ? l8 + a.turning : 2 * l8 + 1;
+  const bool turn0 = a.interleaved ? p0 < 2 * a.turning : l8 < a.turning, turn1 = a.interleaved ? p1 < 2 * a.turning : turn0;
+  // A batch: eight heads of the queries, the keys or the values.  The next one is asked for before one is worked on.
+  struct Batch {
+    Piece<SRC> w0, w1;
+    int side, h;
+  };
+  auto ask = [&](int b) __attribute__((always_inline)) -> Batch {
+    Batch t;
+    t.side = b >= a.first_batch[2] ? 2 : b >= a.first_batch[1] ? 1 : 0;
+    const RopeSide &s = a.side[t.side];
+    t.h = (b - a.first_batch[t.side]) * 8 + slot;
+    const uint8_t *src = s.src + j * s.src_seq + token * s.src_token + (t.h < s.n_heads ? t.h : 0) * s.src_head;
+    t.w0 = load_piece<SRC>(src, t.side == 2 ? l8 : p0);     // values do not turn
+    t.w1 = load_piece<SRC>(src, t.side == 2 ? l8 + 8 : p1);
+    return t;
+  };
+  const Batch first = ask(min(part, a.n_batches - 1));
 
   if (lane < 8 * a.turning) {
 #pragma clang fp contract(off)
@@ -112,13 +139,12 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   }
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const int l8 = lane & 7, slot = lane >> 3;
-  const bool turns_here = l8 < a.turning;
   f2 cs[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) cs[i] = turns_here ? s_turn[wave][8 * l8 + i] : f2{1.0f, 0.0f};
-  const bool side_by_side = a.interleaved || !turns_here;
-  const int p0 = side_by_side ? 2 * l8 : l8, p1 = side_by_side ? 2 * l8 + 1 : l8 + a.turning;
+  for (int i = 0; i < 8; ++i) {
+    const int pair = a.interleaved ? 4 * l8 + i % 4 + (i < 4 ? 0 : 32) : 8 * l8 + i;
+    cs[i] = (i < 4 ? turn0 : turn1) ? s_turn[wave][pair] : f2{1.0f, 0.0f};
+  }
 
   uint8_t *head0 = nullptr;   // the token's place in the tier
   int64_t head_step = 0;
@@ -136,17 +162,12 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     v_off = tv.v_off;
   }
 
-  for (int b = part; b < a.n_batches; b += parts) {
-    const int side = b >= a.first_batch[2] ? 2 : b >= a.first_batch[1] ? 1 : 0;   // queries, keys, values
-    const RopeSide &s = a.side[side];
-    const int h = (b - a.first_batch[side]) * 8 + slot;
-    const bool live = h < s.n_heads;
-    const uint8_t *src = s.src + j * s.src_seq + token * s.src_token + (live ? h : 0) * s.src_head;
-    const Piece<SRC> w0 = load_piece<SRC>(src, p0), w1 = load_piece<SRC>(src, p1);
+  auto work = [&](const Batch &t) __attribute__((always_inline)) {
+    const RopeSide &s = a.side[t.side];
     float x[8], y[8];
-    expand<SRC>(w0, x);
-    expand<SRC>(w1, y);
-    if (side < 2) {
+    expand<SRC>(t.w0, x);
+    expand<SRC>(t.w1, y);
+    if (t.side < 2) {
       if (s.norm) {
         float sq = 0.0f;
 #pragma unroll
@@ -158,47 +179,62 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
           y[i] *= inv;
         }
         if (s.weight) {
+          const float4 *w0 = (const float4 *)(s.weight + 8 * p0), *w1 = (const float4 *)(s.weight + 8 * p1);
+          const float4 u0 = w0[0], u1 = w0[1], v0 = w1[0], v1 = w1[1];
+          const float u[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w}, v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            x[i] *= s.weight[8 * p0 + i];
-            y[i] *= s.weight[8 * p1 + i];
+            x[i] *= u[i];
+            y[i] *= v[i];
           }
         }
       }
-      if (turns_here) {
-        if (a.interleaved) {
+      if (a.interleaved) {
+        auto turn = [&](float (&z)[8], const f2 *t) __attribute__((always_inline)) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float x0 = x[2 * i], x1 = x[2 * i + 1], y0 = y[2 * i], y1 = y[2 * i + 1];
-            x[2 * i] = x0 * cs[i].x - x1 * cs[i].y;
-            x[2 * i + 1] = x1 * cs[i].x + x0 * cs[i].y;
-            y[2 * i] = y0 * cs[4 + i].x - y1 * cs[4 + i].y;
-            y[2 * i + 1] = y1 * cs[4 + i].x + y0 * cs[4 + i].y;
+            const float u = z[2 * i], v = z[2 * i + 1];
+            z[2 * i] = u * t[i].x - v * t[i].y;
+            z[2 * i + 1] = v * t[i].x + u * t[i].y;
           }
-        } else {
+        };
+        if (turn0) turn(x, cs);
+        if (turn1) turn(y, cs + 4);
+      } else if (turn0) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float u = x[i], v = y[i];
-            x[i] = u * cs[i].x - v * cs[i].y;
-            y[i] = v * cs[i].x + u * cs[i].y;
-          }
+        for (int i = 0; i < 8; ++i) {
+          const float u = x[i], v = y[i];
+          x[i] = u * cs[i].x - v * cs[i].y;
+          y[i] = v * cs[i].x + u * cs[i].y;
         }
       }
     }
-    if (!live) continue;
-    uint8_t *dst = a.in_tier && side ? head0 + h * head_step + (side == 2 ? v_off : 0)
-                                     : s.dst + j * s.dst_seq + token * s.dst_token + h * s.dst_head;
-    store_piece<DST>(dst, p0, x);
-    store_piece<DST>(dst, p1, y);
+    if (t.h >= s.n_heads) return;
+    uint8_t *dst = a.in_tier && t.side ? head0 + t.h * head_step + (t.side == 2 ? v_off : 0)
+                                       : s.dst + j * s.dst_seq + token * s.dst_token + t.h * s.dst_head;
+    store_piece<DST, WHOLE>(dst, t.side == 2 ? l8 : p0, x);
+    store_piece<DST, WHOLE>(dst, t.side == 2 ? l8 + 8 : p1, y);
+  };
+  Batch now = first;
+  for (int b = part; b < a.n_batches; b += parts) {
+    Batch next = now;
+    if (b + parts < a.n_batches) next = ask(b + parts);
+    work(now);
+    now = next;
   }
 }
 
+template <int SRC, int DST>
+void launch_kernel(const RopeArgs &a, dim3 grid, hipStream_t s) {
+  if (a.interleaved || a.turning == 0 || a.turning == 8) hipLaunchKernelGGL((rope_kernel<SRC, DST, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_kernel<SRC, DST, false>), grid, dim3(256), 0, s, a);
+}
 template <int SRC>
 void launch_from(const RopeArgs &a, int dst, dim3 grid, hipStream_t s) {
   switch (dst) {
-    case TTKV_F16: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_F16>), grid, dim3(256), 0, s, a); break;
-    case TTKV_BF16: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_BF16>), grid, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((rope_kernel<SRC, TTKV_F32>), grid, dim3(256), 0, s, a); break;
+    case TTKV_F16: launch_kernel<SRC, TTKV_F16>(a, grid, s); break;
+    case TTKV_BF16: launch_kernel<SRC, TTKV_BF16>(a, grid, s); break;
+    default: launch_kernel<SRC, TTKV_F32>(a, grid, s); break;
   }
 }
 

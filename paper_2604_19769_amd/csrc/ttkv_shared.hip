@@ -413,6 +413,7 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
   // Four waves take the item's first half, four the second; one without tokens looks at a live one that counts nothing.
   const int n_half = a.chunk / 2, n_steps = ((min(it.n_tok, n_half) + 31) / 32 + 1) & ~1;   // in pairs: the last ones may have no live token
   const int n_tok = half ? max(it.n_tok - n_half, 0) : min(it.n_tok, n_half);
+  const bool idle = (it.row_tile * 4 + rw) * 32 >= a.rows;   // a wave without rows only helps with the tiles
   if (half && n_tok) it.begin += n_half;
   const int lr = threadIdx.x >> 4 & 15, lp = threadIdx.x & 15;
   char *const s_half = s_tile + half * kHalf;
@@ -461,15 +462,24 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
     constexpr int ODD = decltype(odd_tag)::value;
     __syncthreads();   // keys of s + 1 and values of s - 1 are there; everybody is done with those of s and s - 2
     const char *const v_old = v_at + (1 - ODD) * kValues, *const k_next = k_at + (1 - ODD) * kKeys;
+    if (idle) {
+      put_keys(ODD);
+      put_values(ODD);
+      load_keys();
+      load_values();
+      return;
+    }
     const float mt = step_max(sc);
-    if (__any(mt > r.far)) {   // the outputs take the weights of the old reference first; what is added below is then nothing
+    if (__any(mt > r.far)) {
+      if (s) {   // the outputs take the weights of the old reference first; what is added below is then nothing
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
+        for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_old, d, b), p, b);
+          for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_old, d, b), p, b);
+#pragma unroll
+        for (int u = 0; u < NP; ++u) p[u][0] = p[u][1] = u32x4{0, 0, 0, 0};
+      }
       move_reference(r, mt, o);
-#pragma unroll
-      for (int u = 0; u < NP; ++u) p[u][0] = p[u][1] = u32x4{0, 0, 0, 0};
     }
     put_keys(ODD);       // of s + 2
     put_values(ODD);     // of s

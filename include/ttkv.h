@@ -374,8 +374,9 @@ ttkv_status ttkv_rope_append(ttkv_handle h, ttkv_cache *c, int32_t tier, int32_t
 /* ---------------------------------------------------------------- a prefix that a batch shares */
 
 /* Attention of n_seq sequences' queries over ONE cached prefix, whose bytes are read once for all of them (Alg. 1's Attn on
- * a block, for many queries).  `prefix` is a cache of batch 1, its tiers fp16 / bf16 and in device memory (UNSUPPORTED
- * otherwise); every token is attended.
+ * a block, for many queries).  `prefix` is a cache of batch 1, its tiers in device memory: fp16, bf16, or
+ * row-wise quantized (K / V int8 / int8, int4 / int4 or int8 / int4; keys grouped over tokens and values stored channel-major:
+ * UNSUPPORTED, like host tiers); every token is attended.
  *   q    [device] [n_seq][n_q_heads][128], 16-byte aligned, q_fmt as in ttkv_decode_attn; n_seq up to TTKV_MAX_SHARED_SEQS,
  *        n_seq x n_q_heads < 2^22 (UNSUPPORTED beyond)
  *   out  [device] [n_seq][n_q_heads][128] fp32;  lse [device] [n_seq][n_q_heads] fp32 or NULL; an empty prefix gives 0 and -inf
@@ -391,7 +392,7 @@ size_t ttkv_shared_workspace_bytes(ttkv_handle h, const ttkv_cache *prefix, int3
 int32_t ttkv_prefix_parts(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);
 
 /* ttkv_decode_step for a batch whose sequences share a prefix: each attends the prefix, its own cache and the step's token.
- * The prefix has the cache's head counts and softmax_scale (INVALID_ARG otherwise).  member [host] [batch]: the sequences with
+ * The prefix has the cache's head counts and softmax_scale, q is 16-byte aligned (INVALID_ARG otherwise).  member [host] [batch]: the sequences with
  * a non-zero entry take part, NULL: all; the others attend their own tokens alone.  k_new, v_new both NULL: attend only; with
  * a token, tier 0 must be an fp16 / bf16 device tier of format new_fmt without mean keys (UNSUPPORTED otherwise).  Every live
  * block is attended, host tiers in place; one stream.  Same refusals otherwise. */

@@ -18,6 +18,7 @@ SOURCES = {
     "ttkv_select.hip": ["-ffp-contract=off"],
     "ttkv_rope.hip": [],
     "ttkv_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ttkv_shared_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_probe.hip": [],
 }
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

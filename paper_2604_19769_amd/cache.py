@@ -110,22 +110,25 @@ class Rotary:
         """q [B][T][Hq][128] and / or k [B][T][Hkv][128], any strides but the last, f16 / bf16 / f32 -> (q_out, k_out), new tensors
         of `dtype` (None: the input's) unless given (an output may be its own input).  Token i of sequence b is at
         positions[b][i] (int64 on the device), or first_pos[b] + i (host integers; None: i)."""
-        views, out = [], []
-        shape = (q if q is not None else k).shape[:2]
-        for x, y in ((q, q_out), (k, k_out)):
-            if x is not None:
-                assert x.shape[:2] == shape
-                if y is None:
-                    y = torch.empty(x.shape, dtype=dtype or x.dtype, device=self.device)
-                assert y.shape == x.shape
-                views += [_heads(x, self.device), _heads(y, self.device)]
-                out.append(y)
-            else:
-                views += [None, None]
-                out.append(None)
-        B.ttkv_norm_rope(self.h, self.r, *views, shape[0], shape[1], _host_int64(first_pos, shape[0]), _device_positions(positions, *shape, self.device),
-                         _stream_of(self.device))
-        return tuple(out)
+        dev = self.device
+        n, T = (q if q is not None else k).shape[:2]
+        qv = qo = kv = ko = None
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=dtype or q.dtype, device=dev)
+            assert q_out.shape == q.shape
+            qv, qo = _heads(q, dev), _heads(q_out, dev)
+        else:
+            q_out = None
+        if k is not None:
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=dtype or k.dtype, device=dev)
+            assert k_out.shape == k.shape and k.shape[0] == n and k.shape[1] == T
+            kv, ko = _heads(k, dev), _heads(k_out, dev)
+        else:
+            k_out = None
+        B.ttkv_norm_rope(self.h, self.r, qv, qo, kv, ko, n, T, _host_int64(first_pos, n), _device_positions(positions, n, T, dev), _stream_of(dev))
+        return q_out, k_out
 
 
 class TieredCache:
@@ -199,7 +202,7 @@ class TieredCache:
             self.share(prefix, members)
 
     def share(self, prefix, members=None):
-        """Attend the tokens of `prefix`, a TieredCache of batch 1 with fp16 / bf16 tiers in HBM, in front of every sequence's own
+        """Attend the tokens of `prefix`, a TieredCache of batch 1 with its tiers in HBM, in front of every sequence's own
         from now on (members: truth values, the sequences that do; None: all).  prefix None: no longer."""
         if prefix is not None:
             assert prefix.B == 1 and (prefix.Hq, prefix.Hkv, prefix.device) == (self.Hq, self.Hkv, self.device)

@@ -1111,11 +1111,12 @@ static ttkv_status plan_prefix(const ttkv_cache *c, bool check_tables, int32_t q
   P.parts = 0;
   for (int t = 0; t < c->n_tiers; ++t) {
     const ttkv_tier &T = c->tier[t];
-    if (T.mem != TTKV_MEM_DEVICE || !is_fp(T.k_fmt) || T.k_fmt != T.v_fmt) return TTKV_ERR_UNSUPPORTED;
+    const bool fp = is_fp(T.k_fmt) && T.k_fmt == T.v_fmt;
+    if (T.mem != TTKV_MEM_DEVICE || !(fp || shared_quant_fits(T.k_fmt, T.v_fmt))) return TTKV_ERR_UNSUPPORTED;
     if (T.k_fmt == TTKV_BF16 && q_fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
     P.chunk[t] = 0;
     if (n_seq == 0 || T.len[0] == 0) continue;
-    P.chunk[t] = shared_chunk(n_seq * (c->n_q_heads / c->n_kv_heads), c->n_kv_heads, T.len[0]);
+    P.chunk[t] = shared_chunk(n_seq * (c->n_q_heads / c->n_kv_heads), c->n_kv_heads, T.len[0], !fp);
     P.parts += split_of(T.len[0], P.chunk[t]);
   }
   return TTKV_OK;

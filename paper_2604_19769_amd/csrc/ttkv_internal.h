@@ -342,7 +342,7 @@ struct RopeArgs {
 static_assert(sizeof(RopeArgs) <= 4096, "kernel arguments are passed by value");
 hipError_t launch_rope(RopeArgs &a, int n_seq, int64_t n_tokens, int src_fmt, int dst_fmt, hipStream_t s);
 
-// Attention of many query rows over one run of tokens of one fp tier (shared_kernel).
+// Attention of many query rows over one run of tokens of one tier (shared_kernel and its kin).
 struct SharedArgs {
   const void *q;                 // [sequence][Hq][128]
   int32_t q_fmt, Hq, Hkv, G;
@@ -359,8 +359,10 @@ struct SharedArgs {
   uint8_t member[TTKV_MAX_BATCH];
 };
 // How a run of `len` tokens is cut for `rows` query rows per KV head: tokens per part.
-int shared_chunk(int rows, int n_kv_heads, int64_t len);
+int shared_chunk(int rows, int n_kv_heads, int64_t len, bool quantized);
 hipError_t launch_shared(SharedArgs &a, hipStream_t s);
+bool shared_quant_fits(int k_fmt, int v_fmt);
+hipError_t launch_shared_quant(const SharedArgs &a, dim3 grid, hipStream_t s);
 
 // Load-only kernel over `bytes` (rounded down to 64 KiB) of device memory; sink: 4 writable bytes.
 hipError_t launch_stream_read(const void *src, int64_t bytes, uint32_t *sink, hipStream_t s);

@@ -72,7 +72,8 @@ def test_sizes(dtype, n_seq, Hq, Hkv, n):
 
 
 @pytest.mark.parametrize("dtype,n_seq,Hq,Hkv,n,bt,paged", [("f16", 64, 32, 8, 9001, 128, 3), ("bf16", 24, 32, 32, 4100, 256, None), ("f16", 2, 8, 2, 30000, 64, 4),
-                                                           ("bf16", 40, 8, 2, 20011, 1024, None), ("f16", 300, 8, 4, 3001, 128, None)])
+                                                           ("bf16", 40, 8, 2, 20011, 1024, None), ("f16", 300, 8, 4, 3001, 128, None),
+                                                           ("f16", 1500, 2, 2, 700, 64, 6), ("bf16", 2000, 4, 1, 321, 64, None)])
 def test_long(dtype, n_seq, Hq, Hkv, n, bt, paged):
     c, k, v = make_prefix(Hq, Hkv, dtype, n, bt=bt, paged=paged, extra=2, first_block=1)
     q = rnd(8, n_seq, Hq, 128, dtype=dtype)
@@ -163,6 +164,82 @@ def test_two_tiers_of_a_prefix():
     out, lse = c.attend_shared(q)
     check(out, lse, [reference(x, [(k, v), (k1, v1)], c.c.softmax_scale) for x in q])
     c.close()
+
+
+def stored_values(c, t):
+    """K, V [Hkv][n][128] that tier t of a cache of one sequence stands for."""
+    d, out = c.dump_tier(t, 0), []
+    for name, fmt in (("k", c.cfg[t].k_fmt), ("v", c.cfg[t].v_fmt)):
+        x = d[name]
+        if fmt in ("f16", "bf16"):
+            out.append(torch.from_numpy(x.view(np.int16).copy()).view(DT[fmt]).to(DEV))
+            continue
+        meta = d[name + "_meta"].view(np.float16).astype(np.float32)
+        if fmt == "i8":
+            v = x.view(np.int8).astype(np.float32) * np.repeat(meta, 32, -1)
+        else:
+            codes = np.stack((x & 15, x >> 4), -1).reshape(*x.shape[:-1], 128).astype(np.float32)
+            v = codes * np.repeat(meta[..., 0::2], 64, -1) + np.repeat(meta[..., 1::2], 64, -1)
+        out.append(torch.from_numpy(v).to(DEV))
+    return tuple(out)
+
+
+QUANT = [("i8", "i8"), ("i4", "i4"), ("i8", "i4")]
+
+
+@pytest.mark.parametrize("k_fmt,v_fmt", QUANT)
+@pytest.mark.parametrize("n_seq,Hq,Hkv,n,bt,paged,q_type", [
+    (1, 4, 4, 1, 64, None, "f16"), (3, 8, 2, 31, 64, 3, "bf16"), (9, 28, 4, 65, 128, None, "f16"), (33, 4, 4, 200, 64, 5, "f16"),
+    (64, 8, 2, 1000, 256, 6, "bf16"), (2, 8, 2, 20011, 128, 7, "f16"), (16, 32, 8, 4097, 1024, None, "f16"), (300, 2, 1, 700, 64, None, "f16")])
+def test_quantized_tiers(k_fmt, v_fmt, n_seq, Hq, Hkv, n, bt, paged, q_type):
+    c, _, _ = make_prefix(Hq, Hkv, "f16", 0, tiers=[TierConfig(k_fmt, v_fmt, 10 ** 9, bt, -(-n // bt) + 1, paged_seed=paged)], poison=False)
+    c.pool[0].random_(0, 255)                                  # what is not live is anything
+    c.start[0][:] = n % 3 * bt if -(-n // bt) >= 2 else bt
+    loud = torch.ones(128, device=DEV)
+    loud[::50] = 8.0
+    k, v = (rnd(1, Hkv, n, 128) * loud).half(), rnd(2, Hkv, n, 128, dtype="f16")
+    c.append(0, k, v, seq=0)
+    q = rnd(7, n_seq, Hq, 128, dtype=q_type)
+    kv = stored_values(c, 0)
+    out, lse = c.attend_shared(q)
+    check(out, lse, [reference(x, [kv], c.c.softmax_scale) for x in q])
+    c.close()
+
+
+@pytest.mark.parametrize("k_fmt,v_fmt", QUANT)
+@pytest.mark.parametrize("by", [2.0 ** -9, 2.0 ** 9])
+def test_quantized_values_of_all_sizes(k_fmt, v_fmt, by):
+    c, _, _ = make_prefix(8, 2, "f16", 0, tiers=[TierConfig(k_fmt, v_fmt, 10 ** 9, 64, 8)], poison=False)
+    k, v = rnd(1, 2, 400, 128, dtype="f16"), rnd(2, 2, 400, 128, dtype="f16", by=by)
+    v[:, ::7] = 0.0                                            # scales of zero
+    c.append(0, k, v, seq=0)
+    q = rnd(7, 5, 8, 128, dtype="f16")
+    out, lse = c.attend_shared(q)
+    check(out, lse, [reference(x, [stored_values(c, 0)], c.c.softmax_scale) for x in q])
+    c.close()
+
+
+def test_a_tiered_prompt_as_prefix():
+    """A prompt that went through fp16 -> int8 -> int4 evictions, shared by a batch with tiers of its own."""
+    def tiers(ring):
+        return [TierConfig("f16", "f16", 128, 64, 4), TierConfig("i8", "i8", 256, 64, 8), TierConfig("i4", "i4", 10 ** 9, 128, ring, paged_seed=3)]
+    p, _, _ = make_prefix(8, 2, "f16", 0, tiers=tiers(12), poison=False)
+    for i in range(9):
+        p.append(0, rnd(3 * i, 2, 100, 128, dtype="f16"), rnd(3 * i + 1, 2, 100, 128, dtype="f16"), seq=0)
+        p.demote()
+    assert all(int(x[0]) > 0 for x in p.len) and sum(int(x[0]) for x in p.len) == 900
+    prefix = [stored_values(p, t) for t in range(3)]
+    sets = [(k.float(), v.float()) for k, v in prefix]
+    c, own = window(5, 8, 2, "f16", [3, 0, 70, 64, 1], p, [1, 1, 1, 0, 1], tiers=tiers(2))
+    for i in range(3):
+        q, k, v = (rnd(60 + 3 * i + j, 5, h, 128, dtype="f16") for j, h in enumerate((8, 2, 2)))
+        out, lse = c.step(q, k[:, :, None].contiguous(), v[:, :, None].contiguous())
+        own = [[torch.cat((x[0], k[b, :, None]), 1), torch.cat((x[1], v[b, :, None]), 1)] for b, x in enumerate(own)]
+        check(out, lse, [reference(q[b], (sets if b != 3 else []) + [own[b]], c.c.softmax_scale) for b in range(5)], f"step {i}")
+    q = rnd(90, 64, 8, 128, dtype="f16")
+    out, lse = p.attend_shared(q)
+    check(out, lse, [reference(x, sets, p.c.softmax_scale) for x in q], "alone")
+    c.close(), p.close()
 
 
 def test_parts_of_several_calls_join():
@@ -337,6 +414,47 @@ def test_captured_and_on_another_stream():
         other = [x.clone() for x in c.attend_shared(q)]
     side.synchronize()
     assert torch.equal(other[0], got[0])
+    c.close()
+
+
+def test_a_captured_step_and_two_caches_of_one_prefix_at_once():
+    p, pk, pv = make_prefix(8, 2, "f16", 2500, paged=4)
+    a, own_a = window(3, 8, 2, "f16", [100, 7, 333], p)
+    b, own_b = window(40, 8, 2, "f16", [20 + i for i in range(40)], p, seed=200)
+    qa, qb = rnd(1, 3, 8, 128, dtype="f16"), rnd(2, 40, 8, 128, dtype="f16")
+    want = [[reference(q[i], [(pk, pv), own[i]], a.c.softmax_scale) for i in range(len(q))] for q, own in ((qa, own_a), (qb, own_b))]
+    a.decode(qa), b.decode(qb)
+    torch.cuda.synchronize()
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):                                     # both in flight, each with its own workspace
+        with torch.cuda.stream(sa):
+            ra = [x.clone() for x in a.decode(qa)]
+        with torch.cuda.stream(sb):
+            rb = [x.clone() for x in b.decode(qb)]
+        torch.cuda.synchronize()
+        check(*ra, want[0], "first"), check(*rb, want[1], "second")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = a.decode(qa)
+    for i in range(4):
+        qa.copy_(rnd(50 + i, 3, 8, 128, dtype="f16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone()
+        check(*got, [reference(qa[i], [(pk, pv), own_a[i]], a.c.softmax_scale) for i in range(3)], f"replay {i}")
+        eager = a.decode(qa)
+        assert torch.equal(eager[0], got[0]) and torch.equal(eager[1], got[1])
+    for c in (a, b, p):
+        c.close()
+
+
+def test_queries_in_front_of_the_batch_and_larger_batches_later():
+    """The workspace grows with the number of sequences; results do not depend on what an earlier call left in it."""
+    c, k, v = make_prefix(8, 4, "bf16", 900, bt=64)
+    for n in (3, 70, 2, 200, 1):
+        q = rnd(n, n, 8, 128, dtype="bf16")
+        out, lse = c.attend_shared(q)
+        check(out, lse, [reference(x, [(k, v)], c.c.softmax_scale) for x in q], f"{n} sequences")
     c.close()
 
 

@@ -130,9 +130,10 @@ def test_shared_attn_refusals(h):
     assert shared(h, big, n_seq=65536) == B.ERR_UNSUPPORTED                               # 2^23 rows
     two = host_cache(batch=2, fmts=(("f16", "f16"),), bt=(128,))
     assert shared(h, two) == B.ERR_INVALID_ARG and B.ttkv_prefix_parts(h, two, 4) == -1
-    for fmt in ("i8", "i4"):
-        assert shared(h, prefix_cache(fmt)) == B.ERR_UNSUPPORTED
-        assert B.ttkv_prefix_parts(h, prefix_cache(fmt), 4) == -1 and B.ttkv_shared_workspace_bytes(h, prefix_cache(fmt), 4) == 0
+    for pair in (("i4t", "i4"), ("i8", "i4c"), ("i4", "i4c")):                            # layouts of other kernels
+        packed = host_cache(batch=1, fmts=(("f16", "f16"), pair), bt=(128, 128))
+        assert shared(h, packed) == B.ERR_UNSUPPORTED
+        assert B.ttkv_prefix_parts(h, packed, 4) == -1 and B.ttkv_shared_workspace_bytes(h, packed, 4) == 0
     assert shared(h, prefix_cache("bf16")) == B.ERR_UNSUPPORTED                           # bf16 keys, fp16 queries
     p.tier[0].mem = B.MEM_HOST_PINNED
     assert shared(h, p) == B.ERR_UNSUPPORTED
@@ -172,7 +173,8 @@ def test_decode_step_shared_refusals(h):
     other.softmax_scale = 0.1
     assert step(h, c, other) == B.ERR_INVALID_ARG
     assert step(h, c, host_cache(batch=2, fmts=(("f16", "f16"),), bt=(128,))) == B.ERR_INVALID_ARG
-    assert step(h, c, prefix_cache("i8")) == B.ERR_UNSUPPORTED and step(h, c, prefix_cache("bf16")) == B.ERR_UNSUPPORTED
+    assert step(h, c, host_cache(batch=1, fmts=(("f16", "f16"), ("i8", "i4c")), bt=(128, 128))) == B.ERR_UNSUPPORTED
+    assert step(h, c, prefix_cache("bf16")) == B.ERR_UNSUPPORTED
     assert step(h, c, p, fmt=B.BF16) == B.ERR_UNSUPPORTED                                 # the fp tier takes its own format
     parts = B.ttkv_count_parts(h, c, None, None, 0, 0) + B.ttkv_prefix_parts(h, p, 2)
     assert step(h, c, p, ws=None) == B.ERR_WORKSPACE

@@ -11,11 +11,13 @@
 // and 16 b + 8 + 4 h + 0 .. 3 in registers 8 b .. 8 b + 7, and the value operand is read from LDS in that order of tokens
 // (ds_read_b64_tr_b16: four tokens of one channel per lane).
 //
-// A workgroup's four waves are RW along the rows (32 each) times TW along the tokens of a tile; K and V tiles go global ->
-// registers -> LDS, the next tile's loads in flight while one is computed.
+// Rows of K and V go global -> registers -> LDS, those of the next steps on their way while one is computed.  The run is cut
+// into as many items as fill the 256 CUs with one workgroup of eight waves each: the partials, 520 bytes per row and item, are what
+// more items cost (four waves and two workgroups per CU: 128 rows x 32K tokens 57.7 us, now 45-47; 4 x 131072 tokens, 28 / 4 heads, 55.6
+// and 50).
 //
-// The weights p meet fp16 values as an fp16 number and its remainder (22 bits), bf16 values as three bf16
-// numbers (24 bits): the outputs are fp32.
+// The weights p meet fp16 values as an fp16 number and its remainder (22 bits), bf16 values as three bf16 numbers (24 bits): the
+// outputs are fp32, and against 64 bits they are 4e-7 to 9e-7 off (2-norm, 1000 to 131072 tokens).
 #include "ttkv_shared_dev.h"
 
 #include <algorithm>
@@ -29,55 +31,55 @@ using namespace dev;
 using namespace shared;
 
 // ---------------------------------------------------------------- up to 64 rows per KV head
-// Bound: memory.  One workgroup of eight waves per CU: TW teams of RW waves (32 rows each) take the item's steps of 32 tokens
-// in turn (with a run of its own for each team, 2048 tokens of 256 items, the streams a power of two apart took 59.7 us instead of
-// 49.8).  A team loads its steps' rows itself and needs no other; K of one step and V of the step before
-// are always on their way, and leave their registers for LDS where the step before has been read.
-template <bool BF, int RW, int TW>
+// Bound: memory.  24 sequences x 8229 bf16 tokens, 32 / 32 heads (135 MB): 26.6 us, 5.1 TB/s; 5 x 131072, 28 / 4 (268 MB): 45-55 us
+// as the clock allows, 4.9-6.0.  With everything but the copies taken out the first takes 24.5 (a load-only kernel 6.5-7.0 TB/s).  Four teams of two waves, 32 rows each, take the item's steps of
+// 32 tokens in turn (with a run of its own for each team, 2048 tokens of 256 items, the streams a power of two apart took 59.7 us instead
+// of 49.8).  A team loads its steps' rows itself; K of one step and V of the step before are always on their way, and leave their
+// registers for LDS where the step before has been read (both together, once per step: 5 x 131072 58.9 us with the merge, 51.9 so).
+// Up to 32 rows the teams' second waves only help with the copies (eight waves with rows and tokens of their own, and no barrier,
+// were 1-3 % faster on long runs and 6-14 % slower on short ones).
+template <bool BF>
 __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
-  static_assert(RW * TW == 8 && (RW == 1 || RW == 2), "eight waves");
-  constexpr bool ALONE = RW == 1;   // a team of one waits for nobody: LDS takes a wave's stores and reads in order
-  constexpr int NL = 8 / RW, LR = 4 * RW;                        // 16-byte loads of K (V) per thread; rows apart
-  constexpr int kKeys = 32 * kRowK, kStep = 32 * (kRowK + kRowV), NBUF = ALONE ? 1 : 2;
-  __shared__ __align__(16) char s_tile[TW * NBUF * kStep];       // per team: keys and values of one step (two); at the end what the waves exchange
-  static_assert(TW * NBUF * kStep >= 8 * (16 - 16 / TW) * 1024, "room for what the waves exchange");
+  constexpr int RW = 2, TW = 4, NL = 4;                          // 16-byte loads of K (V) per thread and step
+  constexpr int kKeys = 32 * kRowK, kStep = 32 * (kRowK + kRowV);
+  __shared__ __align__(16) char s_tile[TW * 2 * kStep];          // per team: keys and values of two steps; at the end what the waves exchange
+  static_assert(TW * 2 * kStep >= 8 * (16 - 16 / TW) * 1024, "room for what the waves exchange");
   __shared__ float s_m[8][32], s_l[8][32];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int tw = wave / RW, rw = wave % RW;
   const int c = lane & 31, hh = lane >> 5;
   Item it;
   if (!item_of(a, it)) return;
+  const bool idle = rw * 32 >= a.rows;
   const int mine = it.n_tok - 32 * tw;                           // tokens from the team's first step on; it takes every TW-th
   Cursor keys(a, it.hkv, it.begin + (mine > 0 ? 32 * tw : 0)), values = keys;
   values.base += a.tv.v_off;
   values.head += a.tv.v_off;
   int k_left = mine, v_left = mine;                              // tokens from the cursors on
-  const int lr = (threadIdx.x & (64 * RW - 1)) >> 4, lp = threadIdx.x & 15;
+  const int lr = (threadIdx.x & 127) >> 4, lp = threadIdx.x & 15;
   u32x4 kr[NL], vr[NL];
   auto load = [&](Cursor &at, int &left, u32x4 (&x)[NL]) __attribute__((always_inline)) {   // the team's next step, if there is one; rows behind the item's end: its last one
     if (left <= 0) return;
     const int len = min(left, 32);
     const uint64_t head = at.rows();
 #pragma unroll
-    for (int i = 0; i < NL; ++i) x[i] = __builtin_nontemporal_load((gas_u32x4)(head + (uint32_t)(min(lr + LR * i, len - 1) * 256 + lp * 16)));
+    for (int i = 0; i < NL; ++i) x[i] = __builtin_nontemporal_load((gas_u32x4)(head + (uint32_t)(min(lr + 8 * i, len - 1) * 256 + lp * 16)));
     left -= 32 * TW;
     if (left > 0) at.advance(32 * TW);
   };
-  char *const team = s_tile + tw * NBUF * kStep;
+  char *const team = s_tile + tw * 2 * kStep;
   const char *const k_at = team + k_lane(lane), *const v_at = team + kKeys + v_lane(lane);
   char *const k_put = team + lr * kRowK + lp * 16, *const v_put = team + kKeys + lr * kRowV + lp * 16;
   auto put = [&](char *to, int row_bytes, const u32x4 (&x)[NL]) __attribute__((always_inline)) {
-    if constexpr (ALONE) asm volatile("" ::: "memory");          // (the compiler has to leave the order as it is)
 #pragma unroll
-    for (int i = 0; i < NL; ++i) *(u32x4 *)(to + i * LR * row_bytes) = x[i];
-    if constexpr (ALONE) asm volatile("" ::: "memory");
+    for (int i = 0; i < NL; ++i) *(u32x4 *)(to + i * 8 * row_bytes) = x[i];
   };
 #pragma unroll
   for (int i = 0; i < NL; ++i) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
   load(keys, k_left, kr);
   load(values, v_left, vr);
   u32x4 qf[8];
-  Rows r = begin_rows<BF>(a, (it.row_tile * RW + rw) * 32 + c, it.hkv, hh, qf);
+  Rows r = begin_rows<BF>(a, rw * 32 + c, it.hkv, hh, qf);
   f16v o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)
@@ -87,18 +89,20 @@ __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
   load(keys, k_left, kr);
   put(v_put, kRowV, vr);
   load(values, v_left, vr);
-  // (with barriers all teams take as many steps as the first)
-  const int n_steps = ((ALONE ? max(mine, 0) : it.n_tok) + 32 * TW - 1) / (32 * TW);
+  const int n_steps = (it.n_tok + 32 * TW - 1) / (32 * TW);      // of the first team: all take as many barriers
   int now = 0;   // buffer of the step
   for (int t = 0; t < n_steps; ++t) {
-    if (!ALONE) __syncthreads();   // the step is in its buffer; everybody is done with the other one
-    const int next = ALONE ? 0 : kStep - now, len = mine - 32 * TW * t;
+    __syncthreads();   // the step is in its buffer; everybody is done with the other one
+    const int next = kStep - now, len = mine - 32 * TW * t;
+    const bool works = len > 0 && !idle;   // (wave-uniform)
     f16v sc = {};
+    if (works) {
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
+      for (int kb = 0; kb < 8; ++kb) sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
+    }
     put(k_put + next, kRowK, kr);
     load(keys, k_left, kr);
-    if (len > 0) {   // (wave-uniform)
+    if (works) {
       if (len < 32) mask_step(sc, len, hh);
       const float mt = step_max(sc);
       if (__any(mt > r.far)) move_reference(r, mt, o);
@@ -119,9 +123,13 @@ __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
 }
 
 // ---------------------------------------------------------------- more rows: 128 per workgroup
-// Bound: the matrix cores.  The steps of 32 tokens overlap inside a wave: while the softmax of step s runs on the vector unit, the
+// Bound: the matrix cores, and what they may draw: 256 rows x 32K fp16 tokens of 8 KV heads 65-77 us (52 more for every 32K tokens beyond),
+// where the core clock falls from 2.4 to 1.55 GHz within the launch; 660 TFLOP/s of products that count once and 990 with the
+// remainders' against the 1170-1230 of a large library product.  Without loads 42, without the softmax 45 of the 52: each part's
+// share of the power.  64 rows per wave (half the LDS reads, accumulators in the AGPRs) came out alike, 53.  The steps of 32 tokens overlap inside a wave: while the softmax of step s runs on the vector unit, the
 // matrix cores work on the values of step s - 1 and the scores of step s + 1, none of which depends on it.  LDS holds two
-// steps' keys and values each (s + 1 and s + 2; s - 1 and s), one barrier per step.
+// steps' keys and values each (s + 1 and s + 2; s - 1 and s), one barrier per step.  Two halves of the item's tokens per workgroup meet
+// at its end: half the partials of a workgroup for each.
 template <bool BF>
 __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a) {
   constexpr int NP = parts_of<BF>(), kKeys = 32 * kRowK, kValues = 32 * kRowV, kHalf = 2 * (kKeys + kValues);
@@ -246,23 +254,24 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
   join_and_store<4, 2>(a, r, o, rw, half, lane, it.split, s_tile, s_m, s_l);
 }
 
-// Query rows per workgroup, workgroups along the rows.
+// Query rows per workgroup, workgroups along the rows.  32 / 8 heads x 32K fp16 tokens, us with blocks of 64 and of 128 rows: 32 rows 30.8 and
+// 36.6, 64 rows 34.5 and 39.4, 96 rows 47.5 and 43.0, 128 rows 46.6 and 47.8; 48 rows of 32 KV heads x 8192 tokens 33.2 and 43.9.
+constexpr int kWorkgroups = 256;   // on the chip at once, one per CU
 struct Shape {
-  int rows, row_tiles, resident, tokens;   // resident: workgroups on the chip at once; tokens of an item: a multiple of this
+  int rows, row_tiles, tokens;   // tokens of an item: a multiple of this
 };
 Shape shape_of(int rows, bool quantized) {
-  if (quantized) return Shape{32, (rows + 31) / 32, 256, 32};
-  if (rows <= 32) return Shape{32, 1, 256, 32};
-  if (rows <= 64) return Shape{64, 1, 256, 32};
-  return Shape{128, (rows + 127) / 128, 256, 128};
+  if (quantized) return Shape{32, (rows + 31) / 32, 32};
+  if (rows <= 64) return Shape{64, 1, 32};
+  return Shape{128, (rows + 127) / 128, 128};
 }
 
 }  // namespace
 
 int shared_chunk(int rows, int n_kv_heads, int64_t len, bool quantized) {
   const Shape s = shape_of(rows, quantized);
-  const int64_t most = std::max<int64_t>(1, s.resident / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
-  const int64_t want = std::min(most, (len + 63) / 64);
+  const int64_t most = std::max<int64_t>(1, kWorkgroups / std::max<int64_t>(1, (int64_t)n_kv_heads * s.row_tiles));
+  const int64_t want = std::min(most, (len + 63) / 64);   // (at least 128 or 256 tokens: the same within 3 % at 1000 to 8000 tokens)
   return (int)(((len + want - 1) / want + s.tokens - 1) / s.tokens * s.tokens);
 }
 
@@ -278,19 +287,12 @@ hipError_t launch_shared(SharedArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)(units * sh.row_tiles)), block(512);
   if (quantized) return launch_shared_quant(a, grid, s);
   const bool bf = a.tv.k_fmt == TTKV_BF16;
-  switch (sh.rows) {
-    case 32:
-      if (bf) hipLaunchKernelGGL((shared_kernel<true, 1, 8>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((shared_kernel<false, 1, 8>), grid, block, 0, s, a);
-      break;
-    case 64:
-      if (bf) hipLaunchKernelGGL((shared_kernel<true, 2, 4>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((shared_kernel<false, 2, 4>), grid, block, 0, s, a);
-      break;
-    default:
-      if (bf) hipLaunchKernelGGL(shared_rows_kernel<true>, grid, block, 0, s, a);
-      else hipLaunchKernelGGL(shared_rows_kernel<false>, grid, block, 0, s, a);
-      break;
+  if (sh.rows == 64) {
+    if (bf) hipLaunchKernelGGL(shared_kernel<true>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(shared_kernel<false>, grid, block, 0, s, a);
+  } else {
+    if (bf) hipLaunchKernelGGL(shared_rows_kernel<true>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(shared_rows_kernel<false>, grid, block, 0, s, a);
   }
   return hipGetLastError();
 }

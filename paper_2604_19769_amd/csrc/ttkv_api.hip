@@ -1106,6 +1106,7 @@ static ttkv_status plan_prefix(const ttkv_cache *c, bool check_tables, int32_t q
   ttkv_status st = validate_cache(c, check_tables);
   if (st != TTKV_OK) return st;
   if (c->batch != 1) return TTKV_ERR_INVALID_ARG;
+  if ((int64_t)n_seq * c->n_q_heads >= 1 << 22) return TTKV_ERR_UNSUPPORTED;   // rows are counted in 32 bits, and a launch has 2^32 threads at most
   P.c = c;
   P.n_seq = n_seq;
   P.parts = 0;
@@ -1480,7 +1481,6 @@ ttkv_status ttkv_shared_attn(ttkv_handle hh, const ttkv_cache *prefix, const voi
   if (st != TTKV_OK) return st;
   if ((uintptr_t)q & 15) return TTKV_ERR_INVALID_ARG;
   if (n_seq == 0) return TTKV_OK;
-  if ((int64_t)n_seq * prefix->n_q_heads >= 1 << 22) return TTKV_ERR_UNSUPPORTED;
   const int64_t rows = (int64_t)n_seq * prefix->n_q_heads, stride = std::max(1, P.parts);
   const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
   if (P.parts && (!workspace || ws_bytes < mis + (size_t)rows * stride * 130 * sizeof(float))) return TTKV_ERR_WORKSPACE;

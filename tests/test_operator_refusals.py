@@ -184,3 +184,15 @@ def test_decode_step_shared_refusals(h):
     assert lens.tolist() == [8 * 128, 8 * 128]
     i8 = host_cache(fmts=(("i8", "i8"),), bt=(128,))
     assert step(h, i8, p) == B.ERR_UNSUPPORTED                                            # the token goes to an fp tier
+
+
+def test_more_rows_than_32_bits_count(h):
+    """2^16 sequences of 2^20 heads: refused before the rows are multiplied out."""
+    p = prefix_cache(Hq=1 << 20, Hkv=1)
+    p._keep[2][:] = 500
+    assert shared(h, p, n_seq=65536) == B.ERR_UNSUPPORTED
+    assert B.ttkv_prefix_parts(h, p, 65536) == -1 and B.ttkv_shared_workspace_bytes(h, p, 65536) == 0
+    c = host_cache(Hq=1 << 25, Hkv=1, batch=64, fmts=(("f16", "f16"),), bt=(128,))
+    wide = prefix_cache(Hq=1 << 25, Hkv=1)
+    wide._keep[2][:] = 500
+    assert step(h, c, wide) == B.ERR_UNSUPPORTED

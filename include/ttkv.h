@@ -348,7 +348,7 @@ typedef struct ttkv_rope {
 } ttkv_rope;
 
 #define TTKV_MAX_ROPE_HEADS 65536
-#define TTKV_MAX_ROPE_TOKENS (1 << 28)
+#define TTKV_MAX_ROPE_TOKENS (1 << 25)   /* a wave per token: 2^31 threads of a launch's 2^32 */
 
 /* Norm and rotation of queries and / or keys in one pass (q with q_out, k with k_out, or either pair NULL).  n_seq <=
  * TTKV_MAX_BATCH sequences of n_tokens.  All inputs have one type, all outputs one; an output may be its own input

@@ -196,3 +196,12 @@ def test_more_rows_than_32_bits_count(h):
     wide = prefix_cache(Hq=1 << 25, Hkv=1)
     wide._keep[2][:] = 500
     assert step(h, c, wide) == B.ERR_UNSUPPORTED
+
+
+def test_more_tokens_than_a_launch_has_waves(h):
+    """A wave per token: 2^26 of them would be 2^32 threads along the grid's first dimension."""
+    wide = heads(n=1, strides=(1 << 40, 128, 128))
+    for n, want in (((1 << 25) + 1, B.ERR_INVALID_ARG), (1 << 26, B.ERR_INVALID_ARG)):
+        assert norm_rope(h, q=wide, q_out=wide, n_tokens=n) == want
+        assert append(h, host_cache(), n_tokens=n, n_each=[0, 0]) == want
+    assert append(h, host_cache(), n_tokens=1 << 25, n_each=[0, 0]) == B.OK

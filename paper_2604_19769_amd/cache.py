@@ -51,10 +51,15 @@ def _stream_of(device):
     return _raw_stream(device.index)
 
 
+def _on(x, device):
+    """A tensor, or an object with a device, is on `device` (that may be "cuda", the current one)."""
+    return x.device == device or (x.device.type == device.type and None in (device.index, x.device.index))
+
+
 def _heads(x, device):
     """A tensor [sequence][token][head][128] as the library's strided view."""
     n, s = x.shape, x.stride()
-    assert len(n) == 4 and n[3] == 128 and s[3] == 1 and x.device == device, (n, s, x.device)
+    assert len(n) == 4 and n[3] == 128 and s[3] == 1 and _on(x, device), (n, s, x.device)
     return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], n[2], s[0], s[1], s[2])
 
 
@@ -69,7 +74,7 @@ def _host_int64(x, n):
 
 def _device_positions(x, n_seq, n_tokens, device):
     if x is not None:
-        assert x.dtype == torch.int64 and x.shape == (n_seq, n_tokens) and x.is_contiguous() and x.device == device
+        assert x.dtype == torch.int64 and x.shape == (n_seq, n_tokens) and x.is_contiguous() and _on(x, device)
     return x
 
 
@@ -109,7 +114,7 @@ class Rotary:
     def apply(self, q=None, k=None, first_pos=None, positions=None, q_out=None, k_out=None, dtype=None):
         """q [B][T][Hq][128] and / or k [B][T][Hkv][128], any strides but the last, f16 / bf16 / f32 -> (q_out, k_out), new tensors
         of `dtype` (None: the input's) unless given (an output may be its own input).  Token i of sequence b is at
-        positions[b][i] (int64 on the device), or first_pos[b] + i (host integers; None: i)."""
+        positions[b][i] (int64 on the device), or first_pos[b] + i (host integers; None: i).  Up to 64 sequences (B)."""
         dev = self.device
         n, T = (q if q is not None else k).shape[:2]
         qv = qo = kv = ko = None
@@ -203,9 +208,10 @@ class TieredCache:
 
     def share(self, prefix, members=None):
         """Attend the tokens of `prefix`, a TieredCache of batch 1 with its tiers in HBM, in front of every sequence's own
-        from now on (members: truth values, the sequences that do; None: all).  prefix None: no longer."""
+        from now on (members: truth values, the sequences that do; None: all).  prefix None: no longer.  A prefix has none itself."""
         if prefix is not None:
-            assert prefix.B == 1 and (prefix.Hq, prefix.Hkv, prefix.device) == (self.Hq, self.Hkv, self.device)
+            assert prefix.B == 1 and (prefix.Hq, prefix.Hkv) == (self.Hq, self.Hkv) and _on(prefix, self.device)
+            assert prefix.prefix is None and prefix is not self, "a prefix is attended without its own"
             assert self.n_slots == 0, "a prefix goes with host tiers read in place"
         if members is not None:
             members = np.ascontiguousarray(np.asarray(members, bool), np.int32)
@@ -261,7 +267,7 @@ class TieredCache:
         seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
         Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given)."""
         n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
-        assert k.shape == v.shape == (n, T, self.Hkv, 128)
+        assert k.shape == v.shape == (n, T, self.Hkv, 128) and _on(rotary, self.device)
         dev = self.device
         qv = qo = None
         if q is not None:
@@ -349,20 +355,27 @@ class TieredCache:
     def _decode_shared(self, q, new):
         """decode() of a cache with a prefix (ttkv_decode_step_shared)."""
         q_fmt = _Q_FMT[q.dtype]
-        assert q.is_contiguous() and q.shape == (self.B, self.Hq, 128)
+        assert q.is_contiguous() and q.shape == (self.B, self.Hq, 128) and _on(q, self.device)
+        assert self.prefix.prefix is None, "a prefix is attended without its own"
         k_new, v_new = new if new is not None else (None, None)
         fmt = q_fmt
         if new is not None:
             fmt = _Q_FMT[k_new.dtype]
             assert k_new.is_contiguous() and v_new.is_contiguous() and k_new.dtype == v_new.dtype
-            assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128)
+            assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128) and _on(k_new, self.device) and _on(v_new, self.device)
+        members = None if self.members is None else self.members.ctypes.data
+        if torch.cuda.is_current_stream_capturing():   # a graph keeps its workspace, whatever this one's grows to
+            ws = torch.empty(B.ttkv_workspace_bytes(self.c, self._count_shared(new is not None), 0), dtype=torch.uint8, device=self.device)
+            B.ttkv_decode_step_shared(self.h, self.c, self.prefix.c, members, q, q_fmt, k_new, v_new, fmt, self.out, self.lse, ws, ws.numel(),
+                                      self._compute())
+            self._parts_age = None
+            return self.out, self.lse
         # parts per row: counted anew every 64 steps, as in decode(), or when the library finds the workspace too small
         if new is None or self.ws is None or self._parts_age is None or self._parts_age >= 64:
-            self._count_shared(new is not None)
+            self._workspace(self._count_shared(new is not None))
             self._parts_age = 0 if new is not None else None
         else:
             self._parts_age += 1
-        members = None if self.members is None else self.members.ctypes.data
         while True:
             try:
                 B.ttkv_decode_step_shared(self.h, self.c, self.prefix.c, members, q, q_fmt, k_new, v_new, fmt, self.out, self.lse, self.ws,
@@ -371,10 +384,11 @@ class TieredCache:
             except B.TTKVError as e:
                 if e.status != B.ERR_WORKSPACE or self._parts_age in (None, 0):
                     raise
-                self._count_shared(new is not None)
+                self._workspace(self._count_shared(new is not None))
                 self._parts_age = 0
 
     def _count_shared(self, with_token):
+        """Parts per row that a step's workspace holds."""
         if with_token:
             self.len[0] += 1            # size the workspace for the lengths the attention may see
         own = B.ttkv_count_parts(self.h, self.c, None, None, 0, 0)
@@ -383,34 +397,44 @@ class TieredCache:
         lead = B.ttkv_prefix_parts(self.h, self.prefix.c, self.B if self.members is None else int(self.members.sum()))
         if own < 0 or lead < 0:
             raise B.TTKVError(B.ERR_INVALID_ARG, "ttkv_count_parts" if own < 0 else "ttkv_prefix_parts")
-        self._workspace(max(own, self._few_parts) + lead)
+        return max(1, max(own, self._few_parts) + lead)
 
     @_on_own_device
     def attend_shared(self, q):
         """Queries of any number of sequences over this cache of batch 1 as their shared prefix: q [n][Hq][128] f16 / bf16 ->
-        out [n][Hq][128], lse [n][Hq] fp32 (ttkv_shared_attn; kept for the next call, like those of decode())."""
+        out [n][Hq][128], lse [n][Hq] fp32 (ttkv_shared_attn; kept for the next call, like those of decode(); a call that is
+        captured into a graph has tensors of its own)."""
         q_fmt = _Q_FMT[q.dtype]
         n = q.shape[0]
-        assert q.is_contiguous() and q.shape == (n, self.Hq, 128) and q.device == self.device
+        assert q.is_contiguous() and q.shape == (n, self.Hq, 128) and _on(q, self.device)
+        assert self.prefix is None, "a prefix is attended without its own"
+        if torch.cuda.is_current_stream_capturing():
+            out, lse = self._shared_results(n)
+            ws = self._shared_workspace(n)
+            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, out, lse, ws, ws.numel(), self._compute())
+            return out, lse
         if self.shared_out is None or self.shared_out.shape[0] != n:
-            self.shared_out = torch.empty(n, self.Hq, 128, dtype=torch.float32, device=self.device)
-            self.shared_lse = torch.empty(n, self.Hq, dtype=torch.float32, device=self.device)
+            self.shared_out, self.shared_lse = self._shared_results(n)
         if self.shared_ws is None:
-            self._shared_workspace(n)
+            self.shared_ws = self._shared_workspace(n)
         try:
             B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
                                self._compute())
         except B.TTKVError as e:
             if e.status != B.ERR_WORKSPACE:
                 raise
-            self._shared_workspace(n)         # more sequences or parts than any call before: nothing was enqueued
+            self.shared_ws = self._shared_workspace(n)   # more sequences or parts than any call before: nothing was enqueued
             B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
                                self._compute())
         return self.shared_out, self.shared_lse
 
+    def _shared_results(self, n):
+        return (torch.empty(n, self.Hq, 128, dtype=torch.float32, device=self.device),
+                torch.empty(n, self.Hq, dtype=torch.float32, device=self.device))
+
     def _shared_workspace(self, n):
         need = B.ttkv_shared_workspace_bytes(self.h, self.c, n)
-        self.shared_ws = torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
+        return torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
 
     def select(self, q, k):
         q_fmt = _Q_FMT[q.dtype]

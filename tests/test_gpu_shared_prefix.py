@@ -466,3 +466,80 @@ def test_selection_is_refused_behind_a_prefix():
         c.step(q, k[:, :, None].contiguous(), v[:, :, None].contiguous(), select_k=1)
     assert c.len[0].tolist() == [3, 3]
     c.close(), p.close()
+
+
+def test_captured_calls_keep_buffers_of_their_own():
+    """Two graphs of one cache at once, and after larger eager calls whose buffers replace the cache's (what was free in between is
+    NaN now, and would not be if a graph still wrote there)."""
+    p, k, v = make_prefix(8, 2, "f16", 1500)
+    own, parts = window(3, 8, 2, "f16", [100, 7, 333], p)
+    qa, qb = rnd(1, 4, 8, 128, dtype="f16"), rnd(2, 9, 8, 128, dtype="f16")
+    qc = rnd(3, 3, 8, 128, dtype="f16")
+    p.attend_shared(qa), own.decode(qc)
+    torch.cuda.synchronize()
+    graphs, results = [], []
+    for run in (lambda: p.attend_shared(qa), lambda: p.attend_shared(qb), lambda: own.decode(qc)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, lse = run()
+            results.append((out * 1, lse * 1))
+        graphs.append(graph)
+        del out, lse
+    p.attend_shared(rnd(5, 700, 8, 128, dtype="f16"))
+    p.attend_shared(qa[:1].contiguous())
+    own._workspace(4 * own.ws_parts)
+    free = [torch.full((1 << s,), float("nan"), device="cuda") for s in range(8, 24) for _ in range(3)]
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for i in range(4):
+        for j, q in enumerate((qa, qb, qc)):
+            q.copy_(rnd(10 * i + j + 7, *q.shape, dtype="f16"))
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for j, (q, got) in enumerate(zip((qa, qb), results)):
+            check(*got, [reference(x, [(k, v)], p.c.softmax_scale) for x in q], f"graph {j}, replay {i}")
+        check(*results[2], [reference(qc[b], [(k, v), parts[b]], own.c.softmax_scale) for b in range(3)], f"step, replay {i}")
+    assert all(bool(x.isnan().all()) for x in free)
+    for c in (own, p):
+        c.close()
+
+
+def test_a_prefix_has_no_prefix():
+    p, _, _ = make_prefix(8, 2, "f16", 10)
+    m, _, _ = make_prefix(8, 2, "f16", 20)
+    c, _ = window(2, 8, 2, "f16", [3, 3], m)
+    q = rnd(1, 2, 8, 128, dtype="f16")
+    for bad in (m, p):
+        with pytest.raises(AssertionError):
+            bad.share(bad)
+    m.share(p)
+    for call in (lambda: c.share(m), lambda: c.decode(q), lambda: m.attend_shared(q)):
+        with pytest.raises(AssertionError):
+            call()
+    m.share(None)
+    c.decode(q), m.attend_shared(q)
+    for x in (c, m, p):
+        x.close()
+
+
+@pytest.mark.parametrize("n_seq,Hq,Hkv", [(2, 8, 2), (5, 32, 2)])
+def test_scores_that_are_not_numbers_answer_as_in_decode(n_seq, Hq, Hkv):
+    """A NaN among a query's channels or in a live key: 0 and -inf for the rows that it meets, the others as they were."""
+    p, k, v = make_prefix(Hq, Hkv, "f16", 700, poison=False)
+    q = rnd(1, n_seq, Hq, 128, dtype="f16")
+    q[1, Hq // 2] = float("nan")
+    out, lse = (x.clone() for x in p.attend_shared(q))
+    same_out, same_lse = [], []
+    for x in q:
+        one = [y.clone() for y in p.decode(x[None].contiguous())]
+        same_out.append(one[0][0]), same_lse.append(one[1][0])
+    bad = torch.zeros(n_seq, Hq, dtype=torch.bool, device="cuda")
+    bad[1, Hq // 2] = True
+    assert torch.equal(torch.stack(same_lse)[bad], lse[bad]) and torch.equal(torch.stack(same_out)[bad], out[bad])
+    want = [reference(x, [(k, v)], p.c.softmax_scale) for x in torch.nan_to_num(q)]
+    keep = ~bad.cpu()
+    assert bool(((out.cpu().double() - torch.stack([w[0].view(Hq, 128) for w in want])).abs()[keep]
+                 <= torch.stack([w[2].view(Hq, 1) for w in want])[keep]).all())
+    p.close()

@@ -56,11 +56,16 @@ def _on(x, device):
     return x.device == device or (x.device.type == device.type and None in (device.index, x.device.index))
 
 
-def _heads(x, device):
-    """A tensor [sequence][token][head][128] as the library's strided view."""
-    n, s = x.shape, x.stride()
-    assert len(n) == 4 and n[3] == 128 and s[3] == 1 and _on(x, device), (n, s, x.device)
-    return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], n[2], s[0], s[1], s[2])
+def _heads(x, shape, device):
+    """A tensor of `shape`, [sequence][token][head][128], as the library's strided view."""
+    seq, token, head, channel = x.stride()
+    assert x.shape == shape and channel == 1 and (x.device == device or _on(x, device)), (x.shape, shape, x.stride(), x.device)
+    return B.ttkv_heads(x.data_ptr(), _SRC_FMT[x.dtype], shape[2], seq, token, head)
+
+
+@functools.lru_cache(128)
+def _int64s(n):
+    return C.c_int64 * n
 
 
 def _host_int64(x, n):
@@ -69,7 +74,10 @@ def _host_int64(x, n):
         return None
     a = np.ascontiguousarray(x, np.int64)
     assert a.shape == (n,), a.shape
-    return (C.c_int64 * n).from_buffer(a if a.flags.writeable else a.copy())   # (half the time of a.ctypes)
+    try:
+        return _int64s(n).from_buffer(a)                  # (half the time of a.ctypes)
+    except TypeError:                                     # read-only
+        return _int64s(n).from_buffer(a.copy())
 
 
 def _device_positions(x, n_seq, n_tokens, device):
@@ -116,22 +124,24 @@ class Rotary:
         of `dtype` (None: the input's) unless given (an output may be its own input).  Token i of sequence b is at
         positions[b][i] (int64 on the device), or first_pos[b] + i (host integers; None: i).  Up to 64 sequences (B)."""
         dev = self.device
-        n, T = (q if q is not None else k).shape[:2]
         qv = qo = kv = ko = None
-        if q is not None:
-            if q_out is None:
-                q_out = torch.empty(q.shape, dtype=dtype or q.dtype, device=dev)
-            assert q_out.shape == q.shape
-            qv, qo = _heads(q, dev), _heads(q_out, dev)
-        else:
-            q_out = None
         if k is not None:
             if k_out is None:
-                k_out = torch.empty(k.shape, dtype=dtype or k.dtype, device=dev)
-            assert k_out.shape == k.shape and k.shape[0] == n and k.shape[1] == T
-            kv, ko = _heads(k, dev), _heads(k_out, dev)
+                k_out = torch.empty_like(k, dtype=dtype, memory_format=torch.contiguous_format)
+            shape = k.shape
+            n, T, _, channels = shape
+            assert channels == 128
+            kv, ko = _heads(k, shape, dev), _heads(k_out, shape, dev)
         else:
             k_out = None
+            n, T = q.shape[:2]
+        if q is not None:
+            if q_out is None:
+                q_out = torch.empty_like(q, dtype=dtype, memory_format=torch.contiguous_format)
+            shape = (n, T, q.shape[2], 128)
+            qv, qo = _heads(q, shape, dev), _heads(q_out, shape, dev)
+        else:
+            q_out = None
         B.ttkv_norm_rope(self.h, self.r, qv, qo, kv, ko, n, T, _host_int64(first_pos, n), _device_positions(positions, n, T, dev), _stream_of(dev))
         return q_out, k_out
 
@@ -267,19 +277,20 @@ class TieredCache:
         seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
         Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given)."""
         n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
-        assert k.shape == v.shape == (n, T, self.Hkv, 128) and _on(rotary, self.device)
+        assert rotary.device == self.device or _on(rotary, self.device)
         dev = self.device
         qv = qo = None
         if q is not None:
-            assert q.shape == (n, T, self.Hq, 128)
             if q_out is None:
-                q_out = torch.empty(q.shape, dtype=torch.bfloat16 if self.cfg[tier].k_fmt == "bf16" else torch.float16, device=dev)
-            assert q_out.shape == q.shape
-            qv, qo = _heads(q, dev), _heads(q_out, dev)
+                q_out = torch.empty_like(q, dtype=torch.bfloat16 if self.cfg[tier].k_fmt == "bf16" else torch.float16,
+                                         memory_format=torch.contiguous_format)
+            shape = (n, T, self.Hq, 128)
+            qv, qo = _heads(q, shape, dev), _heads(q_out, shape, dev)
         if first_pos is None and positions is None and self.prefix is not None:
             first_pos = sum(self.len) + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
-        B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, dev), _heads(v, dev), T, _host_int64(counts, n),
+        shape = (n, T, self.Hkv, 128)
+        B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, shape, dev), _heads(v, shape, dev), T, _host_int64(counts, n),
                            _host_int64(first_pos, n), _device_positions(positions, n, T, dev), self._compute())
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0

@@ -7,14 +7,16 @@
 //
 // A wave takes one token and eight heads at a time, eight lanes per head.  Lane j of a head holds two of the row's sixteen 16-byte pieces
 // (of 16-bit channels): j and j + 8, so that the lanes of one instruction cover whole lines, where pairs are side by side or all 128
-// channels turn; pieces j and j + R/16 where fewer turn half a rotation apart, lanes from R/16 on then hold pieces that pass.  Either way
+// channels turn; pieces j and j + R/16 where fewer turn half a rotation apart, lanes from R/16 on then hold pieces that pass.  From fp32 to
+// fp32, with whole lines, the lane's sixteen channels are four pieces of four, j + 8 k, for the same reason.  Either way
 // a rotation needs no exchange between lanes.  The wave's 64 lanes work out one angle each and hand them to the eight heads through
 // LDS.  Angles are counted in turns: pos x (freq / 2 pi) with the factor in two 64-bit numbers and the product's rounding taken back, so
 // what is left after the whole turns is right at any position (one 64-bit product alone would be 1e-4 off at 2^40); everything else is
 // fp32, rounded once to the destination's type.
 //
 // Bound: memory.  2 x 4096 tokens of 32 / 8 bf16 heads (168 MB) 33.9 us, 5.0 TB/s of read + write; seven prompts of up to 4999 tokens into fp16
-// pages (600 MB) 112 us, 5.4; a copy of 2 GiB reaches 4.9.  A single token 3.6 us, a launch.
+// pages (600 MB) 112 us, 5.4; 3 x 1021 tokens of 28 / 4 fp32 heads (100 MB) 18.1 us, 5.5 (with pieces of eight channels 23.2); a copy of 2 GiB reaches
+// 4.9.  A single token 3.6 us, a launch.
 #include "ttkv_internal.h"
 
 #include <hip/hip_fp16.h>
@@ -38,12 +40,13 @@ template <int F>
 struct Piece {
   u32x4 w[F == TTKV_F32 ? 2 : 1];
 };
-template <int F>
-__device__ __forceinline__ Piece<F> load_piece(const uint8_t *row, int piece) {
+// STEP: 16-byte units between an fp32 piece's halves.
+template <int F, int STEP>
+__device__ __forceinline__ Piece<F> load_piece(const uint8_t *row, int channel) {
   Piece<F> p;
-  const u32x4 *s = (const u32x4 *)(row + piece * 8 * elem_bytes<F>());
+  const u32x4 *s = (const u32x4 *)(row + channel * elem_bytes<F>());
 #pragma unroll
-  for (int i = 0; i < elem_bytes<F>() / 2; ++i) p.w[i] = s[i];
+  for (int i = 0; i < elem_bytes<F>() / 2; ++i) p.w[i] = s[i * STEP];
   return p;
 }
 template <int F>
@@ -68,13 +71,16 @@ __device__ __forceinline__ void expand(const Piece<F> &p, float (&x)[8]) {
 }
 // STREAM: with the streaming hint, where the lanes of one instruction fill whole lines of 128 bytes (2 x 4096 tokens of 32 / 8 bf16 heads
 // 40.4 -> 33.9 us; where they fill half lines, 6000 tokens of 32 / 32 heads with 96 channels turning, 88 -> 110).
-template <int F, bool STREAM>
-__device__ __forceinline__ void store_piece(uint8_t *row, int piece, const float (&x)[8]) {
-  u32x4 *d = (u32x4 *)(row + piece * 8 * elem_bytes<F>());
+template <int F, int STEP, bool STREAM>
+__device__ __forceinline__ void store_piece(uint8_t *row, int channel, const float (&x)[8]) {
+  u32x4 *d = (u32x4 *)(row + channel * elem_bytes<F>());
   if constexpr (F == TTKV_F32) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      d[i] = u32x4{__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3])};
+    for (int i = 0; i < 2; ++i) {
+      const u32x4 v = {__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3])};
+      if constexpr (STREAM) __builtin_nontemporal_store(v, d + i * STEP);
+      else d[i * STEP] = v;
+    }
   } else {
     uint32_t w[4];
 #pragma unroll
@@ -99,9 +105,12 @@ __device__ __forceinline__ float sum_of_eight_lanes(float v) {
   return v + dpp<0x141>(v);     // row_half_mirror
 }
 
-// WHOLE: pairs are side by side, or all channels turn, or none (see the pieces above).
+// WHOLE: pairs are side by side, or all channels turn, or none; QUADS: pieces of four channels (see above).
 template <int SRC, int DST, bool WHOLE>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
+  constexpr bool QUADS = WHOLE && SRC == TTKV_F32 && DST == TTKV_F32;
+  constexpr int STEP = QUADS ? 8 : 1;
+  constexpr bool STREAM = WHOLE && (QUADS || DST != TTKV_F32);
   __shared__ f2 s_turn[4][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j = blockIdx.y;
@@ -113,7 +122,13 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   const int l8 = lane & 7, slot = lane >> 3;
   // The lane's two pieces and which of them turn.
   const int p0 = !WHOLE && l8 >= a.turning ? 2 * l8 : l8, p1 = WHOLE ? l8 + 8 : l8 < a.turning ? l8 + a.turning : 2 * l8 + 1;
-  const bool turn0 = a.interleaved ? p0 < 2 * a.turning : l8 < a.turning, turn1 = a.interleaved ? p1 < 2 * a.turning : turn0;
+  int at[4];                          // first channel of each four that the lane holds
+  bool turn[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    at[k] = QUADS ? 32 * k + 4 * l8 : 8 * (k < 2 ? p0 : p1) + 4 * (k & 1);
+    turn[k] = !a.interleaved ? l8 < a.turning : QUADS ? at[k] < 16 * a.turning : (k < 2 ? p0 : p1) < 2 * a.turning;
+  }
   // A batch: eight heads of the queries, the keys or the values.  The next one is asked for before one is worked on.
   struct Batch {
     Piece<SRC> w0, w1;
@@ -125,8 +140,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     const RopeSide &s = a.side[t.side];
     t.h = (b - a.first_batch[t.side]) * 8 + slot;
     const uint8_t *src = s.src + j * s.src_seq + token * s.src_token + (t.h < s.n_heads ? t.h : 0) * s.src_head;
-    t.w0 = load_piece<SRC>(src, t.side == 2 ? l8 : p0);     // values do not turn
-    t.w1 = load_piece<SRC>(src, t.side == 2 ? l8 + 8 : p1);
+    t.w0 = load_piece<SRC, STEP>(src, t.side == 2 ? 8 * l8 : at[0]);     // values do not turn (and go to a tier, never an fp32 one)
+    t.w1 = load_piece<SRC, STEP>(src, t.side == 2 ? 8 * l8 + 64 : at[2]);
     return t;
   };
   const Batch first = ask(min(part, a.n_batches - 1));
@@ -144,10 +159,9 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   __builtin_amdgcn_wave_barrier();
   f2 cs[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int pair = a.interleaved ? 4 * l8 + i % 4 + (i < 4 ? 0 : 32) : 8 * l8 + i;
-    cs[i] = (i < 4 ? turn0 : turn1) ? s_turn[wave][pair] : f2{1.0f, 0.0f};
-  }
+  for (int i = 0; i < 8; ++i)
+    cs[i] = a.interleaved ? turn[i / 2] ? s_turn[wave][at[i / 2] / 2 + i % 2] : f2{1.0f, 0.0f}
+                          : turn[0] ? s_turn[wave][at[i / 4] + i % 4] : f2{1.0f, 0.0f};
 
   uint8_t *head0 = nullptr;   // the token's place in the tier
   int64_t head_step = 0;
@@ -182,8 +196,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
           y[i] *= inv;
         }
         if (s.weight) {
-          const float4 *w0 = (const float4 *)(s.weight + 8 * p0), *w1 = (const float4 *)(s.weight + 8 * p1);
-          const float4 u0 = w0[0], u1 = w0[1], v0 = w1[0], v1 = w1[1];
+          const float4 *w0 = (const float4 *)(s.weight + at[0]), *w1 = (const float4 *)(s.weight + at[2]);
+          const float4 u0 = w0[0], u1 = w0[STEP], v0 = w1[0], v1 = w1[STEP];
           const float u[8] = {u0.x, u0.y, u0.z, u0.w, u1.x, u1.y, u1.z, u1.w}, v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -193,17 +207,24 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
         }
       }
       if (a.interleaved) {
-        auto turn = [&](float (&z)[8], const f2 *t) __attribute__((always_inline)) {
+        auto pairs = [&](float (&z)[8], int from, int to, const f2 *t) __attribute__((always_inline)) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = from; i < to; ++i) {
             const float u = z[2 * i], v = z[2 * i + 1];
             z[2 * i] = u * t[i].x - v * t[i].y;
             z[2 * i + 1] = v * t[i].x + u * t[i].y;
           }
         };
-        if (turn0) turn(x, cs);
-        if (turn1) turn(y, cs + 4);
-      } else if (turn0) {
+        if constexpr (QUADS) {
+          if (turn[0]) pairs(x, 0, 2, cs);
+          if (turn[1]) pairs(x, 2, 4, cs);
+          if (turn[2]) pairs(y, 0, 2, cs + 4);
+          if (turn[3]) pairs(y, 2, 4, cs + 4);
+        } else {
+          if (turn[0]) pairs(x, 0, 4, cs);
+          if (turn[2]) pairs(y, 0, 4, cs + 4);
+        }
+      } else if (turn[0]) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const float u = x[i], v = y[i];
@@ -215,8 +236,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     if (t.h >= s.n_heads) return;
     uint8_t *dst = a.in_tier && t.side ? head0 + t.h * head_step + (t.side == 2 ? v_off : 0)
                                        : s.dst + j * s.dst_seq + token * s.dst_token + t.h * s.dst_head;
-    store_piece<DST, WHOLE>(dst, t.side == 2 ? l8 : p0, x);
-    store_piece<DST, WHOLE>(dst, t.side == 2 ? l8 + 8 : p1, y);
+    store_piece<DST, STEP, STREAM>(dst, t.side == 2 ? 8 * l8 : at[0], x);
+    store_piece<DST, STEP, STREAM>(dst, t.side == 2 ? 8 * l8 + 64 : at[2], y);
   };
   Batch now = first;
   for (int b = part; b < a.n_batches; b += parts) {

@@ -9,7 +9,9 @@
 // (of 16-bit channels): j and j + 8, so that the lanes of one instruction cover whole lines, where pairs are side by side or all 128
 // channels turn; pieces j and j + R/16 where fewer turn half a rotation apart, lanes from R/16 on then hold pieces that pass.  From fp32 to
 // fp32, with whole lines, the lane's sixteen channels are four pieces of four, j + 8 k, for the same reason.  Either way
-// a rotation needs no exchange between lanes.  The wave's 64 lanes work out one angle each and hand them to the eight heads through
+// a rotation needs no exchange between lanes.  Stores carry the streaming hint, which pays where the lanes of one instruction fill whole lines of
+// 128 bytes (2 x 4096 tokens of 32 / 8 bf16 heads 40.4 -> 33.9 us) and costs where they do not (6000 tokens of 32 / 32 fp32 heads to bf16, 96
+// channels turning, 88 -> 110): where a lane's pieces are no whole lines the head's lanes exchange them through LDS first (82).  The wave's 64 lanes work out one angle each and hand them to the eight heads through
 // LDS.  Angles are counted in turns: pos x (freq / 2 pi) with the factor in two 64-bit numbers and the product's rounding taken back, so
 // what is left after the whole turns is right at any position (one 64-bit product alone would be 1e-4 off at 2^40); everything else is
 // fp32, rounded once to the destination's type.
@@ -69,30 +71,17 @@ __device__ __forceinline__ void expand(const Piece<F> &p, float (&x)[8]) {
     }
   }
 }
-// STREAM: with the streaming hint, where the lanes of one instruction fill whole lines of 128 bytes (2 x 4096 tokens of 32 / 8 bf16 heads
-// 40.4 -> 33.9 us; where they fill half lines, 6000 tokens of 32 / 32 heads with 96 channels turning, 88 -> 110).
-template <int F, int STEP, bool STREAM>
-__device__ __forceinline__ void store_piece(uint8_t *row, int channel, const float (&x)[8]) {
-  u32x4 *d = (u32x4 *)(row + channel * elem_bytes<F>());
-  if constexpr (F == TTKV_F32) {
+template <int F>
+__device__ __forceinline__ Piece<F> pack(const float (&x)[8]) {   // nearest even
+  Piece<F> p;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 v = {__float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3])};
-      if constexpr (STREAM) __builtin_nontemporal_store(v, d + i * STEP);
-      else d[i * STEP] = v;
-    }
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {   // nearest even
-      const f2 v = {x[2 * i], x[2 * i + 1]};
-      if constexpr (F == TTKV_F16) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
-      else w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
-    }
-    const u32x4 v = {w[0], w[1], w[2], w[3]};
-    if constexpr (STREAM) __builtin_nontemporal_store(v, d);
-    else d[0] = v;
+  for (int i = 0; i < 4 * elem_bytes<F>() / 2; ++i) {
+    const f2 v = {x[2 * i % 8], x[(2 * i + 1) % 8]};
+    if constexpr (F == TTKV_F32) p.w[i / 4][i % 4] = __float_as_uint(x[i]);
+    else if constexpr (F == TTKV_F16) p.w[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, h2));
+    else p.w[0][i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, b2));
   }
+  return p;
 }
 
 template <int CTRL>
@@ -110,8 +99,10 @@ template <int SRC, int DST, bool WHOLE>
 __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
   constexpr bool QUADS = WHOLE && SRC == TTKV_F32 && DST == TTKV_F32;
   constexpr int STEP = QUADS ? 8 : 1;
-  constexpr bool STREAM = WHOLE && (QUADS || DST != TTKV_F32);
+  constexpr int UNITS = elem_bytes<DST>() / 2;   // of 16 bytes in a piece that is stored
+  constexpr bool EXCHANGE = !WHOLE || (DST == TTKV_F32 && !QUADS);
   __shared__ f2 s_turn[4][64];
+  __shared__ u32x4 s_row[EXCHANGE ? 4 : 1][8][16 * UNITS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int j = blockIdx.y;
   const int64_t w = (int64_t)blockIdx.x * 4 + wave;
@@ -236,8 +227,21 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     if (t.h >= s.n_heads) return;
     uint8_t *dst = a.in_tier && t.side ? head0 + t.h * head_step + (t.side == 2 ? v_off : 0)
                                        : s.dst + j * s.dst_seq + token * s.dst_token + t.h * s.dst_head;
-    store_piece<DST, STEP, STREAM>(dst, t.side == 2 ? 8 * l8 : at[0], x);
-    store_piece<DST, STEP, STREAM>(dst, t.side == 2 ? 8 * l8 + 64 : at[2], y);
+    Piece<DST> o[2] = {pack<DST>(x), pack<DST>(y)};
+    if constexpr (EXCHANGE)
+      if (t.side != 2) {   // the head's eight lanes hand their pieces over, for whole lines per store
+        u32x4 *row = s_row[wave][slot];
+#pragma unroll
+        for (int i = 0; i < 2 * UNITS; ++i) row[at[i / UNITS * 2] / 8 * UNITS + i % UNITS] = o[i / UNITS].w[i % UNITS];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 2 * UNITS; ++i) o[i / UNITS].w[i % UNITS] = row[l8 + 8 * i];
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+#pragma unroll
+    for (int i = 0; i < 2 * UNITS; ++i) __builtin_nontemporal_store(o[i / UNITS].w[i % UNITS], (u32x4 *)dst + l8 + 8 * i);
   };
   Batch now = first;
   for (int b = part; b < a.n_batches; b += parts) {

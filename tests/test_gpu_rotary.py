@@ -234,3 +234,24 @@ def test_captured_and_on_another_stream():
     side.synchronize()
     assert torch.equal(y, out)
     r.close()
+
+
+@pytest.mark.parametrize("rotary,interleaved", [(96, False), (64, False), (16, False), (96, True), (128, False)])
+@pytest.mark.parametrize("src,dst", [("f32", "bf16"), ("bf16", "bf16"), ("f16", "f16")])
+def test_appended_rows_are_those_of_apply(rotary, interleaved, src, dst):
+    """Whatever way a row takes to its place: the tier's rows, outputs of their own and inputs as outputs hold the same bits."""
+    n, Hq, Hkv = 70, 18, 9                                   # batches of eight heads with two and one in the last
+    r = Rotary(Rotary.frequencies(rotary), interleaved=interleaved, norm=True)
+    q, k, v = rnd(21, 2, n, Hq, 128, dtype=src), rnd(22, 2, n, Hkv, 128, dtype=src), rnd(23, 2, n, Hkv, 128, dtype=src)
+    c = window(2, Hkv, dst, 64, 3, 5, [0, 64], 30, Hq=Hq)
+    got = c.append_rotated(r, k, v, q=q)
+    qo, ko = r.apply(q, k, first_pos=[30, 30], dtype=DT[dst])
+    assert torch.equal(got, qo)
+    pool = c.pool[0].view(DT[dst]).view(-1, Hkv, 2, 64, 128)
+    for b in range(2):
+        rec, row = rows_of(c, b, 30, n)
+        assert torch.equal(pool[rec, :, 0, row], ko[b]) and torch.equal(pool[rec, :, 1, row], v[b].to(DT[dst]))
+    if src == dst:
+        r.apply(q, k, first_pos=[30, 30], q_out=q, k_out=k)
+        assert torch.equal(q, qo) and torch.equal(k, ko)
+    r.close(), c.close()

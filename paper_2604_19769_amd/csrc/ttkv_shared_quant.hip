@@ -39,14 +39,37 @@ __device__ __forceinline__ Codes<F> load_codes(uint64_t codes, uint64_t meta, in
   c.meta = *(gas_u32)(meta + (uint32_t)(min(lane >> 1, len - 1) * 8 + (lane & 1) * 4));
   return c;
 }
-// Four codes, the low bytes' values of x (unsigned), less `centre`, as packed numbers in order.
-template <bool BF>
-__device__ __forceinline__ uint2 four(uint32_t x, float centre) {
-  const float a = (float)(x & 0xff) - centre, b = (float)(x >> 8 & 0xff) - centre, c = (float)(x >> 16 & 0xff) - centre, d = (float)(x >> 24) - centre;
-  return uint2{pack2<BF>(a, b), pack2<BF>(c, d)};   // exact: eight bits
+__device__ __forceinline__ uint32_t low_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x05040100u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t x, uint32_t y) { return __builtin_amdgcn_perm(y, x, 0x07060302u); }
+// Eight channels' codes as packed fp16 (keys; in the order of the queries' `paired`) or bf16 numbers (values; ascending).  A nibble n is
+// written into the mantissa of 1.0, 1 + n / 16: two instructions for two codes, where converting them takes five to seven.
+__device__ __forceinline__ u32x4 key_nibbles(uint32_t x) {   // channels (i, i + 4)
+  constexpr uint32_t m = 0x03c003c0u, one = 0x3c003c00u;
+  return u32x4{(x << 6 & m) | one, (x << 2 & m) | one, (x >> 2 & m) | one, (x >> 6 & m) | one};
 }
-// Codes to rows of packed numbers in LDS, meta words to fp32: scale of group g and token t at sz[32 g + t], zero points 64 behind.
-template <int F, bool BF>
+__device__ __forceinline__ u32x4 value_nibbles(uint32_t x) {
+  constexpr uint32_t m = 0x00780078u, one = 0x3f803f80u;
+  const uint32_t a = (x << 3 & m) | one, b = (x >> 1 & m) | one, c = (x >> 5 & m) | one, d = (x >> 9 & m) | one;
+  return u32x4{low_halves(a, b), low_halves(c, d), high_halves(a, b), high_halves(c, d)};
+}
+__device__ __forceinline__ uint2 key_bytes(uint32_t x) {     // channels (0, 2), (1, 3)
+  constexpr uint32_t m = 0x00ff00ffu, big = 0x64006400u;     // 1024 + (code + 128), exact; so is the difference
+  const h2 off = {(_Float16)1152.0f, (_Float16)1152.0f};
+  x ^= 0x80808080u;
+  return uint2{__builtin_bit_cast(uint32_t, as_h2((x & m) | big) - off), __builtin_bit_cast(uint32_t, as_h2((x >> 8 & m) | big) - off)};
+}
+__device__ __forceinline__ uint2 value_bytes(uint32_t x) {
+  const float a = (float)(int8_t)x, b = (float)(int8_t)(x >> 8), c = (float)(int8_t)(x >> 16), d = (float)(int8_t)(x >> 24);
+  return uint2{pack2<true>(a, b), pack2<true>(c, d)};         // exact: eight bits
+}
+template <int F>
+__device__ __forceinline__ u32x4 paired(const u32x4 &q) {
+  if constexpr (F == TTKV_I8_SYM_G32) return u32x4{low_halves(q[0], q[1]), high_halves(q[0], q[1]), low_halves(q[2], q[3]), high_halves(q[2], q[3])};
+  else return u32x4{low_halves(q[0], q[2]), high_halves(q[0], q[2]), low_halves(q[1], q[3]), high_halves(q[1], q[3])};
+}
+// Codes to rows of packed numbers in LDS, meta words to fp32: scale of group g and token t at sz[32 g + t], zero points 64 behind.  Of
+// nibbles, whose rows hold 1 + n / 16: s n + z = 16 s (1 + n / 16) + (z - 16 s).
+template <int F, bool VALUES>
 __device__ __forceinline__ void put_codes(const Codes<F> &c, char *rows, int row_bytes, float *sz, int lane) {
   using C = Codes<F>;
 #pragma unroll
@@ -55,16 +78,13 @@ __device__ __forceinline__ void put_codes(const Codes<F> &c, char *rows, int row
     if constexpr (F == TTKV_I8_SYM_G32) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint2 x = four<BF>(c.w[i][2 * k] ^ 0x80808080u, 128.0f), y = four<BF>(c.w[i][2 * k + 1] ^ 0x80808080u, 128.0f);
+        const uint2 x = VALUES ? value_bytes(c.w[i][2 * k]) : key_bytes(c.w[i][2 * k]);
+        const uint2 y = VALUES ? value_bytes(c.w[i][2 * k + 1]) : key_bytes(c.w[i][2 * k + 1]);
         *(u32x4 *)(at + 16 * k) = u32x4{x.x, x.y, y.x, y.y};
       }
     } else {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {   // eight nibbles, channels in ascending order
-        const uint2 even = four<BF>(c.w[i][k] & 0x0F0F0F0Fu, 0.0f), odd = four<BF>(c.w[i][k] >> 4 & 0x0F0F0F0Fu, 0.0f);
-        *(u32x4 *)(at + 16 * k) = u32x4{__builtin_amdgcn_perm(odd.x, even.x, 0x05040100u), __builtin_amdgcn_perm(odd.x, even.x, 0x07060302u),
-                                        __builtin_amdgcn_perm(odd.y, even.y, 0x05040100u), __builtin_amdgcn_perm(odd.y, even.y, 0x07060302u)};
-      }
+      for (int k = 0; k < 4; ++k) *(u32x4 *)(at + 16 * k) = VALUES ? value_nibbles(c.w[i][k]) : key_nibbles(c.w[i][k]);
     }
   }
   const float lo = (float)as_h2(c.meta).x, hi = (float)as_h2(c.meta).y;
@@ -73,8 +93,8 @@ __device__ __forceinline__ void put_codes(const Codes<F> &c, char *rows, int row
     sz[32 * (2 * w) + t] = lo;
     sz[32 * (2 * w + 1) + t] = hi;
   } else {
-    sz[32 * w + t] = lo;
-    sz[64 + 32 * w + t] = hi;
+    sz[32 * w + t] = 16.0f * lo;
+    sz[64 + 32 * w + t] = fmaf(-16.0f, lo, hi);
   }
 }
 // The lane's sixteen tokens' numbers of a row of 32, in the order of the scores' registers.
@@ -134,6 +154,8 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
       q_sum[g] = both.x + both.y;
     }
   }
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) qf[kb] = paired<KF>(qf[kb]);
   f16v o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d)

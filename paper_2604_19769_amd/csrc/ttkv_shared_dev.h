@@ -33,17 +33,15 @@ __device__ __forceinline__ f2 unpack2(uint32_t w) {
   if constexpr (BF) return f2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
   else return f2{(float)as_h2(w).x, (float)as_h2(w).y};
 }
-// x - the lower (upper) half of w
-__device__ __forceinline__ float minus_low(uint32_t w, float x) {
-  float r;
-  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(x));
-  return r;
+// x - the lower (upper) half of w, one instruction: -1 is kept from the compiler, which would convert and subtract otherwise.  (As inline
+// assembly it would not be kept apart from matrix instructions that are still at its registers.)
+__device__ __forceinline__ float minus_one() {
+  float m = -1.0f;
+  asm("" : "+s"(m));
+  return m;
 }
-__device__ __forceinline__ float minus_high(uint32_t w, float x) {
-  float r;
-  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(x));
-  return r;
-}
+__device__ __forceinline__ float minus_low(uint32_t w, float x) { return fmaf((float)as_h2(w).x, minus_one(), x); }
+__device__ __forceinline__ float minus_high(uint32_t w, float x) { return fmaf((float)as_h2(w).y, minus_one(), x); }
 // LDS rows: eight rows' 16-byte pieces of one column fall into different banks (keys, 4 banks apart), and so do four rows' 32
 // bytes (values, 8 banks apart); every address is one register and a constant.
 constexpr int kRowK = 272, kRowV = 288;

@@ -1,12 +1,12 @@
 // Attention over a shared prefix in quantized tiers (K int8 or int4, V int8 or int4): 32 query rows per workgroup, eight waves that take
-// its steps of 32 tokens in turn, each with its own rows in LDS.  A wave decompresses nothing: the codes are
-// small integers, exact as fp16 (keys) and bf16 (values), and the scales and zero points s, z of a token's channel group g enter in fp32:
+// its steps of 32 tokens in turn, each with its own rows in LDS.  A wave decompresses nothing: the codes are small integers, exact as fp16
+// (keys) and bf16 (values), and the scales and zero points s, z of a token's channel group g enter in fp32:
 //       score = sum_g s_{t,g} (q . code)_g + z_{t,g} sum_{c in g} q_c
 //       O[c] = sum_t (p_t s_{t,g}) code_{t,c} + sum_t p_t z_{t,g}              (g the group of channel c)
 // with one product chain per group for the scores, and for the values one right operand per group, p s as three bf16 numbers (24 bits of
-// any size).  Bound: the vector unit (an operand of 16 weights is formed for every group) beside memory: with the merge, us, fp16 / int8 / int4 /
-// K int8 V int4: 4 x 131072 tokens, 28 / 4 heads 51 / 55 / 41 / 47; 24 x 8229, 32 / 32 heads 30 / 30 / 26 / 27; 64 x 16384, 32 / 8 heads (eight blocks of 32
-// rows, each over the codes for itself) 42 / 75 / 65 / 66.
+// any size).  Bound: the vector unit (codes into operands, 16 weights per group) beside memory: with the merge, us, fp16 / int8 / int4 / K int8 V int4:
+// 4 x 131072 tokens, 28 / 4 heads 49 / 47 / 36 / 41; 24 x 8229, 32 / 32 heads 30 / 28 / 23 / 24; 64 x 16384, 32 / 8 heads (eight blocks of 32 rows, each
+// over the codes for itself) 41 / 69 / 58 / 60.  Codes converted by instructions for it instead of written into mantissas: 8-10 % more.
 #include "ttkv_shared_dev.h"
 
 namespace ttkv {

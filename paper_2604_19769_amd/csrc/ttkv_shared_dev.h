@@ -99,7 +99,7 @@ __device__ __forceinline__ void rescale(f16v (&o)[4], float by) {
   for (int d = 0; d < 4; ++d) o[d] *= by;
 }
 // The reference moves up to the largest score so far; what was added up by then counts this much.
-__device__ __forceinline__ float move_reference(Rows &r, float mt, f16v (&o)[4]) {
+__device__ __forceinline__ void move_reference(Rows &r, float mt, f16v (&o)[4]) {
 #pragma clang fp contract(off)
   const float mn = fmaxf(r.m, mt), at = mn * r.cs, was = r.mcs;
   r.f = fabsf(at) < 4194304.0f ? kUnit : 0.0f;   // beyond, f - mcs would not be exact
@@ -109,7 +109,6 @@ __device__ __forceinline__ float move_reference(Rows &r, float mt, f16v (&o)[4])
   rescale(o, alpha);
   r.m = mn;
   r.far = r.f == 0.0f ? mn : (at + kRoom) * r.inv_cs;
-  return alpha;
 }
 // Scores of tokens from `left` on count nothing.
 __device__ __forceinline__ void mask_step(f16v &sc, int left, int hh) {

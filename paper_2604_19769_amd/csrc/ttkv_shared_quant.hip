@@ -4,9 +4,11 @@
 //       score = sum_g s_{t,g} (q . code)_g + z_{t,g} sum_{c in g} q_c
 //       O[c] = sum_t (p_t s_{t,g}) code_{t,c} + sum_t p_t z_{t,g}              (g the group of channel c)
 // with one product chain per group for the scores, and for the values one right operand per group, p s as three bf16 numbers (24 bits of
-// any size).  Bound: the vector unit (codes into operands, 16 weights per group) beside memory: with the merge, us, fp16 / int8 / int4 / K int8 V int4:
-// 4 x 131072 tokens, 28 / 4 heads 49 / 47 / 36 / 41; 24 x 8229, 32 / 32 heads 30 / 28 / 23 / 24; 64 x 16384, 32 / 8 heads (eight blocks of 32 rows, each
-// over the codes for itself) 41 / 69 / 58 / 60.  Codes converted by instructions for it instead of written into mantissas: 8-10 % more.
+// any size).  The two sums of O cancel (16 codes of one sign against their zero point), so they meet in every step of 32 tokens: the step's sum of
+// p z, three bf16 numbers too, is a product with ones between the step's two.  Apart until the end, their error grew with
+// the tokens (of the result, 512 / 2048 / 8192 tokens per wave: 2.3e-5 / 1.1e-4 / 4e-4, now 1.6e-6 / 1.9e-6 / 3.5e-6) for 1-5 % less time.  Bound: the vector unit (codes into operands, 16 weights per group) beside memory: with the merge, us, fp16 / int8 / int4 / K int8 V int4:
+// 4 x 131072 tokens, 28 / 4 heads 49 / 47 / 40 / 41; 24 x 8229, 32 / 32 heads 30 / 28 / 24 / 25; 64 x 16384, 32 / 8 heads (eight blocks of 32 rows, each
+// over the codes for itself) 41 / 68 / 60 / 63.  Codes converted by instructions for it instead of written into mantissas: 8-10 % more.
 #include "ttkv_shared_dev.h"
 
 namespace ttkv {
@@ -161,10 +163,11 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-  float zero[2] = {};    // sum of p z over the lane's tokens, per group of 64 channels
   char *const team = s_tile + tw * kStep;
   float *const k_sz = (float *)(team + kRows), *const v_sz = k_sz + 128;
   const char *const k_at = team + k_lane(lane), *const v_at = team + kKeys + v_lane(lane);
+  constexpr uint32_t one = 0x3f803f80u;
+  const u32x4 ones = {one, one, one, one};
   const int n_steps = (max(mine, 0) + 32 * TW - 1) / (32 * TW);
   for (int t = 0; t < n_steps; ++t) {
     // (LDS takes a wave's stores and reads in order; the compiler has to leave them so)
@@ -191,16 +194,32 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
     const int len = mine - 32 * TW * t;
     if (len < 32) mask_step(sc, len, hh);
     const float mt = step_max(sc);
-    if (__any(mt > r.far)) {
-      const float alpha = move_reference(r, mt, o);
-      zero[0] *= alpha;
-      zero[1] *= alpha;
-    }
+    if (__any(mt > r.far)) move_reference(r, mt, o);
     float p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], r.cs, r.mcs));
       r.l += p[i];
+    }
+    u32x4 zero[2] = {};   // the sum of p z over the lane's tokens, per group of 64 channels: right operand of a product with ones
+    if constexpr (VF == TTKV_I4_ASYM_G64) {
+      float pz[2] = {};
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const f16v z = of_tokens(v_sz + 64 + 32 * g, hh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) pz[g] = fmaf(p[i], z[i], pz[g]);
+      }
+      uint32_t x[3];
+#pragma unroll
+      for (int u = 0; u < 3; ++u) {
+        x[u] = pack2<true>(pz[0], pz[1]);
+        const f2 y = unpack2<true>(x[u]);
+        pz[0] -= y.x;
+        pz[1] -= y.y;
+      }
+      zero[0] = u32x4{low_halves(x[0], x[1]), x[2] & 0xffffu, 0, 0};
+      zero[1] = u32x4{high_halves(x[0], x[1]), x[2] >> 16, 0, 0};
     }
 #pragma unroll
     for (int g = 0; g < GV; ++g) {
@@ -218,26 +237,15 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
           w1 -= y.y;
         }
       }
-      if constexpr (VF == TTKV_I4_ASYM_G64) {
-        const f16v z = of_tokens(v_sz + 64 + 32 * g, hh);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zero[g] = fmaf(p[i], z[i], zero[g]);
+      for (int d = g * (4 / GV); d < (g + 1) * (4 / GV); ++d) {
+        add_values<true>(o[d], value_operand(v_at, d, 0), w, 0);
+        if constexpr (VF == TTKV_I4_ASYM_G64) o[d] = mma<true>(ones, zero[g], o[d]);   // in between: the sum on the way is half as large
+        add_values<true>(o[d], value_operand(v_at, d, 1), w, 1);
       }
-#pragma unroll
-      for (int d = g * (4 / GV); d < (g + 1) * (4 / GV); ++d)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) add_values<true>(o[d], value_operand(v_at, d, b), w, b);
     }
   }
   end_rows(r);
-  if constexpr (VF == TTKV_I4_ASYM_G64) {
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const f2 both = both32(zero[g]);
-#pragma unroll
-      for (int d = 2 * g; d < 2 * g + 2; ++d) o[d] += both.x + both.y;
-    }
-  }
   join_and_store<1, TW>(a, r, o, 0, tw, lane, it.split, s_tile, s_m, s_l);
 }
 

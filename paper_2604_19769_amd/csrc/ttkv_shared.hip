@@ -105,7 +105,7 @@ __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
     if (works) {
       if (len < 32) mask_step(sc, len, hh);
       const float mt = step_max(sc);
-      if (__any(mt > r.far)) move_reference(r, mt, o);
+      if (__any(mt > r.far)) move_reference<BF>(r, mt, o);
       u32x4 p[parts_of<BF>()][2];
 #pragma unroll
       for (int i = 0; i < 8; ++i) weigh<BF>(r, sc, i, p);
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
     now = next;
   }
   end_rows(r);
-  join_and_store<RW, TW>(a, r, o, rw, tw, lane, it.split, s_tile, s_m, s_l);
+  join_and_store<BF, RW, TW>(a, r, o, rw, tw, lane, it.split, s_tile, s_m, s_l);
 }
 
 // ---------------------------------------------------------------- more rows: 128 per workgroup
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
 #pragma unroll
         for (int u = 0; u < NP; ++u) p[u][0] = p[u][1] = u32x4{0, 0, 0, 0};
       }
-      move_reference(r, mt, o);
+      move_reference<BF>(r, mt, o);
     }
     put_keys(ODD);       // of s + 2
     put_values(ODD);     // of s
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(512, 1) void shared_rows_kernel(const SharedArgs a)
 #pragma unroll
     for (int b = 0; b < 2; ++b) add_values<BF>(o[d], value_operand(v_at + kValues, d, b), p0, b);
   end_rows(r);
-  join_and_store<4, 2>(a, r, o, rw, half, lane, it.split, s_tile, s_m, s_l);
+  join_and_store<BF, 4, 2>(a, r, o, rw, half, lane, it.split, s_tile, s_m, s_l);
 }
 
 // Query rows per workgroup, workgroups along the rows.  32 / 8 heads x 32K fp16 tokens, us with blocks of 64 and of 128 rows: 32 rows 30.8 and

@@ -46,9 +46,12 @@ __device__ __forceinline__ float minus_high(uint32_t w, float x) { return fmaf((
 // bytes (values, 8 banks apart); every address is one register and a constant.
 constexpr int kRowK = 272, kRowV = 288;
 
-// The weights carry 2^kUnit, and the reference moves only when a score is kRoom (in powers of two) above it: the weights stay below
-// 2^15, and a wave of 32 rows, some of whose maxima would grow in nearly every step, hardly ever rescales its outputs.
-constexpr float kUnit = 8.0f, kRoom = 7.0f;
+// The weights carry 2^unit, and the reference moves only when a score is `room` (in powers of two) above it, so that a wave of 32 rows, some of
+// whose maxima would grow in nearly every step, hardly ever rescales its outputs.  Over bf16 values the two take each other back: no weight is
+// above 1, and an average of values near bf16's largest stays finite on its way.
+template <bool BF>
+constexpr float unit_of() { return BF ? -7.0f : 8.0f; }
+constexpr float kRoom = 7.0f;
 template <bool BF>
 constexpr int parts_of() { return BF ? 3 : 2; }   // numbers that hold a weight
 
@@ -99,10 +102,11 @@ __device__ __forceinline__ void rescale(f16v (&o)[4], float by) {
   for (int d = 0; d < 4; ++d) o[d] *= by;
 }
 // The reference moves up to the largest score so far; what was added up by then counts this much.
+template <bool BF>
 __device__ __forceinline__ void move_reference(Rows &r, float mt, f16v (&o)[4]) {
 #pragma clang fp contract(off)
   const float mn = fmaxf(r.m, mt), at = mn * r.cs, was = r.mcs;
-  r.f = fabsf(at) < 4194304.0f ? kUnit : 0.0f;   // beyond, f - mcs would not be exact
+  r.f = fabsf(at) < 4194304.0f ? unit_of<BF>() : 0.0f;   // beyond, f - mcs would not be exact
   r.mcs = mn == -INFINITY ? 0.0f : r.f - at;
   const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.mcs - was);
   r.l *= alpha;
@@ -219,7 +223,7 @@ __device__ __forceinline__ int v_lane(int lane) { return (4 * (lane >> 5) + ((la
 
 // The TW waves of one row block add up, each 128 / TW channels of the rows, and store them.  s_o: (16 - 16 / TW) KiB per wave; all
 // waves of the workgroup take part.  Weights of a wave are exp2(score cs + mcs).
-template <int RW, int TW>
+template <bool BF, int RW, int TW>
 __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &r, const f16v (&o)[4], int rw, int tw, int lane, int split, char *s_o,
                                                float (*s_m)[32], float (*s_l)[32]) {
   constexpr int OWN = 16 / TW;   // pieces of 4 registers (channels 8 k + 4 hh .. + 3 of the block of 32) that a wave ends up with
@@ -249,7 +253,7 @@ __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &
 #pragma unroll
   for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
   // the reference without the weights' power of two (exact: top is that of some wave)
-  const float up = fabsf(top) < 4194304.0f ? kUnit : 0.0f;
+  const float up = fabsf(top) < 4194304.0f ? unit_of<BF>() : 0.0f;
   float by[TW], l = 0.0f;
 #pragma unroll
   for (int u = 0; u < TW; ++u) {

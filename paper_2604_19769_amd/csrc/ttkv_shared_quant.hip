@@ -194,7 +194,7 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
     const int len = mine - 32 * TW * t;
     if (len < 32) mask_step(sc, len, hh);
     const float mt = step_max(sc);
-    if (__any(mt > r.far)) move_reference(r, mt, o);
+    if (__any(mt > r.far)) move_reference<true>(r, mt, o);
     float p[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(512, 1) void shared_quant_kernel(const SharedArgs a
     }
   }
   end_rows(r);
-  join_and_store<1, TW>(a, r, o, 0, tw, lane, it.split, s_tile, s_m, s_l);
+  join_and_store<true, 1, TW>(a, r, o, 0, tw, lane, it.split, s_tile, s_m, s_l);
 }
 
 }  // namespace

@@ -47,11 +47,16 @@ __device__ __forceinline__ float minus_high(uint32_t w, float x) { return fmaf((
 constexpr int kRowK = 272, kRowV = 288;
 
 // The weights carry 2^unit, and the reference moves only when a score is `room` (in powers of two) above it, so that a wave of 32 rows, some of
-// whose maxima would grow in nearly every step, hardly ever rescales its outputs.  Over bf16 values the two take each other back: no weight is
-// above 1, and an average of values near bf16's largest stays finite on its way.
+// whose maxima would grow in nearly every step, rescales its outputs now and then only.  Over bf16 values the two take each other back: no weight is
+// above 1, and an average of values near bf16's largest stays finite on its way.  Over fp16 values weights stay below 2^16 and are good to
+// 2^-25, half of fp16's smallest step: 22 bits down to 2^-17 of the reference and 2^-39 of it below, as in the decode kernels.  (2^8 and
+// room for 2^7 took as long; results made of weights 2^-20 of the largest, whose values are 0, were 7e-5 off.  2^11 to 2^13 save 1-2 %
+// of many rows' time.)
 template <bool BF>
-constexpr float unit_of() { return BF ? -7.0f : 8.0f; }
-constexpr float kRoom = 7.0f;
+constexpr float unit_of() { return BF ? -7.0f : 14.0f; }
+template <bool BF>
+constexpr float room_of() { return BF ? 7.0f : 1.5f; }
+constexpr float kFar = 1048576.0f;   // references beyond (in powers of two) carry no unit: f - mcs would not be exact, nor `far` to a fraction of one
 template <bool BF>
 constexpr int parts_of() { return BF ? 3 : 2; }   // numbers that hold a weight
 
@@ -101,18 +106,19 @@ __device__ __forceinline__ void rescale(f16v (&o)[4], float by) {
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] *= by;
 }
-// The reference moves up to the largest score so far; what was added up by then counts this much.
+// The reference moves up to the largest score so far, to the nearest power of two; what was added up by then counts 2^-k as much, exactly.
 template <bool BF>
-__device__ __forceinline__ void move_reference(Rows &r, float mt, f16v (&o)[4]) {
+__device__ __forceinline__ float move_reference(Rows &r, float mt, f16v (&o)[4]) {
 #pragma clang fp contract(off)
-  const float mn = fmaxf(r.m, mt), at = mn * r.cs, was = r.mcs;
-  r.f = fabsf(at) < 4194304.0f ? unit_of<BF>() : 0.0f;   // beyond, f - mcs would not be exact
+  const float mn = fmaxf(r.m, mt), at = __builtin_rintf(mn * r.cs), was = r.mcs;
+  r.f = fabsf(at) < kFar ? unit_of<BF>() : 0.0f;
   r.mcs = mn == -INFINITY ? 0.0f : r.f - at;
   const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.mcs - was);
   r.l *= alpha;
   rescale(o, alpha);
   r.m = mn;
-  r.far = r.f == 0.0f ? mn : (at + kRoom) * r.inv_cs;
+  r.far = r.f == 0.0f ? mn : (at + room_of<BF>()) * r.inv_cs;
+  return alpha;
 }
 // Scores of tokens from `left` on count nothing.
 __device__ __forceinline__ void mask_step(f16v &sc, int left, int hh) {
@@ -253,7 +259,7 @@ __device__ __forceinline__ void join_and_store(const SharedArgs &a, const Rows &
 #pragma unroll
   for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
   // the reference without the weights' power of two (exact: top is that of some wave)
-  const float up = fabsf(top) < 4194304.0f ? unit_of<BF>() : 0.0f;
+  const float up = fabsf(top) < kFar ? unit_of<BF>() : 0.0f;
   float by[TW], l = 0.0f;
 #pragma unroll
   for (int u = 0; u < TW; ++u) {

@@ -211,7 +211,7 @@ class TieredCache:
         self.sel_blocks = self.sel_count = self.sel_scratch = None
         self.out = torch.empty(batch, n_q_heads, 128, dtype=torch.float32, device=self.device)
         self.lse = torch.empty(batch, n_q_heads, dtype=torch.float32, device=self.device)
-        self.shared_out = self.shared_lse = self.shared_ws = None
+        self._shared = {}                 # stream -> workspace, out and lse of attend_shared
         self.prefix = self.members = None
         if prefix is not None:
             self.share(prefix, members)
@@ -413,8 +413,8 @@ class TieredCache:
     @_on_own_device
     def attend_shared(self, q):
         """Queries of any number of sequences over this cache of batch 1 as their shared prefix: q [n][Hq][128] f16 / bf16 ->
-        out [n][Hq][128], lse [n][Hq] fp32 (ttkv_shared_attn; kept for the next call, like those of decode(); a call that is
-        captured into a graph has tensors of its own)."""
+        out [n][Hq][128], lse [n][Hq] fp32 (ttkv_shared_attn; kept for the next call on the same stream, like those of decode(); a call
+        that is captured into a graph has tensors of its own).  Calls on several streams may overlap."""
         q_fmt = _Q_FMT[q.dtype]
         n = q.shape[0]
         assert q.is_contiguous() and q.shape == (n, self.Hq, 128) and _on(q, self.device)
@@ -424,20 +424,22 @@ class TieredCache:
             ws = self._shared_workspace(n)
             B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, out, lse, ws, ws.numel(), self._compute())
             return out, lse
-        if self.shared_out is None or self.shared_out.shape[0] != n:
-            self.shared_out, self.shared_lse = self._shared_results(n)
-        if self.shared_ws is None:
-            self.shared_ws = self._shared_workspace(n)
+        # Every stream has its own, so that calls on two of them may overlap, and what a larger call replaces belongs to the
+        # stream that used it: its memory is handed out again behind that stream's work only.
+        stream = self._compute()
+        kept = self._shared.get(stream)
+        if kept is None or kept[1].shape[0] != n:
+            kept = self._shared[stream] = (kept[0] if kept else self._shared_workspace(n), *self._shared_results(n))
+        ws, out, lse = kept
         try:
-            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
-                               self._compute())
+            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, out, lse, ws, ws.numel(), stream)
         except B.TTKVError as e:
             if e.status != B.ERR_WORKSPACE:
                 raise
-            self.shared_ws = self._shared_workspace(n)   # more sequences or parts than any call before: nothing was enqueued
-            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, self.shared_out, self.shared_lse, self.shared_ws, self.shared_ws.numel(),
-                               self._compute())
-        return self.shared_out, self.shared_lse
+            ws = self._shared_workspace(n)   # more sequences or parts than any call before: nothing was enqueued
+            self._shared[stream] = ws, out, lse
+            B.ttkv_shared_attn(self.h, self.c, q, q_fmt, n, out, lse, ws, ws.numel(), stream)
+        return out, lse
 
     def _shared_results(self, n):
         return (torch.empty(n, self.Hq, 128, dtype=torch.float32, device=self.device),

@@ -310,6 +310,8 @@ class TieredCache:
             parts = max(parts + 16, int(parts * 1.25), self._few_parts)
             need = B.ttkv_workspace_bytes(self.c, parts, self.n_slots)
             assert need > 0
+            if self.ws is not None:       # it may come from another stream than the one whose work still uses it
+                self.ws.record_stream(torch.cuda.current_stream(self.device))
             self.ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             self.ws_parts, self.ws_slots = parts, self.n_slots
         return self.ws

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from test_gpu_rotary import DEV, rnd
-from test_gpu_shared_prefix import check, make_prefix, reference
+from test_gpu_shared_prefix import check, make_prefix, reference, window
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,23 @@ def test_results_stay_until_the_stream_s_next_call():
     assert c.attend_shared(q)[0].data_ptr() == out.data_ptr()              # the buffers of the call before
     assert torch.equal(out, kept[0])
     c.close()
+
+
+def test_a_workspace_that_another_stream_still_uses_is_not_handed_out():
+    """A cache's step grows its workspace on a stream that did not allocate it: the old one stays out of use until that stream is through."""
+    p, _, _ = make_prefix(8, 2, "f16", 700)
+    c, _ = window(2, 8, 2, "f16", [10, 300], p)
+    q = rnd(1, 2, 8, 128, dtype="f16")
+    c.decode(q)                                                             # allocated here
+    torch.cuda.synchronize()
+    old, size = c.ws.data_ptr(), c.ws.numel()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                                      # some 50 ms
+        c.decode(q)
+        c._workspace(4 * c.ws_parts)
+    fresh = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(3)]
+    assert not side.query()
+    assert all(x.data_ptr() != old for x in fresh)
+    torch.cuda.synchronize()
+    c.close(), p.close()

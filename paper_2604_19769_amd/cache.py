@@ -523,11 +523,16 @@ class TieredCache:
 
     def step_rotated(self, rotary, q, k, v, first_pos=None, positions=None, overlap=True):
         """One decode step from the projections: norm and rotation -> append -> attend (the prefix too) -> evict.  q [B][1][Hq][128],
-        k, v [B][1][Hkv][128] and the positions as in append_rotated."""
-        until = self._until_evict
+        k, v [B][1][Hkv][128] and the positions as in append_rotated.  A step that is refused leaves the cache as it was."""
+        assert q.shape == (self.B, 1, self.Hq, 128) and k.shape == v.shape == (self.B, 1, self.Hkv, 128), "one token of every sequence"
+        until, held = self._until_evict, self.len[0].copy()
         rotated = self.append_rotated(rotary, k, v, q=q, first_pos=first_pos, positions=positions)
         self._until_evict = until         # one token per sequence: nothing jumped
-        out, lse = self.decode(rotated.view(self.B, self.Hq, 128), None, overlap)
+        try:
+            out, lse = self.decode(rotated.view(self.B, self.Hq, 128), None, overlap)
+        except Exception:
+            self.len[0][:] = held         # refused: nor is the token held (its row lies behind the live ones)
+            raise
         self._evict_if_due(overlap)
         return out, lse
 

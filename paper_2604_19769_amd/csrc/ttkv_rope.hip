@@ -141,7 +141,8 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
 #pragma clang fp contract(off)
     const int64_t pos = a.positions ? a.positions[(int64_t)j * a.pos_stride + token] : a.first_pos[j] + token;
     const double x = (double)pos, turns = x * a.turns[lane];
-    const float r = (float)((turns - __builtin_rint(turns)) + (__builtin_fma(x, a.turns[lane], -turns) + x * a.turns_rest[lane]));
+    const double t = (turns - __builtin_rint(turns)) + (__builtin_fma(x, a.turns[lane], -turns) + x * a.turns_rest[lane]);
+    const float r = (float)(t - __builtin_rint(t));   // (beyond 2^53 turns the product's rounding is whole turns itself)
     float s, c;
     sincospif(2.0f * r, &s, &c);
     s_turn[wave][lane] = f2{c * a.magnitude, s * a.magnitude};

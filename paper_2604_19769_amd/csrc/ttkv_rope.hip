@@ -178,10 +178,23 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
     expand<SRC>(t.w1, y);
     if (t.side < 2) {
       if (s.norm) {
-        float sq = 0.0f;
+        auto mean_square = [&]() __attribute__((always_inline)) {
+          float sq = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
-        const float inv = 1.0f / sqrtf(sum_of_eight_lanes(sq) * (1.0f / 128.0f) + a.eps);
+          for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], fmaf(y[i], y[i], sq));
+          return sum_of_eight_lanes(sq) * (1.0f / 128.0f);
+        };
+        float ms = mean_square() + a.eps;
+        if (!(ms >= 0x1p-100f && ms <= 0x1p120f)) {   // squares outside fp32's range, or near its end: of the row times a power of two
+          const float by = ms < 1.0f ? 0x1p100f : 0x1p-70f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] *= by;
+            y[i] *= by;
+          }
+          ms = mean_square() + a.eps * by * by;
+        }
+        const float inv = 1.0f / sqrtf(ms);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           x[i] *= inv;

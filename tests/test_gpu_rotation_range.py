@@ -1,5 +1,5 @@
-"""Rotation at the ends of its range (ttkv_norm_rope): every position up to 2^53 with every frequency below 1e6.  Tolerances:
-those of test_gpu_rotary.py."""
+"""Rotation and norm at the ends of their ranges (ttkv_norm_rope): every position up to 2^53 with every frequency below 1e6, and rows
+whose squares leave fp32's range.  Tolerances: those of test_gpu_rotary.py."""
 from fractions import Fraction
 
 import numpy as np
@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paper_2604_19769_amd.cache import Rotary
-from test_gpu_rotary import DEV, check, rnd
+from test_gpu_rotary import DEV, DT, check, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -38,4 +38,31 @@ def test_far_positions_of_all_frequencies(freq, dtype):
     r = Rotary(freq)
     y, _ = r.apply(x, positions=torch.from_numpy(pos)[None].to(DEV))
     check(y, rotated(x, pos, freq), f"{freq[0]}")
+    r.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6])
+@pytest.mark.parametrize("by", [3e37, 1e25, 1e19, 1.0, 1e-7, 1e-19, 1e-22, 1e-35])
+def test_norm_of_rows_of_all_sizes(dtype, eps, by):
+    """The mean of the squares leaves fp32's range long before the row does."""
+    if dtype == "f16" and not 1e-7 <= by <= 1.0:
+        pytest.skip("not in fp16's range")
+    x = rnd(2, 1, 6, 9, 128).clamp(-4, 4)
+    x[0, 0, 0, 1:] = 0.0                                       # one channel alone
+    x[0, 1, :, 64:] *= 1e-12                                   # large and small ones of a row
+    x = (x * by).to(DT[dtype])
+    x[0, 2, 3] = 0.0
+    wq = rnd(3, 128).abs() + 0.5
+    r = Rotary(Rotary.frequencies(0), norm=True, q_weight=wq, eps=eps)
+    y, _ = r.apply(x, dtype=torch.float32)
+    z = x.double()
+    want = z / torch.sqrt((z * z).mean(-1, keepdim=True) + float(np.float32(eps))) * wq.double()
+    if eps == 0.0:                                             # 0 / 0
+        assert bool(y[0, 2, 3].isnan().all())
+        y[0, 2, 3] = want[0, 2, 3] = 0.0
+    err = (y.double() - want).abs()
+    # the bound of test_gpu_rotary.py for a channel that does not turn; a result (or a factor of it) below 2^-126 is a multiple of 2^-149
+    size = want.abs()
+    assert bool((err <= (2.0 ** -24 + 2.0 ** -19) * size + 2.0 ** -148 * wq.double().amax()).all()), float((err / size.clamp_min(1e-300)).max())
     r.close()

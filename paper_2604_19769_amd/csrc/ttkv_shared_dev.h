@@ -79,13 +79,14 @@ __device__ __forceinline__ Rows begin_rows(const SharedArgs &a, int row, int hkv
   const u32x4 *qp = (const u32x4 *)((const uint16_t *)a.q + ((int64_t)r.seq * a.Hq + r.hq) * 128);
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) qf[kb] = qp[2 * kb + hh];
-  if (!BF && a.q_fmt == TTKV_BF16) {   // bf16 -> fp16 (exact inside the fp16 normal range, clamped outside)
+  if (!BF && a.q_fmt == TTKV_BF16) {   // bf16 -> fp16 (exact inside the fp16 normal range, clamped outside; what is no number stays none)
+    auto clamped = [](float x) { return x != x ? x : fminf(fmaxf(x, -65504.0f), 65504.0f); };
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const f2 v = unpack2<true>(qf[kb][i]);
-        qf[kb][i] = pack2<false>(fminf(fmaxf(v.x, -65504.0f), 65504.0f), fminf(fmaxf(v.y, -65504.0f), 65504.0f));
+        qf[kb][i] = pack2<false>(clamped(v.x), clamped(v.y));
       }
   }
   r.cs = a.scale * kLog2e;

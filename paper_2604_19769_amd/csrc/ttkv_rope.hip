@@ -16,8 +16,8 @@
 // what is left after the whole turns is right at any position (one 64-bit product alone would be 1e-4 off at 2^40); everything else is
 // fp32, rounded once to the destination's type.
 //
-// Bound: memory.  2 x 4096 tokens of 32 / 8 bf16 heads (168 MB) 33.9 us, 5.0 TB/s of read + write; seven prompts of up to 4999 tokens into fp16
-// pages (600 MB) 112 us, 5.4; 3 x 1021 tokens of 28 / 4 fp32 heads (100 MB) 18.1 us, 5.5 (with pieces of eight channels 23.2); a copy of 2 GiB reaches
+// Bound: memory.  2 x 4096 tokens of 32 / 8 bf16 heads (168 MB) 34.4 us, 4.9 TB/s of read + write; seven prompts of up to 4999 tokens into fp16
+// pages (600 MB) 112 us, 5.4; 3 x 1021 tokens of 28 / 4 fp32 heads (100 MB) 18.0 us, 5.6 (with pieces of eight channels 23.2); a copy of 2 GiB reaches
 // 4.9.  A single token 3.6 us, a launch.
 #include "ttkv_internal.h"
 
@@ -185,7 +185,9 @@ __global__ __launch_bounds__(256) void rope_kernel(const RopeArgs a) {
           return sum_of_eight_lanes(sq) * (1.0f / 128.0f);
         };
         float ms = mean_square() + a.eps;
-        if (!(ms >= 0x1p-100f && ms <= 0x1p120f)) {   // squares outside fp32's range, or near its end: of the row times a power of two
+        // squares outside fp32's range, or near its end: those of the row times a power of two (the check takes 1.5 % of 8192 tokens of 32 / 8
+        // bf16 heads, nothing of fp32 rows; fp16 ones stay inside)
+        if (SRC != TTKV_F16 && __builtin_expect(!(ms >= 0x1p-100f && ms <= 0x1p120f), 0)) {
           const float by = ms < 1.0f ? 0x1p100f : 0x1p-70f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {

@@ -381,12 +381,13 @@ ttkv_status ttkv_rope_append(ttkv_handle h, ttkv_cache *c, int32_t tier, int32_t
  *        n_seq x n_q_heads < 2^22 (UNSUPPORTED beyond)
  *   out  [device] [n_seq][n_q_heads][128] fp32;  lse [device] [n_seq][n_q_heads] fp32 or NULL; an empty prefix gives 0 and -inf
  *   workspace [device], ttkv_shared_workspace_bytes: the partials of the prefix's parts.
+ * A row that meets a score that is no number gives 0 and -inf; an infinite value gives NaN in its channel.
  * out and lse of several such calls, or of one and an attention over the sequences' own tokens, are joined by
  * ttkv_merge_partials with m = lse, l = 1, acc = out. */
 #define TTKV_MAX_SHARED_SEQS 65536
 ttkv_status ttkv_shared_attn(ttkv_handle h, const ttkv_cache *prefix, const void *q, int32_t q_fmt, int32_t n_seq, float *out,
                              float *lse, void *workspace, size_t ws_bytes, void *stream);
-size_t ttkv_shared_workspace_bytes(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);   /* 0: invalid, or nothing needed */
+size_t ttkv_shared_workspace_bytes(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);   /* 0: invalid */
 /* Parts per row that a prefix adds for n_seq sequences that take part, or -1: a workspace of ttkv_decode_step_shared holds
  * ttkv_count_parts (of the own cache) + ttkv_prefix_parts parts (ttkv_workspace_bytes). */
 int32_t ttkv_prefix_parts(ttkv_handle h, const ttkv_cache *prefix, int32_t n_seq);

@@ -275,7 +275,8 @@ class TieredCache:
         """Keys normed and rotated on their way into an fp16 / bf16 tier, values beside them, the queries normed and rotated in the
         same launch (ttkv_rope_append).  k, v [B][T][Hkv][128], q [B][T][Hq][128], any strides but the last, f16 / bf16 / f32;
         seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
-        Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given)."""
+        Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given; rows behind a
+        sequence's count are not written, a new tensor's hold anything)."""
         n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
         assert rotary.device == self.device or _on(rotary, self.device)
         dev = self.device

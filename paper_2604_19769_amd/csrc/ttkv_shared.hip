@@ -31,7 +31,7 @@ using namespace dev;
 using namespace shared;
 
 // ---------------------------------------------------------------- up to 64 rows per KV head
-// Bound: memory.  24 sequences x 8229 bf16 tokens, 32 / 32 heads (135 MB): 26.6 us, 5.1 TB/s; 5 x 131072, 28 / 4 (268 MB): 45-55 us
+// Bound: memory.  24 sequences x 8229 bf16 tokens, 32 / 32 heads (135 MB): 27.0 us, 5.0 TB/s; 5 x 131072, 28 / 4 (268 MB): 45-55 us
 // as the clock allows, 4.9-6.0.  With everything but the copies taken out the first takes 24.5 (a load-only kernel 6.5-7.0 TB/s).  Four teams of two waves, 32 rows each, take the item's steps of
 // 32 tokens in turn (with a run of its own for each team, 2048 tokens of 256 items, the streams a power of two apart took 59.7 us instead
 // of 49.8).  A team loads its steps' rows itself; K of one step and V of the step before are always on their way, and leave their
@@ -123,9 +123,9 @@ __global__ __launch_bounds__(512, 1) void shared_kernel(const SharedArgs a) {
 }
 
 // ---------------------------------------------------------------- more rows: 128 per workgroup
-// Bound: the matrix cores, and what they may draw: 256 rows x 32K fp16 tokens of 8 KV heads 65-77 us (52 more for every 32K tokens beyond),
+// Bound: the matrix cores, and what they may draw: 256 rows x 32K fp16 tokens of 8 KV heads 67-79 us (52 more for every 32K tokens beyond),
 // where the core clock falls from 2.4 to 1.55 GHz within the launch; 660 TFLOP/s of products that count once and 990 with the
-// remainders' against the 1170-1230 of a large library product.  Without loads 42, without the softmax 45 of the 52: each part's
+// remainders' against the 1170-1230 of a large library product (matrix cores busy in 40 % of the kernel's cycles, the vector unit in 37).  Without loads 42, without the softmax 45 of the 52: each part's
 // share of the power.  64 rows per wave (half the LDS reads, accumulators in the AGPRs) came out alike, 53.  The steps of 32 tokens overlap inside a wave: while the softmax of step s runs on the vector unit, the
 // matrix cores work on the values of step s - 1 and the scores of step s + 1, none of which depends on it.  LDS holds two
 // steps' keys and values each (s + 1 and s + 2; s - 1 and s), one barrier per step.  Two halves of the item's tokens per workgroup meet

@@ -6,7 +6,8 @@
 // with one product chain per group for the scores, and for the values one right operand per group, p s as three bf16 numbers (24 bits of
 // any size).  The two sums of O cancel (16 codes of one sign against their zero point), so they meet in every step of 32 tokens: the step's sum of
 // p z, three bf16 numbers too, is a product with ones between the step's two.  Apart until the end, their error grew with
-// the tokens (of the result, 512 / 2048 / 8192 tokens per wave: 2.3e-5 / 1.1e-4 / 4e-4, now 1.6e-6 / 1.9e-6 / 3.5e-6) for 1-5 % less time.  Bound: the vector unit (codes into operands, 16 weights per group) beside memory: with the merge, us, fp16 / int8 / int4 / K int8 V int4:
+// the tokens (of the result, 512 / 2048 / 8192 tokens per wave: 2.3e-5 / 1.1e-4 / 4e-4, now 1.6e-6 / 1.9e-6 / 3.5e-6) for 1-5 % less time.
+// Bound: the vector unit (codes into operands, 16 weights per group), busy in 67-75 % of the kernel's cycles, beside memory: with the merge, us, fp16 / int8 / int4 / K int8 V int4:
 // 4 x 131072 tokens, 28 / 4 heads 49 / 47 / 40 / 41; 24 x 8229, 32 / 32 heads 30 / 28 / 24 / 25; 64 x 16384, 32 / 8 heads (eight blocks of 32 rows, each
 // over the codes for itself) 41 / 68 / 60 / 63.  Codes converted by instructions for it instead of written into mantissas: 8-10 % more.
 #include "ttkv_shared_dev.h"

@@ -53,3 +53,22 @@ def test_values_near_the_largest_of_bf16(n_seq, Hq, Hkv, top):
     some = [0, n_seq - 1]
     check(out[some], lse[some], [reference(q[i], [(k, v)], c.c.softmax_scale) for i in some])
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n_seq,Hq,Hkv", [(3, 8, 8), (300, 8, 8), (64, 32, 8)])
+@pytest.mark.parametrize("n", [1500, 8000])
+def test_scores_that_grow_along_the_prefix(dtype, n_seq, Hq, Hkv, n):
+    """References that move every few steps, by up to 30 powers of two in all: outputs, sums and weights on their way are scaled together.  (A score's sum of up
+    to 240 is rounded eight times to 2^-17 at most, 2^-17 sqrt(8 / 12) scale = 5e-7 of a weight on average: the usual bounds hold.)"""
+    c, _, _ = make_prefix(Hq, Hkv, dtype, 0, bt=64, extra=-(-n // 64) + 1, paged=4)
+    k, v = rnd(1, Hkv, n, 128) * 0.3, rnd(2, Hkv, n, 128, dtype=dtype)
+    k[:, :, 5] = 60.0 * torch.arange(n, device=DEV) / n
+    k = k.to(DT[dtype])
+    c.append(0, k, v, seq=0)
+    q = rnd(7, n_seq, Hq, 128, dtype=dtype)
+    q[:, :, 5] = 4.0
+    out, lse = c.attend_shared(q)
+    some = [0, n_seq // 2, n_seq - 1]
+    check(out[some], lse[some], [reference(q[i], [(k, v)], c.c.softmax_scale) for i in some])
+    c.close()

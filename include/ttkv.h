@@ -401,6 +401,58 @@ ttkv_status ttkv_decode_step_shared(ttkv_handle h, ttkv_cache *c, const ttkv_cac
                                     int32_t q_fmt, const void *k_new, const void *v_new, int32_t new_fmt, float *out, float *lse,
                                     void *workspace, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------- a chunk of new tokens */
+
+/* Attention of a chunk's queries (a prompt, a part of one, a few drafted tokens) over the cache that already holds the chunk's own
+ * keys and values (ttkv_rope_append, ttkv_quantize_append): sequence b's n_each[b] queries are those of its newest tokens, and each
+ * attends every token up to its own, tiers from the oldest to the newest (Alg. 1's Attn for many queries at once, causal by position).
+ *   seq, n_tokens, n_each as in ttkv_rope_append; n_tokens up to TTKV_MAX_CHUNK_TOKENS, fewer than 2^28 (query, head) rows in all
+ *           (UNSUPPORTED beyond).  A query in front of the oldest token held sees nothing: its row is 0, its lse -inf.
+ *   prefix  a cache of batch 1 that the sequences with a non-zero entry in member [host] [batch] (NULL: all) attend in front of their own
+ *           tokens, or NULL; conditions as in ttkv_decode_step_shared.
+ *   Tiers   in device memory, fp16 or bf16 (not both in one call) and row-wise quantized (K / V int8 / int8, int4 / int4 or int8 / int4); keys
+ *           grouped over tokens, values stored channel-major and host tiers: UNSUPPORTED.  Beside fp16 queries or tiers decompressed
+ *           values end at 131008.
+ *   q       [entry][token][n_q_heads][128], F16 or BF16 (a BF16 tier needs BF16; otherwise |q| below 65504);
+ *   out     the same shape, F16 or BF16: rounded once from fp32.  Softmax weights meet the values rounded to the product's type (fp16; bf16
+ *           over bf16 tiers, or for bf16 queries where all tiers are quantized), their sums and maxima are fp32.
+ *   lse     [device] fp32 [entry][n_tokens][n_q_heads] or NULL.  Rows of out and lse behind a sequence's count stay as they were.
+ *   workspace [device], ttkv_chunk_workspace_bytes (0: invalid arguments): partials, where few rows are cut along the tokens.
+ * A score that is no number makes a NaN of its row; an infinite value makes a NaN of its channel, in the rows that see it. */
+#define TTKV_MAX_CHUNK_TOKENS (1 << 22)
+ttkv_status ttkv_chunk_attn(ttkv_handle h, const ttkv_cache *c, int32_t seq, const ttkv_cache *prefix, const int32_t *member,
+                            const ttkv_heads *q, const ttkv_heads *out, float *lse, int64_t n_tokens, const int64_t *n_each,
+                            void *workspace, size_t ws_bytes, void *stream);
+size_t ttkv_chunk_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t seq, const ttkv_cache *prefix, const int32_t *member,
+                                  int64_t n_tokens, const int64_t *n_each);
+
+/* ---------------------------------------------------------------- weights of tokens, and the eviction of the lightest */
+
+/* What queries give every token of a tier: weights[token] += sum over the chunk's queries that see it, and over the query heads of the KV
+ * head, of e^(softmax_scale q.k - lse) ("role importance ... high attention scores", Sec. 4.1).  lse: of the whole attention (all tiers,
+ * prefix, the step's token), [device] fp32 [entry][n_tokens][n_q_heads], as ttkv_chunk_attn or (n_tokens 1) a decode step stores it; rows
+ * whose lse is not finite give nothing.
+ *   q, seq, n_tokens, n_each as in ttkv_chunk_attn: queries of the newest tokens (those of the step just made: n_tokens 1).
+ *   n_fresh [host] per entry: so many of the sequence's newest tokens begin at 0, whatever their places hold (NULL: the chunk's own).
+ *   weights [device] fp32 [pool_blocks][n_kv_heads][block_tokens], beside the tier's records.
+ * Tiers in device memory whose keys are fp16, bf16, int8 or int4 (UNSUPPORTED otherwise).  The order of each sum is fixed. */
+ttkv_status ttkv_add_weights(ttkv_handle h, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse,
+                             int64_t n_tokens, const int64_t *n_each, const int64_t *n_fresh, float *weights, void *stream);
+
+/* Eviction by weight: a tier's oldest blocks are freed, as many as leave each sequence at least `keep` tokens (whole blocks: fewer
+ * than block_tokens more), and per KV head the lightest tokens go.  The `recent` <= keep newest tokens stay whatever their weights (the others'
+ * have to be there); of equal weights the newer token goes first, what is no number counts as the least.  The i-th token of the freed
+ * blocks that stays takes the place of the i-th token behind them that goes, and its weight goes with it: tokens no longer lie in
+ * the order of their positions, which attention over position-encoded keys does not see (chunks: keep recent >= the tokens whose
+ * chunk is still to be attended).
+ *   swap 0: the freed blocks leave the tier (start[], len[]).  swap != 0: rows change places and nothing leaves: the tier's oldest blocks
+ *   then hold the lightest tokens, which ttkv_tier_demote / ttkv_evict take into the next tier.
+ *   workspace [device], ttkv_evict_light_workspace_bytes (0: invalid arguments).
+ * Device tiers of formats stored by rows (fp16, bf16, int8, int4) without mean keys; UNSUPPORTED otherwise. */
+ttkv_status ttkv_evict_light(ttkv_handle h, ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent, int32_t swap, float *weights,
+                             void *workspace, size_t ws_bytes, void *stream);
+size_t ttkv_evict_light_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent);
+
 #ifdef __cplusplus
 }
 #endif

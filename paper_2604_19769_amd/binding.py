@@ -63,6 +63,7 @@ EXPORTS = [
     "ttkv_merge_partials", "ttkv_select_blocks", "ttkv_set_split", "ttkv_set_table_check",
     "ttkv_norm_rope", "ttkv_rope_append", "ttkv_shared_attn", "ttkv_shared_workspace_bytes", "ttkv_prefix_parts",
     "ttkv_decode_step_shared",
+    "ttkv_chunk_attn", "ttkv_chunk_workspace_bytes", "ttkv_add_weights", "ttkv_evict_light", "ttkv_evict_light_workspace_bytes",
 ]
 # include/ttkv_bench.h: measurement and inspection aids, not part of the boundary
 BENCH_EXPORTS = ["ttkv_time_attn", "ttkv_time_attn_repeat", "ttkv_read_attn_timing", "ttkv_stream_read", "ttkv_staged_schedule"]
@@ -131,6 +132,13 @@ def lib():
         L.ttkv_shared_workspace_bytes.restype = sz
         L.ttkv_prefix_parts.argtypes = [p, cp, i32]
         L.ttkv_decode_step_shared.argtypes = [p, cp, cp, p, p, i32, p, p, i32, p, p, p, sz, p]
+        L.ttkv_chunk_attn.argtypes = [p, cp, i32, cp, p, hp, hp, p, i64, p, p, sz, p]
+        L.ttkv_chunk_workspace_bytes.argtypes = [p, cp, i32, cp, p, i64, p]
+        L.ttkv_chunk_workspace_bytes.restype = sz
+        L.ttkv_add_weights.argtypes = [p, cp, i32, i32, hp, p, i64, p, p, p, p]
+        L.ttkv_evict_light.argtypes = [p, cp, i32, i64, i64, i32, p, p, sz, p]
+        L.ttkv_evict_light_workspace_bytes.argtypes = [p, cp, i32, i64, i64]
+        L.ttkv_evict_light_workspace_bytes.restype = sz
         L.ttkv_time_attn.argtypes = [p, i32]
         L.ttkv_time_attn_repeat.argtypes = [p, i32]
         L.ttkv_stream_read.argtypes = [p, p, sz, p, p]
@@ -140,7 +148,8 @@ def lib():
             f = getattr(L, name)
             if name not in ("ttkv_get_stats", "ttkv_reset_stats", "ttkv_status_string", "ttkv_record_bytes",
                             "ttkv_workspace_bytes", "ttkv_demote_workspace_bytes",
-                            "ttkv_append_host_workspace_bytes", "ttkv_shared_workspace_bytes", "ttkv_count_parts"):
+                            "ttkv_append_host_workspace_bytes", "ttkv_shared_workspace_bytes", "ttkv_chunk_workspace_bytes",
+                            "ttkv_evict_light_workspace_bytes", "ttkv_count_parts"):
                 f.restype = i32
         _lib = L
     return _lib
@@ -306,6 +315,29 @@ def ttkv_prefix_parts(h, prefix, n_seq):
 def ttkv_decode_step_shared(h, cache, prefix, member, q, q_fmt, k_new, v_new, new_fmt, out, lse, workspace, ws_bytes, stream):
     _check(lib().ttkv_decode_step_shared(h, C.byref(cache), C.byref(prefix), _p(member), _p(q), q_fmt, _p(k_new), _p(v_new), new_fmt,
                                          _p(out), _p(lse), _p(workspace), ws_bytes, _p(stream)), "ttkv_decode_step_shared")
+
+
+def ttkv_chunk_attn(h, cache, seq, prefix, member, q, out, lse, n_tokens, n_each, workspace, ws_bytes, stream):
+    _check(lib().ttkv_chunk_attn(h, C.byref(cache), seq, _ref(prefix), _p(member), _ref(q), _ref(out), _p(lse), n_tokens, _p(n_each),
+                                 _p(workspace), ws_bytes, _p(stream)), "ttkv_chunk_attn")
+
+
+def ttkv_chunk_workspace_bytes(h, cache, seq, prefix, member, n_tokens, n_each):
+    return lib().ttkv_chunk_workspace_bytes(h, C.byref(cache), seq, _ref(prefix), _p(member), n_tokens, _p(n_each))
+
+
+def ttkv_add_weights(h, cache, tier, seq, q, lse, n_tokens, n_each, n_fresh, weights, stream):
+    _check(lib().ttkv_add_weights(h, C.byref(cache), tier, seq, _ref(q), _p(lse), n_tokens, _p(n_each), _p(n_fresh), _p(weights), _p(stream)),
+           "ttkv_add_weights")
+
+
+def ttkv_evict_light(h, cache, tier, keep, recent, swap, weights, workspace, ws_bytes, stream):
+    _check(lib().ttkv_evict_light(h, C.byref(cache), tier, keep, recent, int(swap), _p(weights), _p(workspace), ws_bytes, _p(stream)),
+           "ttkv_evict_light")
+
+
+def ttkv_evict_light_workspace_bytes(h, cache, tier, keep, recent):
+    return lib().ttkv_evict_light_workspace_bytes(h, C.byref(cache), tier, keep, recent)
 
 
 def ttkv_time_attn(h, max_samples):

@@ -22,6 +22,7 @@ class TierConfig:
     mem: str = "device"        # 'device' | 'host'
     paged_seed: int = None     # not None: shuffled block table over a shared pool (paged KV)
     summary: bool = False      # keep mean-key summaries (block identification)
+    weights: bool = False      # keep what attention has given each token (add_weights, evict_light)
 
 
 _Q_FMT = {torch.float16: B.F16, torch.bfloat16: B.BF16}
@@ -163,6 +164,9 @@ class TieredCache:
         c.softmax_scale = float(softmax_scale) if softmax_scale is not None else 1.0 / float(np.sqrt(128.0))
         self._keep = []          # tensors / arrays the descriptor points into
         self.start, self.len, self.pool, self.table = [], [], [], []
+        self.weights = []                 # per tier None, or fp32 [record][KV head][block token] beside the tier's records
+        self._weighed = [np.zeros(batch, np.int64) for _ in self.cfg]   # lifetime ordinal behind the newest token weighed
+        self.evicted = np.zeros(batch, np.int64)   # tokens of each sequence that evict_light dropped (they still count as positions)
         for t, cfg in enumerate(self.cfg):
             T = c.tier[t]
             T.k_fmt, T.v_fmt = B.FMT_NAMES[cfg.k_fmt], B.FMT_NAMES[cfg.v_fmt]
@@ -193,6 +197,8 @@ class TieredCache:
                 T.k_sum, T.k_summary = ksum.data_ptr(), kmu.data_ptr()
                 self._keep += [ksum, kmu]
                 self.ksum, self.kmu = ksum, kmu
+            self.weights.append(torch.zeros(T.pool_blocks, n_kv_heads, cfg.block_tokens, dtype=torch.float32, device=self.device)
+                                if cfg.weights else None)
             self.start.append(start)
             self.len.append(ln)
             self.pool.append(pool)
@@ -212,6 +218,7 @@ class TieredCache:
         self.out = torch.empty(batch, n_q_heads, 128, dtype=torch.float32, device=self.device)
         self.lse = torch.empty(batch, n_q_heads, dtype=torch.float32, device=self.device)
         self._shared = {}                 # stream -> workspace, out and lse of attend_shared
+        self._streams_ws = {}             # (use, stream) -> workspace
         self.prefix = self.members = None
         if prefix is not None:
             self.share(prefix, members)
@@ -275,7 +282,7 @@ class TieredCache:
         """Keys normed and rotated on their way into an fp16 / bf16 tier, values beside them, the queries normed and rotated in the
         same launch (ttkv_rope_append).  k, v [B][T][Hkv][128], q [B][T][Hq][128], any strides but the last, f16 / bf16 / f32;
         seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
-        Rotary.apply; neither given: behind the tokens held (prefix included).  Returns q_out (a new tensor unless given; rows behind a
+        Rotary.apply; neither given: behind the tokens held (prefix included) and those that evict_light dropped.  Returns q_out (a new tensor unless given; rows behind a
         sequence's count are not written, a new tensor's hold anything)."""
         n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
         assert rotary.device == self.device or _on(rotary, self.device)
@@ -287,8 +294,10 @@ class TieredCache:
                                          memory_format=torch.contiguous_format)
             shape = (n, T, self.Hq, 128)
             qv, qo = _heads(q, shape, dev), _heads(q_out, shape, dev)
-        if first_pos is None and positions is None and self.prefix is not None:
-            first_pos = sum(self.len) + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
+        if first_pos is None and positions is None and (self.prefix is not None or self.evicted.any()):
+            first_pos = sum(self.len) + self.evicted
+            if self.prefix is not None:
+                first_pos = first_pos + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
         shape = (n, T, self.Hkv, 128)
         B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, shape, dev), _heads(v, shape, dev), T, _host_int64(counts, n),
@@ -451,6 +460,94 @@ class TieredCache:
     def _shared_workspace(self, n):
         need = B.ttkv_shared_workspace_bytes(self.h, self.c, n)
         return torch.empty(max(256, need), dtype=torch.uint8, device=self.device)
+
+    # ------------------------------------------------------------------ chunks of new tokens
+    def _with_workspace(self, use, call, need):
+        """call(workspace, bytes) with the workspace that `use` has on the current stream, a larger one where the library asks for it
+        (nothing was enqueued then).  What a larger one replaces is handed out again behind that stream's work only; a call
+        that is captured into a graph has one of its own."""
+        if torch.cuda.is_current_stream_capturing():
+            ws = torch.empty(need(), dtype=torch.uint8, device=self.device)
+            return call(ws, ws.numel())
+        key = use, self._compute()
+        ws = self._streams_ws.get(key)
+        try:
+            return call(ws, 0 if ws is None else ws.numel())
+        except B.TTKVError as e:
+            if e.status != B.ERR_WORKSPACE:
+                raise
+        ws = self._streams_ws[key] = torch.empty(need() * 5 // 4, dtype=torch.uint8, device=self.device)
+        return call(ws, ws.numel())
+
+    @_on_own_device
+    def attend_chunk(self, q, counts=None, out=None, lse=None, seq=-1, dtype=None):
+        """Attention of the newest tokens' queries, q [B][T][Hq][128] f16 / bf16 (any strides but the last), over every tier, and the prefix
+        of a cache that has one; the tokens themselves are in the cache already (append, append_rotated).  Causal: each query sees the tokens up to its own.
+        counts: new tokens of each sequence (host integers; None: T); seq >= 0: one sequence's, B = 1.  Returns out (a new tensor of
+        `dtype`, None: q's, f16 or bf16, unless given) and lse [B][T][Hq] fp32 (a new tensor unless given, contiguous); rows
+        behind a sequence's count are not written (ttkv_chunk_attn)."""
+        n, T = (self.B if seq < 0 else 1), q.shape[1]
+        shape = (n, T, self.Hq, 128)
+        if out is None:
+            out = torch.empty_like(q, dtype=dtype, memory_format=torch.contiguous_format)
+        if lse is None:
+            lse = torch.empty(shape[:3], dtype=torch.float32, device=self.device)
+        assert lse.shape == shape[:3] and lse.is_contiguous() and lse.dtype == torch.float32 and _on(lse, self.device)
+        assert self.prefix is None or self.prefix.prefix is None, "a prefix is attended without its own"
+        qv, ov, each = _heads(q, shape, self.device), _heads(out, shape, self.device), _host_int64(counts, n)
+        prefix = None if self.prefix is None else self.prefix.c
+        members = None if self.members is None else self.members.ctypes.data
+        stream = self._compute()
+        self._with_workspace("chunk", lambda ws, size: B.ttkv_chunk_attn(self.h, self.c, seq, prefix, members, qv, ov, lse, T, each, ws, size, stream),
+                             lambda: B.ttkv_chunk_workspace_bytes(self.h, self.c, seq, prefix, members, T, each))
+        return out, lse
+
+    def prefill(self, rotary, q, k, v, counts=None, first_pos=None, positions=None, seq=-1, dtype=None, overlap=True):
+        """A chunk of new tokens from the projections: norm and rotation -> append -> attend -> evict.  q [B][T][Hq][128], k, v
+        [B][T][Hkv][128], arguments as in append_rotated and attend_chunk; tier 0's ring has room for what it holds and the chunk.  A chunk
+        that is refused leaves the cache as it was."""
+        held = self.len[0].copy()
+        rotated = self.append_rotated(rotary, k, v, q=q, counts=counts, first_pos=first_pos, positions=positions, seq=seq)
+        try:
+            out, lse = self.attend_chunk(rotated, counts, seq=seq, dtype=dtype)
+        except Exception:
+            self.len[0][:] = held
+            raise
+        self.demote(overlap)
+        return out, lse
+
+    # ------------------------------------------------------------------ weights of tokens
+    @_on_own_device
+    def add_weights(self, q, lse, counts=None, fresh=None, tier=0, seq=-1):
+        """Adds to self.weights[tier] what the newest tokens' queries give each token (ttkv_add_weights): q [B][T][Hq][128] (or [B][Hq][128]
+        of a decode step) and lse [B][T][Hq] ([B][Hq]) as attend_chunk or step had and returned them, before the tokens lie elsewhere
+        (evicted).  fresh: so many of each sequence's newest tokens begin at 0 (host integers; None: those appended since the last call)."""
+        assert self.weights[tier] is not None, "the tier keeps no weights"
+        n = self.B if seq < 0 else 1
+        if q.dim() == 3:
+            q = q.unsqueeze(1)
+        T = q.shape[1]
+        assert lse.numel() == n * T * self.Hq and lse.is_contiguous() and lse.dtype == torch.float32 and _on(lse, self.device)
+        rows = slice(None) if seq < 0 else slice(seq, seq + 1)
+        end = (self.start[tier] + self.len[tier])[rows]
+        if fresh is None:
+            newer = sum((x[rows] for x in self.len[:tier]), np.zeros(n, np.int64))
+            fresh = np.maximum(0, end - self._weighed[tier][rows]) + newer
+        B.ttkv_add_weights(self.h, self.c, tier, seq, _heads(q, (n, T, self.Hq, 128), self.device), lse, T, _host_int64(counts, n),
+                           _host_int64(fresh, n), self.weights[tier], self._compute())
+        self._weighed[tier][rows] = end
+
+    @_on_own_device
+    def evict_light(self, keep, recent, tier=0, swap=False):
+        """Frees the tier's oldest blocks, as many as leave every sequence at least `keep` tokens: per KV head the tokens of least weight go, the
+        `recent` newest stay (ttkv_evict_light).  swap: nothing goes; the light tokens lie in the oldest blocks afterwards, for demote()."""
+        assert self.weights[tier] is not None, "the tier keeps no weights"
+        held, stream = self.len[tier].copy(), self._compute()
+        self._with_workspace("light", lambda ws, size: B.ttkv_evict_light(self.h, self.c, tier, keep, recent, swap, self.weights[tier], ws, size, stream),
+                             lambda: B.ttkv_evict_light_workspace_bytes(self.h, self.c, tier, keep, recent))
+        self.evicted += held - self.len[tier]
+        self._parts_age = None            # lengths jump: count the parts again at the next step
+        self._until_evict = 0
 
     def select(self, q, k):
         q_fmt = _Q_FMT[q.dtype]

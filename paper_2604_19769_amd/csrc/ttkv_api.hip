@@ -1653,6 +1653,347 @@ ttkv_status ttkv_rope_append(ttkv_handle hh, ttkv_cache *c, int32_t tier, int32_
   return TTKV_OK;
 }
 
+// ---------------------------------------------------------------- a chunk of new tokens
+namespace {
+// One launch of the chunk's attention: what the cache, the prefix and the lengths decide.
+struct ChunkPlan {
+  ChunkArgs a;
+  ChunkShape shape;
+  int64_t rows;        // query rows per KV head, all sequences
+  size_t ws_bytes;     // partials
+};
+int64_t held_tokens(const ttkv_cache *c, int b) {
+  int64_t n = 0;
+  for (int t = 0; t < c->n_tiers; ++t) n += c->tier[t].len[b];
+  return n;
+}
+// The formats of a cache that chunks are attended over; fp16 and bf16 tiers do not go together.
+ttkv_status check_chunk_tiers(const ttkv_cache *c, bool &f16, bool &bf16) {
+  for (int t = 0; t < c->n_tiers; ++t) {
+    const ttkv_tier &T = c->tier[t];
+    const bool fp = is_fp(T.k_fmt) && T.k_fmt == T.v_fmt;
+    if (T.mem != TTKV_MEM_DEVICE || !(fp || shared_quant_fits(T.k_fmt, T.v_fmt))) return TTKV_ERR_UNSUPPORTED;
+    f16 |= T.k_fmt == TTKV_F16;
+    bf16 |= T.k_fmt == TTKV_BF16;
+  }
+  return f16 && bf16 ? TTKV_ERR_UNSUPPORTED : TTKV_OK;
+}
+// Checks and plans; q_fmt < 0: not known yet (it decides nothing about the sizes).  P.rows == 0: nothing to do.
+ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, const ttkv_cache *prefix, const int32_t *member, int32_t q_fmt,
+                       int64_t n_tokens, const int64_t *n_each, ChunkPlan &P) {
+  ttkv_status st = validate_cache(c, check_tables);
+  if (st != TTKV_OK) return st;
+  if (seq < -1 || seq >= c->batch || n_tokens < 0) return TTKV_ERR_INVALID_ARG;
+  bool f16 = false, bf16 = false;
+  if ((st = check_chunk_tiers(c, f16, bf16)) != TTKV_OK) return st;
+  if (prefix) {
+    if ((st = validate_cache(prefix, check_tables)) != TTKV_OK) return st;
+    if (prefix->batch != 1 || prefix->n_q_heads != c->n_q_heads || prefix->n_kv_heads != c->n_kv_heads || prefix->softmax_scale != c->softmax_scale)
+      return TTKV_ERR_INVALID_ARG;
+    if ((st = check_chunk_tiers(prefix, f16, bf16)) != TTKV_OK) return st;
+  }
+  if (bf16 && q_fmt >= 0 && q_fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
+  if (n_tokens > TTKV_MAX_CHUNK_TOKENS) return TTKV_ERR_UNSUPPORTED;
+  const int b0 = seq < 0 ? 0 : seq, n_seq = seq < 0 ? c->batch : 1;
+  ChunkArgs &a = P.a;
+  a.Hq = c->n_q_heads;
+  a.Hkv = c->n_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.scale = c->softmax_scale;
+  a.first_seq = b0;
+  a.n_tokens = (int32_t)n_tokens;
+  a.members = 0;
+  a.n_prefix = prefix ? prefix->n_tiers : 0;
+  a.n_tiers = a.n_prefix + c->n_tiers;
+  bool quantized = false;
+  int64_t lead = 0;
+  for (int i = 0; i < a.n_prefix; ++i) {   // oldest first
+    const ttkv_tier &T = prefix->tier[prefix->n_tiers - 1 - i];
+    a.tv[i] = make_view(T, make_layout(T, c->n_kv_heads));
+    a.prefix_tok[i] = (int32_t)(T.start[0] % ring_tokens(T));
+    a.prefix_len[i] = (int32_t)T.len[0];
+    quantized |= T.len[0] > 0 && !is_fp(T.k_fmt);
+    lead += T.len[0];
+  }
+  for (int i = 0; i < c->n_tiers; ++i) {
+    const ttkv_tier &T = c->tier[c->n_tiers - 1 - i];
+    a.tv[a.n_prefix + i] = make_view(T, make_layout(T, c->n_kv_heads));
+  }
+  // the sequences with new tokens, those whose rows see most first
+  struct Slot {
+    int entry, b;
+    int64_t n, sees;
+  } slot[TTKV_MAX_BATCH];
+  int n_slots = 0;
+  int64_t most_rows = 0;
+  P.rows = 0;
+  for (int j = 0; j < n_seq; ++j) {
+    const int b = b0 + j;
+    const int64_t n = n_each ? n_each[j] : n_tokens;
+    if (n < 0 || n > n_tokens) return TTKV_ERR_INVALID_ARG;
+    const bool in = prefix && (!member || member[b]);
+    if (in) a.members |= 1ull << b;
+    const int64_t total = held_tokens(c, b) + (in ? lead : 0);
+    if (total >= (1ll << 31) - (1 << 24)) return TTKV_ERR_UNSUPPORTED;   // places are counted in 32 bits
+    if (n == 0) continue;
+    for (int t = 0; t < c->n_tiers; ++t) quantized |= c->tier[t].len[b] > 0 && !is_fp(c->tier[t].k_fmt);
+    slot[n_slots++] = Slot{j, b, n, total};
+    P.rows += n * a.G;
+    most_rows = std::max(most_rows, n * a.G);
+  }
+  P.ws_bytes = 0;
+  a.n_items = 0;
+  a.part_stride = 0;
+  if (n_slots == 0) return TTKV_OK;
+  if (P.rows * a.Hkv >= 1ll << 28) return TTKV_ERR_UNSUPPORTED;   // a launch has 2^32 threads at most
+  std::sort(slot, slot + n_slots, [](const Slot &x, const Slot &y) { return x.sees != y.sees ? x.sees > y.sees : x.entry < y.entry; });
+  P.shape = chunk_shape(most_rows, bf16 || (!f16 && q_fmt == TTKV_BF16), quantized);
+  int64_t tiles[TTKV_MAX_BATCH], work = 0;
+  for (int i = 0; i < n_slots; ++i) {
+    tiles[i] = (slot[i].n * a.G + P.shape.rows - 1) / P.shape.rows;
+    work += tiles[i] * ((slot[i].sees + 31) / 32);
+  }
+  const int64_t least = chunk_least_steps(P.shape), slots = chunk_resident(P.shape);
+  // Steps per item: as many rounds of resident workgroups as lose least to the last one's length and to the items' starts.
+  auto split_at = [&](int64_t steps, int i) { return std::max<int64_t>(1, std::min<int64_t>(65535, ((slot[i].sees + 31) / 32 + steps - 1) / steps)); };
+  int64_t whole = 0;
+  for (int i = 0; i < n_slots; ++i) whole += tiles[i];
+  int64_t best_steps = (1ll << 31) / 32;
+  if (whole * a.Hkv < 4 * slots) {
+    double best = 0.0;
+    for (int k = 0; k <= 6; ++k) {   // 0: no split
+      const int64_t steps = k ? std::max(least, (work * a.Hkv + k * slots - 1) / (k * slots)) : best_steps;
+      int64_t items = 0, longest = 1;
+      for (int i = 0; i < n_slots; ++i) {
+        const int64_t n = split_at(steps, i);
+        items += tiles[i] * n;
+        longest = std::max(longest, ((slot[i].sees + 31) / 32 + n - 1) / n);
+      }
+      items *= a.Hkv;
+      const double cost = std::max((double)((items + slots - 1) / slots) * 0.75, (double)work * a.Hkv / longest / slots) * (longest + least);
+      if (k == 0 || cost < 0.95 * best) {
+        best = cost;
+        best_steps = steps;
+      }
+    }
+  }
+  int most = 1;
+  int64_t items = 0, rows = 0;
+  for (int i = 0; i < n_slots; ++i) {
+    const int n = (int)split_at(best_steps, i);
+    a.first_item[i] = (int32_t)items;
+    a.count[i] = (int32_t)slot[i].n;
+    a.row_base[i] = (int32_t)rows;
+    a.n_split[i] = n;
+    a.entry[i] = slot[i].entry;
+    for (int t = 0; t < c->n_tiers; ++t) {
+      const ttkv_tier &T = c->tier[c->n_tiers - 1 - t];
+      a.first_tok[t][i] = (int32_t)(T.start[slot[i].b] % ring_tokens(T));
+      a.len[t][i] = (int32_t)T.len[slot[i].b];
+    }
+    items += tiles[i] * n;
+    rows += slot[i].n * a.G;
+    most = std::max(most, n);
+  }
+  for (int i = n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = a.row_base[i] = INT32_MAX;
+  if (items * a.Hkv >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;
+  a.n_items = (int32_t)items;
+  a.part_stride = most > 1 ? most : 0;
+  a.hkv_magic = a.Hkv > 1 && items * a.Hkv * a.Hkv < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.Hkv - 1) / a.Hkv) : 0;
+  a.g_magic = a.G > 1 && most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
+  P.ws_bytes = (size_t)P.rows * a.Hkv * a.part_stride * 130 * sizeof(float);
+  return TTKV_OK;
+}
+}  // namespace
+
+size_t ttkv_chunk_workspace_bytes(ttkv_handle hh, const ttkv_cache *c, int32_t seq, const ttkv_cache *prefix, const int32_t *member,
+                                  int64_t n_tokens, const int64_t *n_each) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  ChunkPlan P{};
+  if (!h || plan_chunk(c, h->check_tables, seq, prefix, member, -1, n_tokens, n_each, P) != TTKV_OK) return 0;
+  return align256(P.ws_bytes) + 256;
+}
+
+ttkv_status ttkv_chunk_attn(ttkv_handle hh, const ttkv_cache *c, int32_t seq, const ttkv_cache *prefix, const int32_t *member, const ttkv_heads *q,
+                            const ttkv_heads *out, float *lse, int64_t n_tokens, const int64_t *n_each, void *workspace, size_t ws_bytes, void *stream_) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || !q || !out) return TTKV_ERR_INVALID_ARG;
+  ChunkPlan P{};
+  ttkv_status st = plan_chunk(c, h->check_tables, seq, prefix, member, q->fmt, n_tokens, n_each, P);
+  if (st != TTKV_OK) return st;
+  if ((q->fmt != TTKV_F16 && q->fmt != TTKV_BF16) || (out->fmt != TTKV_F16 && out->fmt != TTKV_BF16)) return TTKV_ERR_UNSUPPORTED;
+  ChunkArgs &a = P.a;
+  const int n_seq = seq < 0 ? c->batch : 1;
+  int64_t sq[3], so[3];
+  uint8_t *data = nullptr;
+  if ((st = read_heads(q, n_seq, n_tokens, false, sq, &data)) != TTKV_OK) return st;
+  a.q = data;
+  if ((st = read_heads(out, n_seq, n_tokens, true, so, &data)) != TTKV_OK) return st;
+  a.out = data;
+  if (q->n_heads != a.Hq || out->n_heads != a.Hq) return TTKV_ERR_INVALID_ARG;
+  if (P.rows == 0) return TTKV_OK;
+  a.q_seq = sq[0]; a.q_token = sq[1]; a.q_head = sq[2];
+  a.o_seq = so[0]; a.o_token = so[1]; a.o_head = so[2];
+  a.q_fmt = q->fmt;
+  a.out_fmt = out->fmt;
+  a.lse = lse;
+  const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
+  if (P.ws_bytes && (!workspace || ws_bytes < mis + P.ws_bytes)) return TTKV_ERR_WORKSPACE;
+  const int64_t parts = P.rows * a.Hkv * a.part_stride;
+  if (parts) {
+    a.pacc = (float *)((uint8_t *)workspace + mis);
+    a.pm = a.pacc + parts * 128;
+    a.pl = a.pm + parts;
+  }
+  hipStream_t stream = (hipStream_t)stream_;
+  TTKV_HIP(h, launch_chunk(a, P.shape, stream));
+  if (parts) TTKV_HIP(h, launch_chunk_merge(a, P.rows * a.Hkv, stream));
+  h->stats.kernels += parts ? 2 : 1;
+  return TTKV_OK;
+}
+
+// ---------------------------------------------------------------- weights and what they decide
+ttkv_status ttkv_add_weights(ttkv_handle hh, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse, int64_t n_tokens,
+                             const int64_t *n_each, const int64_t *n_fresh, float *weights, void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || !q) return TTKV_ERR_INVALID_ARG;
+  ttkv_status st = validate_cache(c, h->check_tables);
+  if (st != TTKV_OK) return st;
+  if (tier < 0 || tier >= c->n_tiers || seq < -1 || seq >= c->batch || n_tokens < 0 || !weights) return TTKV_ERR_INVALID_ARG;
+  if (n_tokens > TTKV_MAX_CHUNK_TOKENS) return TTKV_ERR_UNSUPPORTED;
+  const ttkv_tier &T = c->tier[tier];
+  if (T.mem != TTKV_MEM_DEVICE || !(is_fp(T.k_fmt) || T.k_fmt == TTKV_I8_SYM_G32 || T.k_fmt == TTKV_I4_ASYM_G64)) return TTKV_ERR_UNSUPPORTED;
+  if (q->fmt != TTKV_F16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;
+  if (T.k_fmt == TTKV_BF16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
+  const int b0 = seq < 0 ? 0 : seq, n_seq = seq < 0 ? c->batch : 1;
+  WeighArgs a{};
+  int64_t s[3];
+  uint8_t *data = nullptr;
+  if ((st = read_heads(q, n_seq, n_tokens, false, s, &data)) != TTKV_OK) return st;
+  if (q->n_heads != c->n_q_heads) return TTKV_ERR_INVALID_ARG;
+  a.q = data;
+  a.q_seq = s[0]; a.q_token = s[1]; a.q_head = s[2];
+  a.q_fmt = q->fmt;
+  a.Hq = c->n_q_heads;
+  a.Hkv = c->n_kv_heads;
+  a.G = a.Hq / a.Hkv;
+  a.scale = c->softmax_scale;
+  a.first_seq = b0;
+  a.n_tokens = (int32_t)n_tokens;
+  a.lse = lse;
+  a.weights = weights;
+  a.tv = make_view(T, make_layout(T, c->n_kv_heads));
+  int n_slots = 0;
+  int64_t items = 0, most_rows = 0, queries = 0;
+  for (int j = 0; j < n_seq; ++j) {
+    const int b = b0 + j;
+    const int64_t n = n_each ? n_each[j] : n_tokens, fresh = n_fresh ? n_fresh[j] : n;
+    if (n < 0 || n > n_tokens || fresh < 0) return TTKV_ERR_INVALID_ARG;
+    const int64_t total = held_tokens(c, b);
+    int64_t before = 0;   // tokens of older tiers
+    for (int t = tier + 1; t < c->n_tiers; ++t) before += c->tier[t].len[b];
+    queries += n;
+    if (T.len[b] == 0 || (n == 0 && (n_fresh ? fresh : 0) == 0)) continue;
+    a.first_item[n_slots] = (int32_t)items;
+    a.count[n_slots] = (int32_t)n;
+    a.sees[n_slots] = (int32_t)std::max<int64_t>(std::min<int64_t>(total - n + 1 - before, 1ll << 30), -(1ll << 30));
+    a.first_tok[n_slots] = (int32_t)(T.start[b] % ring_tokens(T));
+    a.len[n_slots] = (int32_t)T.len[b];
+    // tokens newer than the tier's own count as new, too
+    const int64_t newer = total - before - T.len[b];
+    a.first_fresh[n_slots] = (int32_t)(T.len[b] - std::min(T.len[b], std::max<int64_t>(0, fresh - newer)));
+    a.entry[n_slots] = j;
+    ++n_slots;
+    items += (T.len[b] + 255) / 256;
+    most_rows = std::max(most_rows, n * a.G);
+  }
+  if (n_slots == 0) return TTKV_OK;
+  if (queries && !lse) return TTKV_ERR_INVALID_ARG;
+  if (most_rows >= 1ll << 28 || items * a.Hkv >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;
+  for (int i = n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = INT32_MAX;
+  a.n_items = (int32_t)items;
+  a.hkv_magic = a.Hkv > 1 && items * a.Hkv * a.Hkv < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.Hkv - 1) / a.Hkv) : 0;
+  a.g_magic = a.G > 1 && most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
+  TTKV_HIP(h, launch_weigh(a, T.k_fmt == TTKV_BF16 || (T.k_fmt != TTKV_F16 && q->fmt == TTKV_BF16), (hipStream_t)stream));
+  h->stats.kernels += 1;
+  return TTKV_OK;
+}
+
+namespace {
+// Tokens that go from each sequence, and the launch that makes room for them at the front.
+ttkv_status plan_light(const ttkv_cache *c, bool check_tables, int32_t tier, int64_t keep, int64_t recent, LightArgs &a, int64_t gone[TTKV_MAX_BATCH],
+                       int32_t &most_moves, size_t &ws_bytes) {
+  ttkv_status st = validate_cache(c, check_tables);
+  if (st != TTKV_OK) return st;
+  if (tier < 0 || tier >= c->n_tiers || recent < 0 || keep < recent) return TTKV_ERR_INVALID_ARG;
+  const ttkv_tier &T = c->tier[tier];
+  auto by_row = [](int f) { return is_fp(f) || f == TTKV_I8_SYM_G32 || f == TTKV_I4_ASYM_G64; };
+  if (T.mem != TTKV_MEM_DEVICE || !by_row(T.k_fmt) || !by_row(T.v_fmt) || T.k_sum) return TTKV_ERR_UNSUPPORTED;
+  const Layout L = make_layout(T, c->n_kv_heads);
+  a.Hkv = c->n_kv_heads;
+  a.kc = L.kc; a.km = L.km; a.vc = L.vc; a.vm = L.vm;
+  a.tv = make_view(T, L);
+  a.n_slots = 0;
+  most_moves = 0;
+  int64_t moves = 0;
+  for (int b = 0; b < c->batch; ++b) {
+    gone[b] = T.len[b] > keep ? (T.len[b] - keep) / L.bt * L.bt : 0;
+    if (gone[b] == 0) continue;
+    const int i = a.n_slots++;
+    const int64_t old = T.len[b] - recent;
+    a.seq[i] = b;
+    a.first_tok[i] = (int32_t)(T.start[b] % ring_tokens(T));
+    a.old[i] = (int32_t)old;
+    a.gone[i] = (int32_t)gone[b];
+    a.most_moves[i] = (int32_t)std::min(gone[b], old - gone[b]);
+    a.move_base[i] = moves;
+    moves += (int64_t)a.most_moves[i] * a.Hkv;
+    most_moves = std::max(most_moves, a.most_moves[i]);
+  }
+  ws_bytes = align256((size_t)a.n_slots * a.Hkv * 4) + (size_t)moves * 8;
+  return TTKV_OK;
+}
+}  // namespace
+
+size_t ttkv_evict_light_workspace_bytes(ttkv_handle hh, const ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  LightArgs a{};
+  int64_t gone[TTKV_MAX_BATCH];
+  int32_t most;
+  size_t need;
+  if (!h || plan_light(c, h->check_tables, tier, keep, recent, a, gone, most, need) != TTKV_OK) return 0;
+  return align256(need) + 256;
+}
+
+ttkv_status ttkv_evict_light(ttkv_handle hh, ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent, int32_t swap, float *weights, void *workspace,
+                             size_t ws_bytes, void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h) return TTKV_ERR_INVALID_ARG;
+  LightArgs a{};
+  int64_t gone[TTKV_MAX_BATCH];
+  int32_t most;
+  size_t need;
+  const ttkv_status st = plan_light(c, h->check_tables, tier, keep, recent, a, gone, most, need);
+  if (st != TTKV_OK) return st;
+  if (!weights) return TTKV_ERR_INVALID_ARG;
+  if (a.n_slots == 0) return TTKV_OK;
+  const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
+  if (!workspace || ws_bytes < mis + need) return TTKV_ERR_WORKSPACE;
+  a.weights = weights;
+  a.swap = swap != 0;
+  a.count = (int32_t *)((uint8_t *)workspace + mis);
+  a.moves = (int32_t *)((uint8_t *)workspace + mis + align256((size_t)a.n_slots * a.Hkv * 4));
+  int nk = 0;
+  TTKV_HIP(h, launch_light(a, most, (hipStream_t)stream, &nk));
+  h->stats.kernels += nk;
+  if (!swap)
+    for (int b = 0; b < c->batch; ++b) {
+      c->tier[tier].start[b] += gone[b];
+      c->tier[tier].len[b] -= gone[b];
+    }
+  return TTKV_OK;
+}
+
 ttkv_status ttkv_merge_partials(ttkv_handle hh, const float *m, const float *l, const float *acc, int32_t n_parts,
                                 int32_t part_stride, const int32_t *n_parts_row, int32_t rows, float *out, float *lse,
                                 void *stream) {

@@ -364,6 +364,82 @@ hipError_t launch_shared(SharedArgs &a, hipStream_t s);
 bool shared_quant_fits(int k_fmt, int v_fmt);
 hipError_t launch_shared_quant(const SharedArgs &a, dim3 grid, hipStream_t s);
 
+// Attention of a chunk of new tokens over the tiers that hold them (chunk_kernel and its kin).  Tiers oldest first, those of a
+// prefix in front of the sequences' own.  Sequences lie in slots, the dearest rows first.  Strides in bytes.
+struct ChunkArgs {
+  int32_t n_items, Hq, Hkv, G;
+  uint32_t hkv_magic, g_magic;     // divisions by Hkv and G by a multiplication; 0: by a division
+  int32_t n_tiers, n_prefix;       // tiers, and how many of them are the prefix's
+  float scale;
+  int32_t q_fmt, out_fmt;
+  int32_t part_stride;             // partials per row; 0: every row tile is one item, which stores the result
+  int32_t n_tokens, first_seq;     // lse's rows per entry; sequence of entry 0
+  const uint8_t *q;
+  uint8_t *out;
+  float *lse;                      // nullable
+  float *pm, *pl, *pacc;
+  int64_t q_seq, q_token, q_head, o_seq, o_token, o_head;
+  uint64_t members;                // sequences that attend the prefix
+  TierView tv[2 * TTKV_MAX_TIERS];
+  int32_t prefix_tok[TTKV_MAX_TIERS], prefix_len[TTKV_MAX_TIERS];
+  int32_t first_item[TTKV_MAX_BATCH];   // of the slot, INT32_MAX behind the last
+  int32_t count[TTKV_MAX_BATCH];        // new tokens
+  int32_t row_base[TTKV_MAX_BATCH];     // query rows per KV head of the slots before
+  // (32 bits wide like the others: arrays of narrower numbers beside them made the compiler add an index in bytes to a scalar load's
+  // base, whose two low bits the load leaves out)
+  int32_t n_split[TTKV_MAX_BATCH];      // items per row tile
+  int32_t entry[TTKV_MAX_BATCH];
+  int32_t first_tok[TTKV_MAX_TIERS][TTKV_MAX_BATCH], len[TTKV_MAX_TIERS][TTKV_MAX_BATCH];   // ring token and length of a slot's runs
+};
+static_assert(sizeof(ChunkArgs) <= 4096, "kernel arguments are passed by value");
+// Query rows per workgroup, and the kernels that a launch takes.
+struct ChunkShape {
+  int rows;
+  bool bf, quantized;
+};
+ChunkShape chunk_shape(int64_t most_rows, bool bf, bool quantized);
+int64_t chunk_least_steps(const ChunkShape &s);   // of 32 tokens, that an item should have
+int64_t chunk_resident(const ChunkShape &s);      // workgroups on the chip at once
+hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+hipError_t launch_chunk_merge(const ChunkArgs &a, int64_t n_rows, hipStream_t stream);   // rows of all heads
+
+// What the queries of a chunk give each token of one tier (weigh_kernel).
+struct WeighArgs {
+  int32_t n_items, Hq, Hkv, G;
+  uint32_t hkv_magic, g_magic;
+  float scale;
+  int32_t q_fmt;
+  int32_t n_tokens, first_seq;     // lse's rows per entry; sequence of entry 0
+  const uint8_t *q;
+  const float *lse;
+  float *weights;
+  int64_t q_seq, q_token, q_head;  // bytes
+  TierView tv;
+  int32_t first_item[TTKV_MAX_BATCH];   // of the slot, INT32_MAX behind the last
+  int32_t count[TTKV_MAX_BATCH];
+  int32_t sees[TTKV_MAX_BATCH];         // tokens of the tier that the slot's first query sees (less than none: below 0)
+  int32_t first_tok[TTKV_MAX_BATCH], len[TTKV_MAX_BATCH];
+  int32_t first_fresh[TTKV_MAX_BATCH];  // the first token whose weight begins at 0
+  int32_t entry[TTKV_MAX_BATCH];
+};
+static_assert(sizeof(WeighArgs) <= 4096, "kernel arguments are passed by value");
+hipError_t launch_weigh(const WeighArgs &a, bool bf, hipStream_t s);
+
+// The lightest tokens of a tier leave their places to tokens of its oldest blocks (light_select_kernel, light_move_kernel).
+struct LightArgs {
+  int32_t n_slots, Hkv, swap;
+  int32_t kc, km, vc, vm;          // bytes per row
+  float *weights;
+  int32_t *count;                  // [slot][Hkv] rows that move
+  int32_t *moves;                  // [slot][Hkv] lists of most_moves pairs each (from, to), tokens of the tier; the slot's lists begin at move_base
+  TierView tv;
+  int32_t seq[TTKV_MAX_BATCH], first_tok[TTKV_MAX_BATCH];
+  int32_t old[TTKV_MAX_BATCH], gone[TTKV_MAX_BATCH], most_moves[TTKV_MAX_BATCH];   // tokens that may go, that do, that may move
+  int64_t move_base[TTKV_MAX_BATCH];
+};
+static_assert(sizeof(LightArgs) <= 4096, "kernel arguments are passed by value");
+hipError_t launch_light(const LightArgs &a, int32_t most_moves, hipStream_t s, int *n_kernels);
+
 // Load-only kernel over `bytes` (rounded down to 64 KiB) of device memory; sink: 4 writable bytes.
 hipError_t launch_stream_read(const void *src, int64_t bytes, uint32_t *sink, hipStream_t s);
 

@@ -93,208 +93,141 @@ __device__ __forceinline__ void move_chunk_reference(ChunkRows &r, float mt, f16
   r.m = mn;
   r.far = unit ? (at + kRoom16) * r.inv_cs : mn;
 }
-// Where a row is kept from a token whose value is infinite or no number, a weight of 0 would still make a NaN of it.  So such values meet
-// the product as 0, and a row that does see one (its weight's operand `seen` is 1) gets NaN in that channel.
-template <bool BF>
-__device__ __forceinline__ void add_guarded(f16v &o, u32x4 va, const u32x4 &p, const u32x4 &seen) {
-  constexpr uint32_t exp1 = BF ? 0x7f80u : 0x7c00u, one = BF ? 0x3f80u : 0x3c00u;
-  u32x4 bad;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool low = (va[i] & exp1) == exp1, high = (va[i] >> 16 & exp1) == exp1;
-    va[i] &= ~((low ? 0xffffu : 0u) | (high ? 0xffff0000u : 0u));
-    bad[i] = (low ? one : 0u) | (high ? one << 16 : 0u);
+// Where a row is kept from a token whose value is infinite or no number, a weight of 0 would still make a NaN of it.  So in steps that not every row
+// of a tile sees such values go into LDS as 0 and into a list of bits, a byte for eight channels of a token, and a row that does see one gets
+// a NaN in that channel.
+struct Wild {
+  int step[2];                 // per buffer: the last step with such a value
+  uint8_t bits[2][32][16];
+};
+// Step's tokens below lim, by lane.
+__device__ __forceinline__ void spoil(f16v (&o)[4], const uint8_t (&bits)[32][16], int lim, int hh) {
+  u32x4 all = {0, 0, 0, 0};
+  for (int t = 0; t < 32; ++t) {
+    const u32x4 w = *(const u32x4 *)bits[t];
+    if (t < lim) all |= w;
   }
-  o = mma<BF>(va, p, o);
-  const f16v n = mma<BF>(bad, seen, f16v{});
 #pragma unroll
-  for (int i = 0; i < 16; ++i)
-    if (n[i] > 0.0f) o[i] = __builtin_nanf("");
-  __builtin_amdgcn_sched_barrier(0);   // one at a time: this is rare, and registers are dear
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)   // channel 32 d + 8 (i / 4) + 4 hh + i % 4
+      if (all[d] >> (8 * (i / 4) + 4 * hh + i % 4) & 1) o[d][i] = __builtin_nanf("");
 }
 
-// ---------------------------------------------------------------- the kernel
+// ---------------------------------------------------------------- a workgroup's part
 // RW waves of 32 rows each share the tokens' tiles, TW such teams take the steps of 32 tokens in turn.
-template <bool BF, bool QUANT, int RW, int TW>
-__global__ __launch_bounds__(64 * RW * TW, 1) void chunk_kernel(const ChunkArgs a) {
-  constexpr int NL = 8 / RW;                                     // pieces per thread of a step's keys (values)
-  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kParts = QUANT ? 2 : 1, kStep = kParts * (kKeys + kValues);
-  __shared__ __align__(16) char s_tile[TW * 2 * kStep];          // per team: keys and values of two steps; at the end what the waves exchange
-  __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
-  __shared__ int s_wild[TW][2];                                  // per buffer: the last step with a value that is infinite or none
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tw = wave / RW, rw = wave % RW, c = lane & 31, hh = lane >> 5;
-  const int tid = threadIdx.x & (64 * RW - 1);
-  const ChunkItem it = chunk_item(a, 32 * RW);
-  int total = 0;
-  for (int t = 0; t < a.n_tiers; ++t) total += chunk_tier(a, it, t).len;
-  const int row0 = it.row_tile * 32 * RW + rw * 32;
-  const bool idle = row0 >= it.rows;                             // a wave without rows only helps with the tiles
-  u32x4 qf[8];
-  ChunkRows r = begin_chunk_rows<BF>(a, it, total, row0 + c, hh, qf);
-  f16v o[4];
-#pragma unroll
-  for (int d = 0; d < 4; ++d) o[d] = f16v{};
-  // what the tile's rows see together, what this wave's first row and its last one see
-  const int base = total - it.count;
-  const int sees = max(0, base + 1 + token_of(a, min(it.row_tile * 32 * RW + 32 * RW, it.rows) - 1));
-  const int tile_sees = base + 1 + token_of(a, it.row_tile * 32 * RW);   // its first row
-  const int first_sees = base + 1 + token_of(a, min(row0, it.rows - 1)), last_sees = base + 1 + token_of(a, min(row0 + 31, it.rows - 1));
-  // this item's share of the steps, tiers one behind the other
-  int n_steps = 0, before = 0;
-  for (int t = 0; t < a.n_tiers; ++t) {
-    const int len = chunk_tier(a, it, t).len, n = min(max(sees - before, 0), len);
-    n_steps += (n + 31) / 32;
-    before += len;
-  }
-  const int per = ((n_steps + it.n_split - 1) / it.n_split + TW - 1) / TW * TW;
-  const int s0 = min(it.split * per, n_steps), s1 = min(s0 + per, n_steps);
-  char *const team = s_tile + tw * 2 * kStep;
-  const char *const k_at = team + k_lane(lane), *const v_at = team + kParts * kKeys + v_lane(lane);
-
-  auto run = [&](auto kf, auto vf, const TierView &tv, int seq, int tok, int len, int lo, int hi, int ahead) __attribute__((always_inline)) {
-    // steps lo .. hi - 1 of a tier of len tokens; `ahead`: tokens in the tiers before it
-    constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
-    const int mine = lo + tw;
-    Place keys(tv, seq, it.hkv, tok + 32 * (mine < hi ? mine : lo)), values = keys;
-    int ks = mine, vs = mine;
-    Piece<KF> kr[NL];
-    Piece<VF> vr[NL];
-    auto load_keys = [&]() __attribute__((always_inline)) {   // the team's next step, if there is one; behind the tier's end its last row
-      if (ks >= hi) return;
-      const int last = min(31, len - 32 * ks - 1);
-      const uint64_t codes = keys.head, meta = keys.head + tv.k_meta_off;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) kr[i] = load_piece<KF>(codes, meta, keys.row + min((tid >> 4) + 4 * RW * i, last), tid & 15);
-      ks += TW;
-      if (ks < hi) keys.advance(32 * TW);
-    };
-    auto load_values = [&]() __attribute__((always_inline)) {
-      if (vs >= hi) return;
-      const int last = min(31, len - 32 * vs - 1);
-      const uint64_t codes = values.head + tv.v_off, meta = values.head + tv.v_meta_off;
-#pragma unroll
-      for (int i = 0; i < NL; ++i) vr[i] = load_piece<VF>(codes, meta, values.row + min((tid >> 4) + 4 * RW * i, last), tid & 15);
-      vs += TW;
-      if (vs < hi) values.advance(32 * TW);
-    };
-    auto put_keys = [&](int at) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        char *const to = team + at + ((tid >> 4) + 4 * RW * i) * kRowK + (tid & 15) * 16;
-        put_piece<BF, KF>(kr[i], to, to + kKeys);
-      }
-    };
-    auto put_values = [&](int at, int step) __attribute__((always_inline)) {
-      if (32 * step + 32 <= tile_sees - ahead) {   // every row of the tile sees the step
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          char *const to = team + at + kParts * kKeys + ((tid >> 4) + 4 * RW * i) * kRowV + (tid & 15) * 16;
-          put_piece<BF, VF>(vr[i], to, to + kValues);
-        }
-      } else {
-        bool wild = false;
-#pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          char *const to = team + at + kParts * kKeys + ((tid >> 4) + 4 * RW * i) * kRowV + (tid & 15) * 16;
-          wild |= put_piece<BF, VF, true>(vr[i], to, to + kValues);
-        }
-        if (wild) s_wild[tw][at != 0] = step;
-      }
-    };
-    constexpr bool two_k = QUANT && KF != TTKV_F16 && KF != TTKV_BF16, two_v = QUANT && VF != TTKV_F16 && VF != TTKV_BF16;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) kr[i] = Piece<KF>{}, vr[i] = Piece<VF>{};
-    __syncthreads();   // everybody is done with the tier before
-    load_keys();
-    load_values();
-    put_keys(0);
-    load_keys();
-    if (tid == 0) s_wild[tw][0] = s_wild[tw][1] = -1;
-    __syncthreads();
-    put_values(0, mine);
-    load_values();
-    const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
-    int now = 0;
-    for (int t = 0; t < n_it; ++t) {
-      __syncthreads();   // the step is in its buffer; everybody is done with the other one
-      const int next = kStep - now, s = mine + TW * t;
-      const bool works = s < hi && !idle && 32 * s < last_sees - ahead;   // (wave-uniform)
-      f16v sc = {};
-      if (works) {
-#pragma unroll
-        for (int kb = 0; kb < 8; ++kb) {
-          sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
-          if constexpr (two_k) sc = mma<BF>(*(const u32x4 *)(k_at + now + kKeys + 32 * kb), qf[kb], sc);
-        }
-      }
-      put_keys(next);
-      load_keys();
-      if (works) {
-        const bool masked = 32 * s + 32 > min(first_sees - ahead, len), wild = masked && s_wild[tw][now != 0] == s;
-        if (masked) mask_from(sc, min(r.pos + 1 - ahead, len) - 32 * s, hh);
-        const float mt = step_max(sc);
-        if (__any(mt > r.far)) move_chunk_reference<BF>(r, mt, o);
-        u32x4 p[2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float w0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], r.cs, r.mcs)), w1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], r.cs, r.mcs));
-          r.l += w0 + w1;
-          p[i / 4][i % 4] = pack2<BF>(w0, w1);
-        }
-        if (wild) {
-          constexpr uint32_t one = BF ? 0x3f80u : 0x3c00u;
-          u32x4 seen[2];
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            seen[i / 4][i % 4] = (sc[2 * i] == -INFINITY ? 0u : one) | (sc[2 * i + 1] == -INFINITY ? 0u : one << 16);
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              add_guarded<BF>(o[d], value_operand(v_at + now, d, b), p[b], seen[b]);
-              if constexpr (two_v) add_guarded<BF>(o[d], value_operand(v_at + now + kValues, d, b), p[b], seen[b]);
-            }
-        } else {
-#pragma unroll
-          for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              o[d] = mma<BF>(value_operand(v_at + now, d, b), p[b], o[d]);
-              if constexpr (two_v) o[d] = mma<BF>(value_operand(v_at + now + kValues, d, b), p[b], o[d]);
-            }
-        }
-      }
-      put_values(next, s + TW);
-      load_values();
-      now = next;
+template <int RW, int TW>
+struct Share {
+  ChunkItem it;
+  int lane, tw, rw, c, hh, tid;      // tid: of the team
+  int row0;                          // of the wave
+  bool idle;                         // a wave without rows only helps with the tiles
+  int total, base;                   // tokens that the sequence attends; place of the first new one
+  int sees, tile_sees;               // tokens that the tile's last row sees, its first one
+  int first_sees, last_sees;         // of the wave's rows
+  int s0, s1;                        // this item's steps, tiers one behind the other
+  __device__ __forceinline__ explicit Share(const ChunkArgs &a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63;
+    tw = wave / RW;
+    rw = wave % RW;
+    c = lane & 31;
+    hh = lane >> 5;
+    tid = threadIdx.x & (64 * RW - 1);
+    it = chunk_item(a, 32 * RW);
+    total = 0;
+    for (int t = 0; t < a.n_tiers; ++t) total += chunk_tier(a, it, t).len;
+    row0 = it.row_tile * 32 * RW + rw * 32;
+    idle = row0 >= it.rows;
+    base = total - it.count;
+    sees = max(0, base + 1 + token_of(a, min(it.row_tile * 32 * RW + 32 * RW, it.rows) - 1));
+    tile_sees = base + 1 + token_of(a, it.row_tile * 32 * RW);
+    first_sees = base + 1 + token_of(a, min(row0, it.rows - 1));
+    last_sees = base + 1 + token_of(a, min(row0 + 31, it.rows - 1));
+    int n_steps = 0, before = 0;
+    for (int t = 0; t < a.n_tiers; ++t) {
+      const int len = chunk_tier(a, it, t).len, n = min(max(sees - before, 0), len);
+      n_steps += (n + 31) / 32;
+      before += len;
     }
-  };
-
-  int at = 0;
-  before = 0;
-  for (int t = 0; t < a.n_tiers; ++t) {
-    const ChunkTier T = chunk_tier(a, it, t);
-    const int n = (min(max(sees - before, 0), T.len) + 31) / 32;
-    const int lo = max(s0 - at, 0), hi = min(s1 - at, n);
-    if (lo < hi) {
-      const TierView &tv = a.tv[t];
-      const int seq = t < a.n_prefix ? 0 : it.seq;
-      constexpr int FP = BF ? TTKV_BF16 : TTKV_F16;
-      if constexpr (QUANT) {
-        if (tv.k_fmt == FP) run(num<FP>{}, num<FP>{}, tv, seq, T.tok, T.len, lo, hi, before);
-        else if (tv.k_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I4_ASYM_G64>{}, num<TTKV_I4_ASYM_G64>{}, tv, seq, T.tok, T.len, lo, hi, before);
-        else if (tv.v_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I4_ASYM_G64>{}, tv, seq, T.tok, T.len, lo, hi, before);
-        else run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I8_SYM_G32>{}, tv, seq, T.tok, T.len, lo, hi, before);
-      } else {
-        run(num<FP>{}, num<FP>{}, tv, seq, T.tok, T.len, lo, hi, before);
-      }
-    }
-    at += n;
-    before += T.len;
+    const int per = ((n_steps + it.n_split - 1) / it.n_split + TW - 1) / TW * TW;
+    s0 = min(it.split * per, n_steps);
+    s1 = min(s0 + per, n_steps);
   }
+  // f(tier, its run, its sequence, steps lo .. hi - 1 of it, tokens before it) for every tier that the item has steps of
+  template <typename F>
+  __device__ __forceinline__ void tiers(const ChunkArgs &a, F &&f) const {
+    int at = 0, before = 0;
+    for (int t = 0; t < a.n_tiers; ++t) {
+      const ChunkTier T = chunk_tier(a, it, t);
+      const int n = (min(max(sees - before, 0), T.len) + 31) / 32;
+      const int lo = max(s0 - at, 0), hi = min(s1 - at, n);
+      if (lo < hi) f(a.tv[t], T, t < a.n_prefix ? 0 : it.seq, lo, hi, before);
+      at += n;
+      before += T.len;
+    }
+  }
+};
 
-  // The teams' results meet: each wave ends with 128 / TW channels of its rows.
+// A team's rows of one tier on their way: steps mine, mine + TW, .. below hi; keys and values apart.
+template <int F, int RW, int TW>
+struct Stream {
+  static constexpr int NL = 8 / RW;   // pieces per thread and step
+  Place at;
+  int step, hi, len, tid;
+  uint32_t codes, meta;               // offsets of the sections in the head's part
+  Piece<F> x[NL];
+  __device__ __forceinline__ Stream(const Place &from, int mine, int hi_, int len_, int tid_, uint32_t codes_, uint32_t meta_)
+      : at(from), step(mine), hi(hi_), len(len_), tid(tid_), codes(codes_), meta(meta_) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) x[i] = Piece<F>{};
+  }
+  __device__ __forceinline__ void load() {   // the next step, if there is one; behind the tier's end its last row
+    if (step >= hi) return;
+    const int last = min(31, len - 32 * step - 1);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) x[i] = load_piece<F>(at.head + codes, at.head + meta, at.row + min((tid >> 4) + 4 * RW * i, last), tid & 15);
+    step += TW;
+    if (step < hi) at.advance(32 * TW);
+  }
+  template <bool BF>
+  __device__ __forceinline__ void put(char *to, int row_bytes, int part_bytes) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      char *const p = to + ((tid >> 4) + 4 * RW * i) * row_bytes + (tid & 15) * 16;
+      put_piece<BF, F>(x[i], p, p + part_bytes);
+    }
+  }
+  // Values of step `of`; all_see: tokens of the tier that every row of the tile sees.
+  template <bool BF>
+  __device__ __forceinline__ void put_values(char *to, int part_bytes, int of, int all_see, Wild &wild, int buffer) const {
+    if (32 * of + 32 <= all_see) return put<BF>(to, kRowV, part_bytes);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = (tid >> 4) + 4 * RW * i;
+      char *const p = to + row * kRowV + (tid & 15) * 16;
+      const uint32_t bits = put_piece<BF, F, true>(x[i], p, p + part_bytes);
+      wild.bits[buffer][row][tid & 15] = (uint8_t)bits;
+      if (bits) wild.step[buffer] = of;
+    }
+  }
+};
+
+// The rounded weights 2 i and 2 i + 1 of a step.
+template <bool BF>
+__device__ __forceinline__ void weigh2(ChunkRows &r, const f16v &sc, int i, u32x4 (&p)[2]) {
+  const float w0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], r.cs, r.mcs)), w1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], r.cs, r.mcs));
+  r.l += w0 + w1;
+  p[i / 4][i % 4] = pack2<BF>(w0, w1);
+}
+constexpr bool is_quant(int f) { return f != TTKV_F16 && f != TTKV_BF16; }
+
+// What the workgroup's rows come to: the teams' results meet, each wave ends with 128 / TW channels of its rows and stores them.
+template <int RW, int TW>
+__device__ __forceinline__ void finish(const ChunkArgs &a, const Share<RW, TW> &w, ChunkRows &r, f16v (&o)[4], char *s_tile, float (*s_m)[32], float (*s_l)[32]) {
+  const int lane = w.lane, tw = w.tw, rw = w.rw, c = w.c, hh = w.hh;
+  const ChunkItem &it = w.it;
+  const int row0 = w.row0;
   const f2 both = both32(r.l);
   r.l = both.x + both.y;
   float top = r.m == -INFINITY ? -INFINITY : -r.mcs, l = r.l;
@@ -390,6 +323,224 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_kernel(const ChunkArgs 
     a.lse[((int64_t)it.entry * a.n_tokens + r.token) * a.Hq + r.hq] = l == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(l) + top) * kLn2;
 }
 
+// run(key format, value format, ..) for every tier that the item has steps of.
+template <bool BF, bool QUANT, int RW, int TW, typename R>
+__device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW> &w, R &run) {
+  constexpr int FP = BF ? TTKV_BF16 : TTKV_F16;
+  w.tiers(a, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    if constexpr (QUANT) {
+      if (tv.k_fmt == FP) run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
+      else if (tv.k_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I4_ASYM_G64>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
+      else if (tv.v_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
+      else run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I8_SYM_G32>{}, tv, T, seq, lo, hi, ahead);
+    } else {
+      run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
+    }
+  });
+}
+
+// ---------------------------------------------------------------- few rows
+// Bound: memory.  Keys of one step and values of the one before are on their way while one is computed.
+template <bool BF, bool QUANT, int RW, int TW>
+__global__ __launch_bounds__(64 * RW * TW, 1) void chunk_kernel(const ChunkArgs a) {
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kParts = QUANT ? 2 : 1, kStep = kParts * (kKeys + kValues);
+  __shared__ __align__(16) char s_tile[TW * 2 * kStep];          // per team: keys and values of two steps; at the end what the waves exchange
+  __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
+  __shared__ Wild s_wild[TW];
+  const Share<RW, TW> w(a);
+  u32x4 qf[8];
+  ChunkRows r = begin_chunk_rows<BF>(a, w.it, w.total, w.row0 + w.c, w.hh, qf);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) o[d] = f16v{};
+  char *const team = s_tile + w.tw * 2 * kStep;
+  const char *const k_at = team + k_lane(w.lane), *const v_at = team + kParts * kKeys + v_lane(w.lane);
+
+  auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF);
+    const int mine = lo + w.tw;
+    const Place from(tv, seq, w.it.hkv, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    Wild &wild = s_wild[w.tw];
+    auto put_values = [&](int at, int step) __attribute__((always_inline)) {
+      values.template put_values<BF>(team + at + kParts * kKeys, kValues, step, w.tile_sees - ahead, wild, at != 0);
+    };
+    __syncthreads();   // everybody is done with the tier before
+    keys.load();
+    values.load();
+    if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
+    __syncthreads();
+    keys.template put<BF>(team, kRowK, kKeys);
+    keys.load();
+    put_values(0, mine);
+    values.load();
+    const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
+    int now = 0;
+    for (int t = 0; t < n_it; ++t) {
+      __syncthreads();   // the step is in its buffer; everybody is done with the other one
+      const int next = kStep - now, s = mine + TW * t;
+      const bool works = s < hi && !w.idle && 32 * s < w.last_sees - ahead;   // (wave-uniform)
+      f16v sc = {};
+      if (works) {
+#pragma unroll
+        for (int kb = 0; kb < 8; ++kb) {
+          sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
+          if constexpr (two_k) sc = mma<BF>(*(const u32x4 *)(k_at + now + kKeys + 32 * kb), qf[kb], sc);
+        }
+      }
+      keys.template put<BF>(team + next, kRowK, kKeys);
+      keys.load();
+      if (works) {
+        const bool masked = 32 * s + 32 > min(w.first_sees - ahead, T.len);
+        const int lim = min(r.pos + 1 - ahead, T.len) - 32 * s;
+        if (masked) mask_from(sc, lim, w.hh);
+        const float mt = step_max(sc);
+        if (__any(mt > r.far)) move_chunk_reference<BF>(r, mt, o);
+        u32x4 p[2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) weigh2<BF>(r, sc, i, p);
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            o[d] = mma<BF>(value_operand(v_at + now, d, b), p[b], o[d]);
+            if constexpr (two_v) o[d] = mma<BF>(value_operand(v_at + now + kValues, d, b), p[b], o[d]);
+          }
+        if (32 * s + 32 > w.tile_sees - ahead && wild.step[now != 0] == s) spoil(o, wild.bits[now != 0], lim, w.hh);
+      }
+      put_values(next, s + TW);
+      values.load();
+      now = next;
+    }
+  };
+  each_tier<BF, QUANT>(a, w, run);
+  finish(a, w, r, o, s_tile, s_m, s_l);
+}
+
+// ---------------------------------------------------------------- many rows
+// Bound: the matrix cores and the vector unit alike.  The steps overlap inside a wave: while the softmax of step s runs on the vector
+// unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  LDS holds two steps' keys and values (s + 1 and
+// s + 2; s - 1 and s), one barrier per step.
+template <bool BF, bool QUANT, int RW, int TW>
+__global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kParts = QUANT ? 2 : 1, kTeam = 2 * kParts * (kKeys + kValues);
+  __shared__ __align__(16) char s_tile[TW * kTeam];              // per team: keys of even and odd steps, values of even and odd steps
+  __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
+  __shared__ Wild s_wild[TW];
+  const Share<RW, TW> w(a);
+  u32x4 qf[8];
+  ChunkRows r = begin_chunk_rows<BF>(a, w.it, w.total, w.row0 + w.c, w.hh, qf);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) o[d] = f16v{};
+  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 2 * kParts * kKeys;
+  const char *const k_at = team + k_lane(w.lane), *const v_at = team_v + v_lane(w.lane);
+
+  auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF);
+    const int mine = lo + w.tw;
+    const Place from(tv, seq, w.it.hkv, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    const int seen_by_all = min(w.first_sees - ahead, T.len), seen = w.idle ? 0 : min(32 * hi, w.last_sees - ahead);   // by the wave's rows
+    const int lim = min(r.pos + 1 - ahead, T.len);
+    auto put_keys = [&](int odd) __attribute__((always_inline)) { keys.template put<BF>(team + odd * kParts * kKeys, kRowK, kKeys); };
+    Wild &wild = s_wild[w.tw];
+    auto put_values = [&](int odd, int step) __attribute__((always_inline)) {
+      values.template put_values<BF>(team_v + odd * kParts * kValues, kValues, step, w.tile_sees - ahead, wild, odd);
+    };
+    auto score = [&](f16v &x, int odd, int kb) __attribute__((always_inline)) {
+      const char *const k = k_at + odd * kParts * kKeys + 32 * kb;
+      x = mma<BF>(*(const u32x4 *)k, qf[kb], x);
+      if constexpr (two_k) x = mma<BF>(*(const u32x4 *)(k + kKeys), qf[kb], x);
+    };
+    auto value = [&](int odd, int d, int b, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+      const char *const v = v_at + odd * kParts * kValues;
+      o[d] = mma<BF>(value_operand(v, d, b), p[b], o[d]);
+      if constexpr (two_v) o[d] = mma<BF>(value_operand(v + kValues, d, b), p[b], o[d]);
+    };
+    // The weights of step s meet its values, by themselves.
+    auto flush = [&](int odd, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) value(odd, d, b, p);
+    };
+    auto spoil_by = [&](int odd, int s) __attribute__((always_inline)) {
+      if (32 * s + 32 > w.tile_sees - ahead && wild.step[odd] == s) spoil(o, wild.bits[odd], lim - 32 * s, w.hh);
+    };
+    // Step s, in buffers ODD: sc its scores, p the weights of the step before, which wait where `pending`; next and pn receive the next step's scores and
+    // its own weights.
+    auto body = [&](int s, auto odd_tag, f16v &sc, f16v &next, u32x4 (&p)[2], u32x4 (&pn)[2], bool &pending) __attribute__((always_inline)) {
+      constexpr int ODD = decltype(odd_tag)::value;
+      __syncthreads();   // keys of the next step and values of the one before are there; everybody is done with those of this one and the one before that
+      if (pending) spoil_by(1 - ODD, s - TW);
+      const bool works = 32 * s < seen;   // (wave-uniform)
+      const float mt = step_max(sc);
+      const bool moves = works && __any(mt > r.far);
+      if (pending && (moves || !works)) {
+        flush(1 - ODD, p);
+        pending = false;
+      }
+      if (moves) move_chunk_reference<BF>(r, mt, o);
+      put_keys(ODD);
+      put_values(ODD, s);
+      keys.load();
+      values.load();
+      if (works) {
+        f16v nx = {};
+        if (pending) {
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
+            value(1 - ODD, g / 2, g % 2, p);
+            score(nx, 1 - ODD, g);
+            weigh2<BF>(r, sc, g, pn);
+          }
+        } else {
+#pragma unroll
+          for (int g = 0; g < 8; ++g) {
+            score(nx, 1 - ODD, g);
+            weigh2<BF>(r, sc, g, pn);
+          }
+        }
+        if (32 * (s + TW) + 32 > seen_by_all) mask_from(nx, lim - 32 * (s + TW), w.hh);
+        next = nx;
+      }
+      pending = works;
+    };
+    u32x4 p0[2], p1[2];
+    __syncthreads();   // everybody is done with the tier before
+    if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
+    keys.load();
+    put_keys(0);
+    keys.load();
+    put_keys(1);
+    keys.load();
+    values.load();
+    __syncthreads();
+    f16v s0 = {}, s1 = {};
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) score(s0, 0, kb);
+    if (32 * mine + 32 > seen_by_all) mask_from(s0, lim - 32 * mine, w.hh);
+    bool pending = false;
+    const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
+    for (int t = 0; t < n_it; t += 2) {
+      body(mine + TW * t, num<0>{}, s0, s1, p0, p1, pending);
+      body(mine + TW * (t + 1), num<1>{}, s1, s0, p1, p0, pending);
+    }
+    __syncthreads();
+    if (pending) {
+      spoil_by(1, mine + TW * ((n_it + 1) / 2 * 2 - 1));
+      flush(1, p0);
+    }
+  };
+  each_tier<BF, QUANT>(a, w, run);
+  finish(a, w, r, o, s_tile, s_m, s_l);
+}
+
 // The items of a row tile joined: a wave per query row, two channels per lane.
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int n_rows) {
   const int lane = threadIdx.x & 63;
@@ -421,8 +572,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int
 template <bool BF, bool QUANT>
 void start(const ChunkArgs &a, int rows, hipStream_t s) {
   const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv);
-  if (rows == 256) hipLaunchKernelGGL((chunk_kernel<BF, QUANT, 8, 1>), grid, dim3(512), 0, s, a);
-  else if (rows == 128) hipLaunchKernelGGL((chunk_kernel<BF, QUANT, 4, 2>), grid, dim3(512), 0, s, a);
+  if (rows == 256) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, 8, 1>), grid, dim3(512), 0, s, a);
+  else if (rows == 128) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, 4, 2>), grid, dim3(512), 0, s, a);
   else if constexpr (!QUANT) hipLaunchKernelGGL((chunk_kernel<BF, QUANT, 2, 4>), grid, dim3(512), 0, s, a);
 }
 

@@ -61,14 +61,18 @@ __device__ __forceinline__ void two_parts(const float (&v)[8], u32x4 &hi, u32x4 
     lo[i] = pack2<BF>(v[2 * i] - h.x, v[2 * i + 1] - h.y);
   }
 }
-// Whether one of eight numbers is infinite or none.
+// Which of eight numbers are infinite or none, a bit each; they become 0.
 template <bool BF>
-__device__ __forceinline__ bool any_wild(const u32x4 &w) {
-  constexpr uint32_t exp1 = BF ? 0x7f80u : 0x7c00u, exp2 = exp1 << 16;
-  bool any = false;
+__device__ __forceinline__ uint32_t take_wild(u32x4 &w) {
+  constexpr uint32_t exp1 = BF ? 0x7f80u : 0x7c00u;
+  uint32_t bits = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) any |= (w[i] & exp1) == exp1 || (w[i] & exp2) == exp2;
-  return any;
+  for (int i = 0; i < 4; ++i) {
+    const bool low = (w[i] & exp1) == exp1, high = (w[i] >> 16 & exp1) == exp1;
+    bits |= (low ? 1u << 2 * i : 0u) | (high ? 2u << 2 * i : 0u);
+    w[i] &= ~((low ? 0xffffu : 0u) | (high ? 0xffff0000u : 0u));
+  }
+  return bits;
 }
 // Eight decompressed channels as two numbers each.
 template <bool BF, int F>
@@ -86,17 +90,20 @@ __device__ __forceinline__ void unpack_piece(const Piece<F> &x, u32x4 &hi, u32x4
   two_parts<BF>(v, hi, lo);
 }
 template <bool BF, int F, bool CHECK = false>
-__device__ __forceinline__ bool put_piece(const Piece<F> &x, char *hi, char *lo) {
+__device__ __forceinline__ uint32_t put_piece(const Piece<F> &x, char *hi, char *lo) {
+  uint32_t wild = 0;
   if constexpr (F == TTKV_I8_SYM_G32 || F == TTKV_I4_ASYM_G64) {
     u32x4 h, l;
     unpack_piece<BF, F>(x, h, l);
+    if constexpr (CHECK) wild = take_wild<BF>(h) | take_wild<BF>(l);
     *(u32x4 *)hi = h;
     *(u32x4 *)lo = l;
-    return CHECK && (any_wild<BF>(h) || any_wild<BF>(l));
   } else {
-    *(u32x4 *)hi = x.w;
-    return CHECK && any_wild<BF>(x.w);
+    u32x4 h = x.w;
+    if constexpr (CHECK) wild = take_wild<BF>(h);
+    *(u32x4 *)hi = h;
   }
+  return wild;
 }
 // Queries of a bf16 model over fp16 tiers (exact inside the fp16 normal range, clamped outside; what is no number stays none).
 __device__ __forceinline__ void to_fp16(u32x4 &x) {

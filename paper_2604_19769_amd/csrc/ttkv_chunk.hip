@@ -98,11 +98,12 @@ __device__ __forceinline__ void move_chunk_reference(ChunkRows &r, float mt, f16
 // a NaN in that channel.
 struct Wild {
   int step[2];                 // per buffer: the last step with such a value
-  uint8_t bits[2][32][16];
+  __align__(16) uint8_t bits[2][32][16];
 };
 // Step's tokens below lim, by lane.
 __device__ __forceinline__ void spoil(f16v (&o)[4], const uint8_t (&bits)[32][16], int lim, int hh) {
   u32x4 all = {0, 0, 0, 0};
+#pragma unroll 1
   for (int t = 0; t < 32; ++t) {
     const u32x4 w = *(const u32x4 *)bits[t];
     if (t < lim) all |= w;
@@ -419,6 +420,22 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_kernel(const ChunkArgs 
   finish(a, w, r, o, s_tile, s_m, s_l);
 }
 
+// Keeps a step's products and its softmax side by side: after every product some vector instructions and the next operands' loads.
+template <bool TWO_K, bool TWO_V>
+__device__ __forceinline__ void interleave() {
+  constexpr int pairs = 1 + (TWO_K && TWO_V), vector = 6 / (2 * pairs);
+  __builtin_amdgcn_sched_group_barrier(0x100, 9, 0);
+#pragma unroll
+  for (int i = 0; i < 8 * pairs; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, vector, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, vector, 0);
+  }
+}
+
 // ---------------------------------------------------------------- many rows
 // Bound: the matrix cores and the vector unit alike.  The steps overlap inside a wave: while the softmax of step s runs on the vector
 // unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  LDS holds two steps' keys and values (s + 1 and
@@ -472,8 +489,8 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
     auto spoil_by = [&](int odd, int s) __attribute__((always_inline)) {
       if (32 * s + 32 > w.tile_sees - ahead && wild.step[odd] == s) spoil(o, wild.bits[odd], lim - 32 * s, w.hh);
     };
-    // Step s, in buffers ODD: sc its scores, p the weights of the step before, which wait where `pending`; next and pn receive the next step's scores and
-    // its own weights.
+    // Step s, in buffers ODD: sc its scores, p the weights of the step before (zeros where its values are added already); next and pn receive
+    // the next step's scores and its own weights.
     auto body = [&](int s, auto odd_tag, f16v &sc, f16v &next, u32x4 (&p)[2], u32x4 (&pn)[2], bool &pending) __attribute__((always_inline)) {
       constexpr int ODD = decltype(odd_tag)::value;
       __syncthreads();   // keys of the next step and values of the one before are there; everybody is done with those of this one and the one before that
@@ -481,38 +498,36 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
       const bool works = 32 * s < seen;   // (wave-uniform)
       const float mt = step_max(sc);
       const bool moves = works && __any(mt > r.far);
-      if (pending && (moves || !works)) {
-        flush(1 - ODD, p);
-        pending = false;
+      if (moves || !works) {
+        if (pending) flush(1 - ODD, p);
+        p[0] = p[1] = u32x4{0, 0, 0, 0};
+        if (moves) move_chunk_reference<BF>(r, mt, o);
       }
-      if (moves) move_chunk_reference<BF>(r, mt, o);
       put_keys(ODD);
       put_values(ODD, s);
       keys.load();
       values.load();
       if (works) {
         f16v nx = {};
-        if (pending) {
 #pragma unroll
-          for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
-            value(1 - ODD, g / 2, g % 2, p);
-            score(nx, 1 - ODD, g);
-            weigh2<BF>(r, sc, g, pn);
-          }
-        } else {
-#pragma unroll
-          for (int g = 0; g < 8; ++g) {
-            score(nx, 1 - ODD, g);
-            weigh2<BF>(r, sc, g, pn);
-          }
+        for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
+          value(1 - ODD, g / 2, g % 2, p);
+          score(nx, 1 - ODD, g);
+          weigh2<BF>(r, sc, g, pn);
         }
+        // (kept here: the weights are wanted in the next step only, and would be worked out there, behind the products)
+        asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(r.l));
+        interleave<two_k, two_v>();
         if (32 * (s + TW) + 32 > seen_by_all) mask_from(nx, lim - 32 * (s + TW), w.hh);
         next = nx;
       }
       pending = works;
     };
     u32x4 p0[2], p1[2];
+    p0[0] = p0[1] = u32x4{0, 0, 0, 0};
     __syncthreads();   // everybody is done with the tier before
+    // there is no step before the first: weights of zero meet zeros
+    for (int i = w.tid; i < kParts * kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + kParts * kValues))[i] = u32x4{0, 0, 0, 0};
     if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
     keys.load();
     put_keys(0);

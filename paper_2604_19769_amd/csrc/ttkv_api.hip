@@ -1747,7 +1747,7 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
   if (n_slots == 0) return TTKV_OK;
   if (P.rows * a.Hkv >= 1ll << 28) return TTKV_ERR_UNSUPPORTED;   // a launch has 2^32 threads at most
   std::sort(slot, slot + n_slots, [](const Slot &x, const Slot &y) { return x.sees != y.sees ? x.sees > y.sees : x.entry < y.entry; });
-  P.shape = chunk_shape(most_rows, bf16 || (!f16 && q_fmt == TTKV_BF16), quantized);
+  P.shape = chunk_shape(most_rows, bf16, quantized);
   int64_t tiles[TTKV_MAX_BATCH], work = 0;
   for (int i = 0; i < n_slots; ++i) {
     tiles[i] = (slot[i].n * a.G + P.shape.rows - 1) / P.shape.rows;
@@ -1914,7 +1914,7 @@ ttkv_status ttkv_add_weights(ttkv_handle hh, const ttkv_cache *c, int32_t tier, 
   a.n_items = (int32_t)items;
   a.hkv_magic = a.Hkv > 1 && items * a.Hkv * a.Hkv < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.Hkv - 1) / a.Hkv) : 0;
   a.g_magic = a.G > 1 && most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
-  TTKV_HIP(h, launch_weigh(a, T.k_fmt == TTKV_BF16 || (T.k_fmt != TTKV_F16 && q->fmt == TTKV_BF16), (hipStream_t)stream));
+  TTKV_HIP(h, launch_weigh(a, (hipStream_t)stream));
   h->stats.kernels += 1;
   return TTKV_OK;
 }

@@ -6,8 +6,9 @@
 // rows as columns, so a lane has 16 scores of ONE row and the scores' registers are the second product's operand as they lie.
 //
 // Outputs are 16 bits wide, so the weights are rounded once to the product's type; their sum, the maximum and the log-sum-exp stay fp32.
-// A quantized tier's rows are decompressed on their way into LDS, into two numbers of the product's type each (22 or 16 bits), and
-// every product is made of both.
+// Quantized tiers are worked on in fp16 whatever the others' type, in front of them.  Their rows are decompressed on their way into LDS, keys
+// into two numbers each (22 bits: the log-sum-exp is an fp32 number), values into two where the outputs are fp16, into one where bf16 outputs
+// end far above what that rounds.
 #include "ttkv_chunk_dev.h"
 
 #include <algorithm>
@@ -61,25 +62,28 @@ struct ChunkRows {
   int token, hq, pos;     // new token, query head, place behind the oldest token
   bool on;
 };
-template <bool BF>
-__device__ __forceinline__ ChunkRows begin_chunk_rows(const ChunkArgs &a, const ChunkItem &it, int total, int row, int hh, u32x4 (&qf)[8]) {
+__device__ __forceinline__ ChunkRows begin_chunk_rows(const ChunkArgs &a, const ChunkItem &it, int total, int row) {
   ChunkRows r;
   r.on = row < it.rows;
   row = min(row, it.rows - 1);
   r.token = token_of(a, row);
   r.hq = it.hkv * a.G + row - r.token * a.G;
   r.pos = total - it.count + r.token;
+  r.cs = a.scale * kLog2e;
+  r.inv_cs = 1.0f / r.cs;
+  r.m = r.far = -INFINITY;
+  r.l = r.mcs = 0.0f;
+  return r;
+}
+// The row's channels 16 kb + 8 hh .. + 7 in qf[kb], in the product's type.
+template <bool BF>
+__device__ __forceinline__ void load_query(const ChunkArgs &a, const ChunkItem &it, const ChunkRows &r, int hh, u32x4 (&qf)[8]) {
   const u32x4 *qp = (const u32x4 *)(a.q + it.entry * a.q_seq + r.token * a.q_token + r.hq * a.q_head);
 #pragma unroll
   for (int kb = 0; kb < 8; ++kb) qf[kb] = qp[2 * kb + hh];
   if (!BF && a.q_fmt == TTKV_BF16)
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb) to_fp16(qf[kb]);
-  r.cs = a.scale * kLog2e;
-  r.inv_cs = 1.0f / r.cs;
-  r.m = r.far = -INFINITY;
-  r.l = r.mcs = 0.0f;
-  return r;
 }
 template <bool BF>
 __device__ __forceinline__ void move_chunk_reference(ChunkRows &r, float mt, f16v (&o)[4]) {
@@ -155,15 +159,16 @@ struct Share {
     s0 = min(it.split * per, n_steps);
     s1 = min(s0 + per, n_steps);
   }
-  // f(tier, its run, its sequence, steps lo .. hi - 1 of it, tokens before it) for every tier that the item has steps of
+  // f(tier, its run, its sequence, steps lo .. hi - 1 of it, tokens before it) for every quantized (or every other) tier that the item has
+  // steps of
   template <typename F>
-  __device__ __forceinline__ void tiers(const ChunkArgs &a, F &&f) const {
+  __device__ __forceinline__ void tiers(const ChunkArgs &a, bool quantized, F &&f) const {
     int at = 0, before = 0;
     for (int t = 0; t < a.n_tiers; ++t) {
       const ChunkTier T = chunk_tier(a, it, t);
       const int n = (min(max(sees - before, 0), T.len) + 31) / 32;
       const int lo = max(s0 - at, 0), hi = min(s1 - at, n);
-      if (lo < hi) f(a.tv[t], T, t < a.n_prefix ? 0 : it.seq, lo, hi, before);
+      if (lo < hi && quantized == is_quant(a.tv[t].k_fmt)) f(a.tv[t], T, t < a.n_prefix ? 0 : it.seq, lo, hi, before);
       at += n;
       before += T.len;
     }
@@ -174,12 +179,13 @@ struct Share {
 template <int F, int RW, int TW>
 struct Stream {
   static constexpr int NL = 8 / RW;   // pieces per thread and step
+  const Ring &ring;
   Place at;
   int step, hi, len, tid;
   uint32_t codes, meta;               // offsets of the sections in the head's part
   Piece<F> x[NL];
-  __device__ __forceinline__ Stream(const Place &from, int mine, int hi_, int len_, int tid_, uint32_t codes_, uint32_t meta_)
-      : at(from), step(mine), hi(hi_), len(len_), tid(tid_), codes(codes_), meta(meta_) {
+  __device__ __forceinline__ Stream(const Ring &g, const Place &from, int mine, int hi_, int len_, int tid_, uint32_t codes_, uint32_t meta_)
+      : ring(g), at(from), step(mine), hi(hi_), len(len_), tid(tid_), codes(codes_), meta(meta_) {
 #pragma unroll
     for (int i = 0; i < NL; ++i) x[i] = Piece<F>{};
   }
@@ -189,25 +195,25 @@ struct Stream {
 #pragma unroll
     for (int i = 0; i < NL; ++i) x[i] = load_piece<F>(at.head + codes, at.head + meta, at.row + min((tid >> 4) + 4 * RW * i, last), tid & 15);
     step += TW;
-    if (step < hi) at.advance(32 * TW);
+    if (step < hi) at.advance(ring, 32 * TW);
   }
-  template <bool BF>
+  template <bool BF, bool TWO>
   __device__ __forceinline__ void put(char *to, int row_bytes, int part_bytes) const {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       char *const p = to + ((tid >> 4) + 4 * RW * i) * row_bytes + (tid & 15) * 16;
-      put_piece<BF, F>(x[i], p, p + part_bytes);
+      put_piece<BF, F, TWO>(x[i], p, p + part_bytes);
     }
   }
   // Values of step `of`; all_see: tokens of the tier that every row of the tile sees.
-  template <bool BF>
+  template <bool BF, bool TWO>
   __device__ __forceinline__ void put_values(char *to, int part_bytes, int of, int all_see, Wild &wild, int buffer) const {
-    if (32 * of + 32 <= all_see) return put<BF>(to, kRowV, part_bytes);
+    if (32 * of + 32 <= all_see) return put<BF, TWO>(to, kRowV, part_bytes);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = (tid >> 4) + 4 * RW * i;
       char *const p = to + row * kRowV + (tid & 15) * 16;
-      const uint32_t bits = put_piece<BF, F, true>(x[i], p, p + part_bytes);
+      const uint32_t bits = put_piece<BF, F, TWO, true>(x[i], p, p + part_bytes);
       wild.bits[buffer][row][tid & 15] = (uint8_t)bits;
       if (bits) wild.step[buffer] = of;
     }
@@ -221,7 +227,6 @@ __device__ __forceinline__ void weigh2(ChunkRows &r, const f16v &sc, int i, u32x
   r.l += w0 + w1;
   p[i / 4][i % 4] = pack2<BF>(w0, w1);
 }
-constexpr bool is_quant(int f) { return f != TTKV_F16 && f != TTKV_BF16; }
 
 // What the workgroup's rows come to: the teams' results meet, each wave ends with 128 / TW channels of its rows and stores them.
 template <int RW, int TW>
@@ -324,99 +329,135 @@ __device__ __forceinline__ void finish(const ChunkArgs &a, const Share<RW, TW> &
     a.lse[((int64_t)it.entry * a.n_tokens + r.token) * a.Hq + r.hq] = l == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(l) + top) * kLn2;
 }
 
-// run(key format, value format, ..) for every tier that the item has steps of.
+// run(key format, value format, ..) for every tier that the item has steps of, the quantized ones first.  Their weights are fp16 numbers and carry that
+// type's power of two; beside bf16 tiers it changes in between.
 template <bool BF, bool QUANT, int RW, int TW, typename R>
-__device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW> &w, R &run) {
+__device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW> &w, ChunkRows &r, f16v (&o)[4], u32x4 (&qf)[8], R &run) {
   constexpr int FP = BF ? TTKV_BF16 : TTKV_F16;
-  w.tiers(a, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
-    if constexpr (QUANT) {
-      if (tv.k_fmt == FP) run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
-      else if (tv.k_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I4_ASYM_G64>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
+  if constexpr (QUANT) {
+    load_query<false>(a, w.it, r, w.hh, qf);
+    w.tiers(a, true, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+      if (tv.k_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I4_ASYM_G64>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
       else if (tv.v_fmt == TTKV_I4_ASYM_G64) run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
       else run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I8_SYM_G32>{}, tv, T, seq, lo, hi, ahead);
-    } else {
-      run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
+    });
+    if constexpr (BF) {
+      constexpr float step = unit16<true>() - unit16<false>();
+      if (fabsf(r.mcs) < kFar) {   // (a reference beyond carries none)
+        const float by = __builtin_amdgcn_exp2f(step);
+        if (r.m != -INFINITY) r.mcs += step;
+        r.l *= by;
+        rescale(o, by);
+      }
     }
+  }
+  if constexpr (BF || !QUANT) load_query<BF>(a, w.it, r, w.hh, qf);
+  w.tiers(a, false, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
   });
 }
 
 // ---------------------------------------------------------------- few rows
-// Bound: memory.  Keys of one step and values of the one before are on their way while one is computed.
-template <bool BF, bool QUANT, int RW, int TW>
-__global__ __launch_bounds__(64 * RW * TW, 1) void chunk_kernel(const ChunkArgs a) {
-  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kParts = QUANT ? 2 : 1, kStep = kParts * (kKeys + kValues);
-  __shared__ __align__(16) char s_tile[TW * 2 * kStep];          // per team: keys and values of two steps; at the end what the waves exchange
+// Bound: memory.  Keys of one step and values of the one before are on their way while one is computed.  With quantized tiers LDS holds one step
+// only, so that a CU has two workgroups: one decompresses while the other computes.
+template <bool BF, bool QUANT, bool V2, int RW, int TW>
+__global__ __launch_bounds__(64 * RW * TW, QUANT ? 2 : 1) void chunk_kernel(const ChunkArgs a) {
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = QUANT ? 2 : 1, kPartsV = V2 ? 2 : 1, kStep = kPartsK * kKeys + kPartsV * kValues;
+  constexpr int kBuffers = QUANT ? 1 : 2;
+  __shared__ __align__(16) char s_tile[TW * kBuffers * kStep];   // per team: keys and values of two steps (one); at the end what the waves exchange
+  static_assert(TW * kBuffers * kStep >= TW * RW * (16 - 16 / TW) * 1024, "room for what the waves exchange");
   __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
   __shared__ Wild s_wild[TW];
   const Share<RW, TW> w(a);
   u32x4 qf[8];
-  ChunkRows r = begin_chunk_rows<BF>(a, w.it, w.total, w.row0 + w.c, w.hh, qf);
+  ChunkRows r = begin_chunk_rows(a, w.it, w.total, w.row0 + w.c);
   f16v o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] = f16v{};
-  char *const team = s_tile + w.tw * 2 * kStep;
-  const char *const k_at = team + k_lane(w.lane), *const v_at = team + kParts * kKeys + v_lane(w.lane);
+  char *const team = s_tile + w.tw * kBuffers * kStep;
+  const char *const k_at = team + k_lane(w.lane), *const v_at = team + kPartsK * kKeys + v_lane(w.lane);
 
   auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
     constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
-    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF);
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF) && V2, BT = BF && !is_quant(KF);   // the product's type: quantized tiers in fp16
     const int mine = lo + w.tw;
-    const Place from(tv, seq, w.it.hkv, T.tok + 32 * (mine < hi ? mine : lo));
-    Stream<KF, RW, TW> keys(from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
-    Stream<VF, RW, TW> values(from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    const Ring ring(tv, seq, w.it.hkv);
+    const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
     Wild &wild = s_wild[w.tw];
     auto put_values = [&](int at, int step) __attribute__((always_inline)) {
-      values.template put_values<BF>(team + at + kParts * kKeys, kValues, step, w.tile_sees - ahead, wild, at != 0);
+      values.template put_values<BT, two_v>(team + at + kPartsK * kKeys, kValues, step, w.tile_sees - ahead, wild, at != 0);
+    };
+    auto put_keys = [&](int at) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + at, kRowK, kKeys); };
+    auto works = [&](int s) __attribute__((always_inline)) { return s < hi && !w.idle && 32 * s < w.last_sees - ahead; };   // (wave-uniform)
+    auto scores = [&](int at, f16v &sc) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb) {
+        sc = mma<BT>(*(const u32x4 *)(k_at + at + 32 * kb), qf[kb], sc);
+        if constexpr (two_k) sc = mma<BT>(*(const u32x4 *)(k_at + at + kKeys + 32 * kb), qf[kb], sc);
+      }
+    };
+    auto attend = [&](int at, int s, f16v &sc) __attribute__((always_inline)) {
+      const int lim = min(r.pos + 1 - ahead, T.len) - 32 * s;
+      if (32 * s + 32 > min(w.first_sees - ahead, T.len)) mask_from(sc, lim, w.hh);
+      const float mt = step_max(sc);
+      if (__any(mt > r.far)) move_chunk_reference<BT>(r, mt, o);
+      u32x4 p[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) weigh2<BT>(r, sc, i, p);
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          o[d] = mma<BT>(value_operand(v_at + at, d, b), p[b], o[d]);
+          if constexpr (two_v) o[d] = mma<BT>(value_operand(v_at + at + kValues, d, b), p[b], o[d]);
+        }
+      if (32 * s + 32 > w.tile_sees - ahead && wild.step[at != 0] == s) spoil(o, wild.bits[at != 0], lim, w.hh);
     };
     __syncthreads();   // everybody is done with the tier before
     keys.load();
     values.load();
     if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
     __syncthreads();
-    keys.template put<BF>(team, kRowK, kKeys);
-    keys.load();
-    put_values(0, mine);
-    values.load();
     const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
-    int now = 0;
-    for (int t = 0; t < n_it; ++t) {
-      __syncthreads();   // the step is in its buffer; everybody is done with the other one
-      const int next = kStep - now, s = mine + TW * t;
-      const bool works = s < hi && !w.idle && 32 * s < w.last_sees - ahead;   // (wave-uniform)
-      f16v sc = {};
-      if (works) {
-#pragma unroll
-        for (int kb = 0; kb < 8; ++kb) {
-          sc = mma<BF>(*(const u32x4 *)(k_at + now + 32 * kb), qf[kb], sc);
-          if constexpr (two_k) sc = mma<BF>(*(const u32x4 *)(k_at + now + kKeys + 32 * kb), qf[kb], sc);
+    if constexpr (QUANT) {
+      for (int t = 0; t < n_it; ++t) {
+        const int s = mine + TW * t;
+        put_keys(0);
+        put_values(0, s);
+        keys.load();
+        values.load();
+        __syncthreads();
+        if (works(s)) {
+          f16v sc = {};
+          scores(0, sc);
+          attend(0, s, sc);
         }
+        __syncthreads();
       }
-      keys.template put<BF>(team + next, kRowK, kKeys);
+    } else {
+      put_keys(0);
       keys.load();
-      if (works) {
-        const bool masked = 32 * s + 32 > min(w.first_sees - ahead, T.len);
-        const int lim = min(r.pos + 1 - ahead, T.len) - 32 * s;
-        if (masked) mask_from(sc, lim, w.hh);
-        const float mt = step_max(sc);
-        if (__any(mt > r.far)) move_chunk_reference<BF>(r, mt, o);
-        u32x4 p[2];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) weigh2<BF>(r, sc, i, p);
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            o[d] = mma<BF>(value_operand(v_at + now, d, b), p[b], o[d]);
-            if constexpr (two_v) o[d] = mma<BF>(value_operand(v_at + now + kValues, d, b), p[b], o[d]);
-          }
-        if (32 * s + 32 > w.tile_sees - ahead && wild.step[now != 0] == s) spoil(o, wild.bits[now != 0], lim, w.hh);
-      }
-      put_values(next, s + TW);
+      put_values(0, mine);
       values.load();
-      now = next;
+      int now = 0;
+      for (int t = 0; t < n_it; ++t) {
+        __syncthreads();   // the step is in its buffer; everybody is done with the other one
+        const int next = kStep - now, s = mine + TW * t;
+        const bool on = works(s);
+        f16v sc = {};
+        if (on) scores(now, sc);
+        put_keys(next);
+        keys.load();
+        if (on) attend(now, s, sc);
+        put_values(next, s + TW);
+        values.load();
+        now = next;
+      }
     }
   };
-  each_tier<BF, QUANT>(a, w, run);
+  each_tier<BF, QUANT>(a, w, r, o, qf, run);
   finish(a, w, r, o, s_tile, s_m, s_l);
 }
 
@@ -440,44 +481,45 @@ __device__ __forceinline__ void interleave() {
 // Bound: the matrix cores and the vector unit alike.  The steps overlap inside a wave: while the softmax of step s runs on the vector
 // unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  LDS holds two steps' keys and values (s + 1 and
 // s + 2; s - 1 and s), one barrier per step.
-template <bool BF, bool QUANT, int RW, int TW>
+template <bool BF, bool QUANT, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
-  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kParts = QUANT ? 2 : 1, kTeam = 2 * kParts * (kKeys + kValues);
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = QUANT ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 2 * (kPartsK * kKeys + kPartsV * kValues);
   __shared__ __align__(16) char s_tile[TW * kTeam];              // per team: keys of even and odd steps, values of even and odd steps
   __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
   __shared__ Wild s_wild[TW];
   const Share<RW, TW> w(a);
   u32x4 qf[8];
-  ChunkRows r = begin_chunk_rows<BF>(a, w.it, w.total, w.row0 + w.c, w.hh, qf);
+  ChunkRows r = begin_chunk_rows(a, w.it, w.total, w.row0 + w.c);
   f16v o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] = f16v{};
-  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 2 * kParts * kKeys;
+  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 2 * kPartsK * kKeys;
   const char *const k_at = team + k_lane(w.lane), *const v_at = team_v + v_lane(w.lane);
 
   auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
     constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
-    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF);
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF) && V2, BT = BF && !is_quant(KF);   // the product's type: quantized tiers in fp16
     const int mine = lo + w.tw;
-    const Place from(tv, seq, w.it.hkv, T.tok + 32 * (mine < hi ? mine : lo));
-    Stream<KF, RW, TW> keys(from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
-    Stream<VF, RW, TW> values(from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    const Ring ring(tv, seq, w.it.hkv);
+    const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
     const int seen_by_all = min(w.first_sees - ahead, T.len), seen = w.idle ? 0 : min(32 * hi, w.last_sees - ahead);   // by the wave's rows
     const int lim = min(r.pos + 1 - ahead, T.len);
-    auto put_keys = [&](int odd) __attribute__((always_inline)) { keys.template put<BF>(team + odd * kParts * kKeys, kRowK, kKeys); };
+    auto put_keys = [&](int odd) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + odd * kPartsK * kKeys, kRowK, kKeys); };
     Wild &wild = s_wild[w.tw];
     auto put_values = [&](int odd, int step) __attribute__((always_inline)) {
-      values.template put_values<BF>(team_v + odd * kParts * kValues, kValues, step, w.tile_sees - ahead, wild, odd);
+      values.template put_values<BT, two_v>(team_v + odd * kPartsV * kValues, kValues, step, w.tile_sees - ahead, wild, odd);
     };
     auto score = [&](f16v &x, int odd, int kb) __attribute__((always_inline)) {
-      const char *const k = k_at + odd * kParts * kKeys + 32 * kb;
-      x = mma<BF>(*(const u32x4 *)k, qf[kb], x);
-      if constexpr (two_k) x = mma<BF>(*(const u32x4 *)(k + kKeys), qf[kb], x);
+      const char *const k = k_at + odd * kPartsK * kKeys + 32 * kb;
+      x = mma<BT>(*(const u32x4 *)k, qf[kb], x);
+      if constexpr (two_k) x = mma<BT>(*(const u32x4 *)(k + kKeys), qf[kb], x);
     };
     auto value = [&](int odd, int d, int b, const u32x4 (&p)[2]) __attribute__((always_inline)) {
-      const char *const v = v_at + odd * kParts * kValues;
-      o[d] = mma<BF>(value_operand(v, d, b), p[b], o[d]);
-      if constexpr (two_v) o[d] = mma<BF>(value_operand(v + kValues, d, b), p[b], o[d]);
+      const char *const v = v_at + odd * kPartsV * kValues;
+      o[d] = mma<BT>(value_operand(v, d, b), p[b], o[d]);
+      if constexpr (two_v) o[d] = mma<BT>(value_operand(v + kValues, d, b), p[b], o[d]);
     };
     // The weights of step s meet its values, by themselves.
     auto flush = [&](int odd, const u32x4 (&p)[2]) __attribute__((always_inline)) {
@@ -501,7 +543,7 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
       if (moves || !works) {
         if (pending) flush(1 - ODD, p);
         p[0] = p[1] = u32x4{0, 0, 0, 0};
-        if (moves) move_chunk_reference<BF>(r, mt, o);
+        if (moves) move_chunk_reference<BT>(r, mt, o);
       }
       put_keys(ODD);
       put_values(ODD, s);
@@ -513,7 +555,7 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
         for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
           value(1 - ODD, g / 2, g % 2, p);
           score(nx, 1 - ODD, g);
-          weigh2<BF>(r, sc, g, pn);
+          weigh2<BT>(r, sc, g, pn);
         }
         // (kept here: the weights are wanted in the next step only, and would be worked out there, behind the products)
         asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(r.l));
@@ -527,7 +569,7 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
     p0[0] = p0[1] = u32x4{0, 0, 0, 0};
     __syncthreads();   // everybody is done with the tier before
     // there is no step before the first: weights of zero meet zeros
-    for (int i = w.tid; i < kParts * kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + kParts * kValues))[i] = u32x4{0, 0, 0, 0};
+    for (int i = w.tid; i < kPartsV * kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + kPartsV * kValues))[i] = u32x4{0, 0, 0, 0};
     if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
     keys.load();
     put_keys(0);
@@ -552,7 +594,7 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
       flush(1, p0);
     }
   };
-  each_tier<BF, QUANT>(a, w, run);
+  each_tier<BF, QUANT>(a, w, r, o, qf, run);
   finish(a, w, r, o, s_tile, s_m, s_l);
 }
 
@@ -584,26 +626,29 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int
   if (a.lse && lane == 0) a.lse[((int64_t)entry * a.n_tokens + token) * a.Hq + hq] = l == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(l) + top) * kLn2;
 }
 
-template <bool BF, bool QUANT>
+template <bool BF, bool QUANT, bool V2>
 void start(const ChunkArgs &a, int rows, hipStream_t s) {
   const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv);
-  if (rows == 256) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, 8, 1>), grid, dim3(512), 0, s, a);
-  else if (rows == 128) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, 4, 2>), grid, dim3(512), 0, s, a);
-  else if constexpr (!QUANT) hipLaunchKernelGGL((chunk_kernel<BF, QUANT, 2, 4>), grid, dim3(512), 0, s, a);
+  if (rows == 256) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, V2, 8, 1>), grid, dim3(512), 0, s, a);
+  else if (rows == 128) hipLaunchKernelGGL((chunk_rows_kernel<BF, QUANT, V2, 4, 2>), grid, dim3(512), 0, s, a);
+  else if constexpr (QUANT) hipLaunchKernelGGL((chunk_kernel<BF, QUANT, V2, 2, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((chunk_kernel<BF, QUANT, V2, 2, 4>), grid, dim3(512), 0, s, a);
 }
 
 }  // namespace
 
 ChunkShape chunk_shape(int64_t most_rows, bool bf, bool quantized) {
-  return ChunkShape{most_rows <= 64 && !quantized ? 64 : most_rows <= 128 ? 128 : 256, bf, quantized};
+  return ChunkShape{most_rows <= 64 ? 64 : most_rows <= 128 ? 128 : 256, bf, quantized};
 }
 
 int64_t chunk_least_steps(const ChunkShape &s) { return s.rows == 256 ? 4 : s.rows == 128 ? 8 : 8; }
-int64_t chunk_resident(const ChunkShape &) { return 256; }
+int64_t chunk_resident(const ChunkShape &s) { return s.rows == 64 && s.quantized ? 512 : 256; }
 
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream) {
-  if (s.bf) s.quantized ? start<true, true>(a, s.rows, stream) : start<true, false>(a, s.rows, stream);
-  else s.quantized ? start<false, true>(a, s.rows, stream) : start<false, false>(a, s.rows, stream);
+  const bool fine = a.out_fmt == TTKV_F16;
+  if (!s.quantized) s.bf ? start<true, false, false>(a, s.rows, stream) : start<false, false, false>(a, s.rows, stream);
+  else if (s.bf) fine ? start<true, true, true>(a, s.rows, stream) : start<true, true, false>(a, s.rows, stream);
+  else fine ? start<false, true, true>(a, s.rows, stream) : start<false, true, false>(a, s.rows, stream);
   return hipGetLastError();
 }
 

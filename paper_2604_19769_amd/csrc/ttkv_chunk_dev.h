@@ -10,6 +10,8 @@ namespace chunk {
 using namespace dev;
 using namespace shared;
 
+constexpr bool is_quant(int f) { return f != TTKV_F16 && f != TTKV_BF16; }
+
 template <int N>
 using num = std::integral_constant<int, N>;
 
@@ -46,21 +48,6 @@ __device__ __forceinline__ Piece<F> load_piece(uint64_t codes, uint64_t meta, in
   }
   return x;
 }
-// v as the nearest number of the product's type and what that leaves.  fp16's first number ends at 65504: the second one has the rest.
-template <bool BF>
-__device__ __forceinline__ void two_parts(const float (&v)[8], u32x4 &hi, u32x4 &lo) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x = v[2 * i], y = v[2 * i + 1];
-    if constexpr (!BF) {
-      x = __builtin_amdgcn_fmed3f(x, -65504.0f, 65504.0f);
-      y = __builtin_amdgcn_fmed3f(y, -65504.0f, 65504.0f);
-    }
-    hi[i] = pack2<BF>(x, y);
-    const f2 h = unpack2<BF>(hi[i]);
-    lo[i] = pack2<BF>(v[2 * i] - h.x, v[2 * i + 1] - h.y);
-  }
-}
 // Which of eight numbers are infinite or none, a bit each; they become 0.
 template <bool BF>
 __device__ __forceinline__ uint32_t take_wild(u32x4 &w) {
@@ -74,30 +61,75 @@ __device__ __forceinline__ uint32_t take_wild(u32x4 &w) {
   }
   return bits;
 }
-// Eight decompressed channels as two numbers each.
-template <bool BF, int F>
+// Eight decompressed channels as fp16 numbers and what those leave (22 bits; the first ones end at 65504, the others have the rest).  Codes
+// are written into the mantissa of 1024 and are exact; code x scale (+ zero) in packed fp16 is rounded once, and the remainder comes from fused
+// steps in fp32.
+template <int F, bool TWO>
 __device__ __forceinline__ void unpack_piece(const Piece<F> &x, u32x4 &hi, u32x4 &lo) {
-  float v[8];
+  h2 s2, z2 = {};
+  uint32_t n[4];
+  bool beyond;   // some value may
   if constexpr (F == TTKV_I8_SYM_G32) {
-    const float s = h2f(x.s);
+    const _Float16 s = __builtin_bit_cast(_Float16, x.s);
+    s2 = h2{s, s};
+    beyond = !(fabsf((float)s) < 515.0f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)((int)(x.w[i / 4] << (24 - 8 * (i % 4))) >> 24) * s;
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w = x.w[i] ^ 0x80808080u;                                // code + 128
+      n[2 * i] = __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u);          // 1024 + that, two at a time
+      n[2 * i + 1] = __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n[i] = __builtin_bit_cast(uint32_t, as_h2(n[i]) - h2{(_Float16)1152, (_Float16)1152});
   } else {
-    const float s = (float)as_h2(x.sz).x, z = (float)as_h2(x.sz).y;
+    const h2 sz = as_h2(x.sz);
+    s2 = h2{sz.x, sz.x};
+    z2 = h2{sz.y, sz.y};
+    beyond = !(fmaf(15.0f, fabsf((float)sz.x), fabsf((float)sz.y)) < 65504.0f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf((float)(x.w >> (4 * i) & 15u), s, z);
+    for (int i = 0; i < 4; ++i) {                                             // nibbles 2 i and 2 i + 1
+      const uint32_t w = x.w >> (8 * i);
+      n[i] = __builtin_bit_cast(uint32_t, as_h2((w & 15u) | (w << 12 & 0xf0000u) | 0x64006400u) - h2{(_Float16)1024, (_Float16)1024});
+    }
   }
-  two_parts<BF>(v, hi, lo);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    h2 h;
+    if constexpr (F == TTKV_I8_SYM_G32) h = as_h2(n[i]) * s2;
+    else h = __builtin_elementwise_fma(as_h2(n[i]), s2, z2);
+    hi[i] = __builtin_bit_cast(uint32_t, h);
+  }
+  if (__any(beyond)) {
+    auto end = [](_Float16 v) { return v != v ? v : (_Float16)fminf(fmaxf((float)v, -65504.0f), 65504.0f); };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[i] = __builtin_bit_cast(uint32_t, h2{end(as_h2(hi[i]).x), end(as_h2(hi[i]).y)});
+  }
+  if constexpr (TWO) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float m1 = minus_one(), s = (float)s2.x;
+      float a, b;
+      if constexpr (F == TTKV_I8_SYM_G32) {
+        a = fmaf((float)as_h2(n[i]).x, s, -(float)as_h2(hi[i]).x);
+        b = fmaf((float)as_h2(n[i]).y, s, -(float)as_h2(hi[i]).y);
+      } else {
+        a = fmaf((float)as_h2(n[i]).x, s, fmaf((float)as_h2(hi[i]).x, m1, (float)z2.x));
+        b = fmaf((float)as_h2(n[i]).y, s, fmaf((float)as_h2(hi[i]).y, m1, (float)z2.x));
+      }
+      lo[i] = pack2<false>(a, b);
+    }
+  }
 }
-template <bool BF, int F, bool CHECK = false>
+template <bool BF, int F, bool TWO, bool CHECK = false>
 __device__ __forceinline__ uint32_t put_piece(const Piece<F> &x, char *hi, char *lo) {
   uint32_t wild = 0;
-  if constexpr (F == TTKV_I8_SYM_G32 || F == TTKV_I4_ASYM_G64) {
+  if constexpr (is_quant(F)) {
     u32x4 h, l;
-    unpack_piece<BF, F>(x, h, l);
-    if constexpr (CHECK) wild = take_wild<BF>(h) | take_wild<BF>(l);
+    unpack_piece<F, TWO>(x, h, l);
+    if constexpr (CHECK) wild = take_wild<false>(h);
+    if constexpr (CHECK && TWO) wild |= take_wild<false>(l);
     *(u32x4 *)hi = h;
-    *(u32x4 *)lo = l;
+    if constexpr (TWO) *(u32x4 *)lo = l;
   } else {
     u32x4 h = x.w;
     if constexpr (CHECK) wild = take_wild<BF>(h);
@@ -120,44 +152,50 @@ template <typename A>
 __device__ __forceinline__ int token_of(const A &a, int row) {
   return a.G == 1 ? row : a.g_magic ? (int)mul_high((uint32_t)row, a.g_magic) : row / a.G;
 }
-// A place in a run, kept in scalar registers: the KV head's part of a ring block, and a row of it.
-struct Place {
-  uint64_t base, head, table;
+// A KV head's part of a sequence's ring, in scalar registers, and places in it.
+struct Ring {
+  uint64_t base, table;
   int64_t rec_bytes;
-  int bt, ring_blocks, block, row, seq;
-  __device__ __forceinline__ int64_t record() const { return table ? (int64_t)((const_i32)table)[block] : (int64_t)seq * ring_blocks + block; }
-  __device__ __forceinline__ void find() { head = base + (table ? (int64_t)((const_i32)table)[block] : (int64_t)block) * rec_bytes; }
-  __device__ __forceinline__ Place(const TierView &tv, int seq_, int hkv, int tok) {
-    seq = seq_;
+  int bt, blocks;
+  __device__ __forceinline__ Ring(const TierView &tv, int seq, int hkv) {
     bt = tv.bt;
-    ring_blocks = tv.ring_blocks;
+    blocks = tv.ring_blocks;
     rec_bytes = tv.rec_bytes;
     table = (uint64_t)tv.table;
     base = (uint64_t)tv.base + (int64_t)hkv * tv.head_bytes;
-    if (table) table += (uint64_t)((int64_t)seq * ring_blocks) * 4;
-    else base += (uint64_t)((int64_t)seq * ring_blocks * rec_bytes);
-    if (tok >= ring_blocks * bt) tok -= ring_blocks * bt;
-    block = div_bt(tok, bt, tv.bt_magic);
-    row = tok - block * bt;
-    asm volatile("" : "+s"(bt), "+s"(ring_blocks), "+s"(rec_bytes), "+s"(table), "+s"(base));
-    find();
-  }
-  __device__ __forceinline__ void advance(int rows) {
-    row += rows;
-    if (row < bt) return;
-    do {
-      row -= bt;
-      block = block + 1 == ring_blocks ? 0 : block + 1;
-    } while (row >= bt);
-    find();
+    if (table) table += (uint64_t)((int64_t)seq * blocks) * 4;
+    else base += (uint64_t)((int64_t)seq * blocks * rec_bytes);
+    asm volatile("" : "+s"(bt), "+s"(blocks), "+s"(rec_bytes), "+s"(table), "+s"(base));
   }
 };
-
+struct Place {
+  uint64_t head;   // the block's part of the KV head
+  int block, row;
+  __device__ __forceinline__ void find(const Ring &g) {
+    head = g.base + (g.table ? (int64_t)((const_i32)g.table)[block] : (int64_t)block) * g.rec_bytes;
+  }
+  __device__ __forceinline__ Place(const Ring &g, uint32_t magic, int tok) {
+    if (tok >= g.blocks * g.bt) tok -= g.blocks * g.bt;
+    block = div_bt(tok, g.bt, magic);
+    row = tok - block * g.bt;
+    find(g);
+  }
+  __device__ __forceinline__ void advance(const Ring &g, int rows) {
+    row += rows;
+    if (row < g.bt) return;
+    do {
+      row -= g.bt;
+      block = block + 1 == g.blocks ? 0 : block + 1;
+    } while (row >= g.bt);
+    find(g);
+  }
+};
 // Tokens from `lim` on count nothing; lim by lane.
 __device__ __forceinline__ void mask_from(f16v &sc, int lim, int hh) {
+  const int left = lim - 4 * hh;   // (against numbers that an instruction holds)
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    if (8 * (i / 4) + 4 * hh + i % 4 >= lim) sc[i] = -INFINITY;
+    if (8 * (i / 4) + i % 4 >= left) sc[i] = -INFINITY;
     asm volatile("" : "+v"(sc[i]));   // stays a branch, not sixteen selects in every step
   }
 }

@@ -423,7 +423,7 @@ struct WeighArgs {
   int32_t entry[TTKV_MAX_BATCH];
 };
 static_assert(sizeof(WeighArgs) <= 4096, "kernel arguments are passed by value");
-hipError_t launch_weigh(const WeighArgs &a, bool bf, hipStream_t s);
+hipError_t launch_weigh(const WeighArgs &a, hipStream_t s);
 
 // The lightest tokens of a tier leave their places to tokens of its oldest blocks (light_select_kernel, light_move_kernel).
 struct LightArgs {

@@ -19,7 +19,7 @@ using namespace chunk;
 constexpr int kWaves = 4, kTokens = 64 * kWaves;   // of a workgroup
 template <bool BF, int KF>
 __global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a) {
-  constexpr bool two = KF != TTKV_F16 && KF != TTKV_BF16;
+  constexpr bool two = is_quant(KF);
   __shared__ __align__(16) char s_q[2][32 * kRowK];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hh = lane >> 5;
   const uint32_t id = blockIdx.x;
@@ -29,7 +29,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a
   const int entry = a.entry[slot], seq = a.first_seq + entry, rows = a.count[slot] * a.G, sees = a.sees[slot], len = a.len[slot];
   const int tile = (item - a.first_item[slot]) * kTokens, t0 = tile + 64 * wave;
   const bool idle = t0 >= len;
-  const Place at(a.tv, seq, hkv, a.first_tok[slot] + (idle ? tile : t0));
+  const Ring ring(a.tv, seq, hkv);
+  const Place at(ring, a.tv.bt_magic, a.first_tok[slot] + (idle ? tile : t0));
   // keys as left operands: lane -> token 32 g + c, channels 16 kb + 8 hh .. + 7
   u32x4 kf[2][8], kl[two ? 2 : 1][two ? 8 : 1];
   const int last = max(min(63, len - t0 - 1), 0);
@@ -38,7 +39,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb) {
       const Piece<KF> x = load_piece<KF>(at.head, at.head + a.tv.k_meta_off, at.row + min(32 * g + c, last), 2 * kb + hh);
-      if constexpr (two) unpack_piece<BF, KF>(x, kf[g][kb], kl[g][kb]);
+      if constexpr (two) unpack_piece<KF, true>(x, kf[g][kb], kl[g][kb]);
       else kf[g][kb] = x.w;
     }
   float acc[2][16];
@@ -116,7 +117,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a
   for (int g = 0; g < 2; ++g) {
     const int t = 32 * g + 8 * (c / 4) + 4 * hh + c % 4;
     if (t0 + t >= len) continue;
-    float *const w = a.weights + ((int64_t)at.record() * a.Hkv + hkv) * a.tv.bt + at.row + t;
+    const int64_t r = (int64_t)seq * ring.blocks + at.block, rec = a.tv.table ? (int64_t)a.tv.table[r] : r;
+    float *const w = a.weights + (rec * a.Hkv + hkv) * ring.bt + at.row + t;
     *w = t0 + t >= a.first_fresh[slot] ? mine[g] : *w + mine[g];
   }
 }
@@ -262,18 +264,13 @@ __global__ __launch_bounds__(256) void light_move_kernel(const LightArgs a) {
 
 }  // namespace
 
-hipError_t launch_weigh(const WeighArgs &a, bool bf, hipStream_t s) {
+hipError_t launch_weigh(const WeighArgs &a, hipStream_t s) {
   const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv), block(64 * kWaves);
   switch (a.tv.k_fmt) {
     case TTKV_F16: hipLaunchKernelGGL((weigh_kernel<false, TTKV_F16>), grid, block, 0, s, a); break;
     case TTKV_BF16: hipLaunchKernelGGL((weigh_kernel<true, TTKV_BF16>), grid, block, 0, s, a); break;
-    case TTKV_I8_SYM_G32:
-      if (bf) hipLaunchKernelGGL((weigh_kernel<true, TTKV_I8_SYM_G32>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((weigh_kernel<false, TTKV_I8_SYM_G32>), grid, block, 0, s, a);
-      break;
-    default:
-      if (bf) hipLaunchKernelGGL((weigh_kernel<true, TTKV_I4_ASYM_G64>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((weigh_kernel<false, TTKV_I4_ASYM_G64>), grid, block, 0, s, a);
+    case TTKV_I8_SYM_G32: hipLaunchKernelGGL((weigh_kernel<false, TTKV_I8_SYM_G32>), grid, block, 0, s, a); break;
+    default: hipLaunchKernelGGL((weigh_kernel<false, TTKV_I4_ASYM_G64>), grid, block, 0, s, a);
   }
   return hipGetLastError();
 }

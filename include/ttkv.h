@@ -435,9 +435,13 @@ size_t ttkv_chunk_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t se
  *   q, seq, n_tokens, n_each as in ttkv_chunk_attn: queries of the newest tokens (those of the step just made: n_tokens 1).
  *   n_fresh [host] per entry: so many of the sequence's newest tokens begin at 0, whatever their places hold (NULL: the chunk's own).
  *   weights [device] fp32 [pool_blocks][n_kv_heads][block_tokens], beside the tier's records.
+ *   workspace [device], ttkv_weights_workspace_bytes (0: invalid arguments): partial sums, where many rows meet few tokens.
  * Tiers in device memory whose keys are fp16, bf16, int8 or int4 (UNSUPPORTED otherwise).  The order of each sum is fixed. */
 ttkv_status ttkv_add_weights(ttkv_handle h, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse,
-                             int64_t n_tokens, const int64_t *n_each, const int64_t *n_fresh, float *weights, void *stream);
+                             int64_t n_tokens, const int64_t *n_each, const int64_t *n_fresh, float *weights, void *workspace,
+                             size_t ws_bytes, void *stream);
+size_t ttkv_weights_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t tier, int32_t seq, int64_t n_tokens, const int64_t *n_each,
+                                    const int64_t *n_fresh);
 
 /* Eviction by weight: a tier's oldest blocks are freed, as many as leave each sequence at least `keep` tokens (whole blocks: fewer
  * than block_tokens more), and per KV head the lightest tokens go.  The `recent` <= keep newest tokens stay whatever their weights (the others'

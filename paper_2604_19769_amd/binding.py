@@ -63,7 +63,8 @@ EXPORTS = [
     "ttkv_merge_partials", "ttkv_select_blocks", "ttkv_set_split", "ttkv_set_table_check",
     "ttkv_norm_rope", "ttkv_rope_append", "ttkv_shared_attn", "ttkv_shared_workspace_bytes", "ttkv_prefix_parts",
     "ttkv_decode_step_shared",
-    "ttkv_chunk_attn", "ttkv_chunk_workspace_bytes", "ttkv_add_weights", "ttkv_evict_light", "ttkv_evict_light_workspace_bytes",
+    "ttkv_chunk_attn", "ttkv_chunk_workspace_bytes", "ttkv_add_weights", "ttkv_weights_workspace_bytes",
+    "ttkv_evict_light", "ttkv_evict_light_workspace_bytes",
 ]
 # include/ttkv_bench.h: measurement and inspection aids, not part of the boundary
 BENCH_EXPORTS = ["ttkv_time_attn", "ttkv_time_attn_repeat", "ttkv_read_attn_timing", "ttkv_stream_read", "ttkv_staged_schedule"]
@@ -135,7 +136,9 @@ def lib():
         L.ttkv_chunk_attn.argtypes = [p, cp, i32, cp, p, hp, hp, p, i64, p, p, sz, p]
         L.ttkv_chunk_workspace_bytes.argtypes = [p, cp, i32, cp, p, i64, p]
         L.ttkv_chunk_workspace_bytes.restype = sz
-        L.ttkv_add_weights.argtypes = [p, cp, i32, i32, hp, p, i64, p, p, p, p]
+        L.ttkv_add_weights.argtypes = [p, cp, i32, i32, hp, p, i64, p, p, p, p, sz, p]
+        L.ttkv_weights_workspace_bytes.argtypes = [p, cp, i32, i32, i64, p, p]
+        L.ttkv_weights_workspace_bytes.restype = sz
         L.ttkv_evict_light.argtypes = [p, cp, i32, i64, i64, i32, p, p, sz, p]
         L.ttkv_evict_light_workspace_bytes.argtypes = [p, cp, i32, i64, i64]
         L.ttkv_evict_light_workspace_bytes.restype = sz
@@ -149,7 +152,7 @@ def lib():
             if name not in ("ttkv_get_stats", "ttkv_reset_stats", "ttkv_status_string", "ttkv_record_bytes",
                             "ttkv_workspace_bytes", "ttkv_demote_workspace_bytes",
                             "ttkv_append_host_workspace_bytes", "ttkv_shared_workspace_bytes", "ttkv_chunk_workspace_bytes",
-                            "ttkv_evict_light_workspace_bytes", "ttkv_count_parts"):
+                            "ttkv_evict_light_workspace_bytes", "ttkv_weights_workspace_bytes", "ttkv_count_parts"):
                 f.restype = i32
         _lib = L
     return _lib
@@ -326,9 +329,13 @@ def ttkv_chunk_workspace_bytes(h, cache, seq, prefix, member, n_tokens, n_each):
     return lib().ttkv_chunk_workspace_bytes(h, C.byref(cache), seq, _ref(prefix), _p(member), n_tokens, _p(n_each))
 
 
-def ttkv_add_weights(h, cache, tier, seq, q, lse, n_tokens, n_each, n_fresh, weights, stream):
-    _check(lib().ttkv_add_weights(h, C.byref(cache), tier, seq, _ref(q), _p(lse), n_tokens, _p(n_each), _p(n_fresh), _p(weights), _p(stream)),
-           "ttkv_add_weights")
+def ttkv_add_weights(h, cache, tier, seq, q, lse, n_tokens, n_each, n_fresh, weights, workspace, ws_bytes, stream):
+    _check(lib().ttkv_add_weights(h, C.byref(cache), tier, seq, _ref(q), _p(lse), n_tokens, _p(n_each), _p(n_fresh), _p(weights), _p(workspace),
+                                  ws_bytes, _p(stream)), "ttkv_add_weights")
+
+
+def ttkv_weights_workspace_bytes(h, cache, tier, seq, n_tokens, n_each, n_fresh):
+    return lib().ttkv_weights_workspace_bytes(h, C.byref(cache), tier, seq, n_tokens, _p(n_each), _p(n_fresh))
 
 
 def ttkv_evict_light(h, cache, tier, keep, recent, swap, weights, workspace, ws_bytes, stream):

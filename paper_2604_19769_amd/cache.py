@@ -533,8 +533,9 @@ class TieredCache:
         if fresh is None:
             newer = sum((x[rows] for x in self.len[:tier]), np.zeros(n, np.int64))
             fresh = np.maximum(0, end - self._weighed[tier][rows]) + newer
-        B.ttkv_add_weights(self.h, self.c, tier, seq, _heads(q, (n, T, self.Hq, 128), self.device), lse, T, _host_int64(counts, n),
-                           _host_int64(fresh, n), self.weights[tier], self._compute())
+        qv, each, begin, stream = _heads(q, (n, T, self.Hq, 128), self.device), _host_int64(counts, n), _host_int64(fresh, n), self._compute()
+        self._with_workspace("weights", lambda ws, size: B.ttkv_add_weights(self.h, self.c, tier, seq, qv, lse, T, each, begin, self.weights[tier], ws, size, stream),
+                             lambda: B.ttkv_weights_workspace_bytes(self.h, self.c, tier, seq, T, each, begin))
         self._weighed[tier][rows] = end
 
     @_on_own_device

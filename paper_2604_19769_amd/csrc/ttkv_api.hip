@@ -1853,38 +1853,33 @@ ttkv_status ttkv_chunk_attn(ttkv_handle hh, const ttkv_cache *c, int32_t seq, co
 }
 
 // ---------------------------------------------------------------- weights and what they decide
-ttkv_status ttkv_add_weights(ttkv_handle hh, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse, int64_t n_tokens,
-                             const int64_t *n_each, const int64_t *n_fresh, float *weights, void *stream) {
-  Handle *h = reinterpret_cast<Handle *>(hh);
-  if (!h || !q) return TTKV_ERR_INVALID_ARG;
-  ttkv_status st = validate_cache(c, h->check_tables);
+namespace {
+struct WeighPlan {
+  WeighArgs a;
+  int n_slots;
+  int64_t most_rows, queries;
+  size_t ws_bytes;
+};
+ttkv_status plan_weigh(const ttkv_cache *c, bool check_tables, int32_t tier, int32_t seq, int64_t n_tokens, const int64_t *n_each,
+                       const int64_t *n_fresh, WeighPlan &P) {
+  ttkv_status st = validate_cache(c, check_tables);
   if (st != TTKV_OK) return st;
-  if (tier < 0 || tier >= c->n_tiers || seq < -1 || seq >= c->batch || n_tokens < 0 || !weights) return TTKV_ERR_INVALID_ARG;
+  if (tier < 0 || tier >= c->n_tiers || seq < -1 || seq >= c->batch || n_tokens < 0) return TTKV_ERR_INVALID_ARG;
   if (n_tokens > TTKV_MAX_CHUNK_TOKENS) return TTKV_ERR_UNSUPPORTED;
   const ttkv_tier &T = c->tier[tier];
   if (T.mem != TTKV_MEM_DEVICE || !(is_fp(T.k_fmt) || T.k_fmt == TTKV_I8_SYM_G32 || T.k_fmt == TTKV_I4_ASYM_G64)) return TTKV_ERR_UNSUPPORTED;
-  if (q->fmt != TTKV_F16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;
-  if (T.k_fmt == TTKV_BF16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
   const int b0 = seq < 0 ? 0 : seq, n_seq = seq < 0 ? c->batch : 1;
-  WeighArgs a{};
-  int64_t s[3];
-  uint8_t *data = nullptr;
-  if ((st = read_heads(q, n_seq, n_tokens, false, s, &data)) != TTKV_OK) return st;
-  if (q->n_heads != c->n_q_heads) return TTKV_ERR_INVALID_ARG;
-  a.q = data;
-  a.q_seq = s[0]; a.q_token = s[1]; a.q_head = s[2];
-  a.q_fmt = q->fmt;
+  WeighArgs &a = P.a;
   a.Hq = c->n_q_heads;
   a.Hkv = c->n_kv_heads;
   a.G = a.Hq / a.Hkv;
   a.scale = c->softmax_scale;
   a.first_seq = b0;
   a.n_tokens = (int32_t)n_tokens;
-  a.lse = lse;
-  a.weights = weights;
   a.tv = make_view(T, make_layout(T, c->n_kv_heads));
-  int n_slots = 0;
-  int64_t items = 0, most_rows = 0, queries = 0;
+  int64_t tiles = 0;
+  P.n_slots = 0;
+  P.most_rows = P.queries = 0;
   for (int j = 0; j < n_seq; ++j) {
     const int b = b0 + j;
     const int64_t n = n_each ? n_each[j] : n_tokens, fresh = n_fresh ? n_fresh[j] : n;
@@ -1892,30 +1887,75 @@ ttkv_status ttkv_add_weights(ttkv_handle hh, const ttkv_cache *c, int32_t tier, 
     const int64_t total = held_tokens(c, b);
     int64_t before = 0;   // tokens of older tiers
     for (int t = tier + 1; t < c->n_tiers; ++t) before += c->tier[t].len[b];
-    queries += n;
-    if (T.len[b] == 0 || (n == 0 && (n_fresh ? fresh : 0) == 0)) continue;
-    a.first_item[n_slots] = (int32_t)items;
-    a.count[n_slots] = (int32_t)n;
-    a.sees[n_slots] = (int32_t)std::max<int64_t>(std::min<int64_t>(total - n + 1 - before, 1ll << 30), -(1ll << 30));
-    a.first_tok[n_slots] = (int32_t)(T.start[b] % ring_tokens(T));
-    a.len[n_slots] = (int32_t)T.len[b];
-    // tokens newer than the tier's own count as new, too
-    const int64_t newer = total - before - T.len[b];
-    a.first_fresh[n_slots] = (int32_t)(T.len[b] - std::min(T.len[b], std::max<int64_t>(0, fresh - newer)));
-    a.entry[n_slots] = j;
-    ++n_slots;
-    items += (T.len[b] + 255) / 256;
-    most_rows = std::max(most_rows, n * a.G);
+    P.queries += n;
+    if (T.len[b] == 0 || (n == 0 && fresh == 0)) continue;
+    const int i = P.n_slots++;
+    a.count[i] = (int32_t)n;
+    a.sees[i] = (int32_t)std::max<int64_t>(std::min<int64_t>(total - n + 1 - before, 1ll << 30), -(1ll << 30));
+    a.first_tok[i] = (int32_t)(T.start[b] % ring_tokens(T));
+    a.len[i] = (int32_t)T.len[b];
+    const int64_t newer = total - before - T.len[b];   // of newer tiers: the newest tokens
+    a.first_fresh[i] = (int32_t)(T.len[b] - std::min(T.len[b], std::max<int64_t>(0, fresh - newer)));
+    a.entry[i] = j;
+    tiles += (T.len[b] + 255) / 256;
+    P.most_rows = std::max(P.most_rows, n * a.G);
   }
-  if (n_slots == 0) return TTKV_OK;
-  if (queries && !lse) return TTKV_ERR_INVALID_ARG;
-  if (most_rows >= 1ll << 28 || items * a.Hkv >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;
-  for (int i = n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = INT32_MAX;
+  P.ws_bytes = 0;
+  if (P.n_slots == 0) return TTKV_OK;
+  if (P.most_rows >= 1ll << 28) return TTKV_ERR_UNSUPPORTED;
+  weigh_shape(P.most_rows, tiles, a.Hkv, T.k_fmt, a.chunk, a.n_split);
+  int64_t items = 0;
+  for (int i = 0; i < P.n_slots; ++i) {
+    a.first_item[i] = (int32_t)items;
+    items += (a.len[i] + a.chunk - 1) / a.chunk;
+  }
+  for (int i = P.n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = INT32_MAX;
+  if (items * a.Hkv * a.n_split >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;   // a launch has 2^32 threads at most
   a.n_items = (int32_t)items;
+  a.n_sums = items * a.chunk;
   a.hkv_magic = a.Hkv > 1 && items * a.Hkv * a.Hkv < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.Hkv - 1) / a.Hkv) : 0;
-  a.g_magic = a.G > 1 && most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
-  TTKV_HIP(h, launch_weigh(a, (hipStream_t)stream));
-  h->stats.kernels += 1;
+  a.g_magic = a.G > 1 && P.most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
+  if (a.n_split > 1) P.ws_bytes = (size_t)a.n_split * a.Hkv * a.n_sums * sizeof(float);
+  return TTKV_OK;
+}
+}  // namespace
+
+size_t ttkv_weights_workspace_bytes(ttkv_handle hh, const ttkv_cache *c, int32_t tier, int32_t seq, int64_t n_tokens, const int64_t *n_each,
+                                    const int64_t *n_fresh) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  WeighPlan P{};
+  if (!h || plan_weigh(c, h->check_tables, tier, seq, n_tokens, n_each, n_fresh, P) != TTKV_OK) return 0;
+  return align256(P.ws_bytes) + 256;
+}
+
+ttkv_status ttkv_add_weights(ttkv_handle hh, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse, int64_t n_tokens,
+                             const int64_t *n_each, const int64_t *n_fresh, float *weights, void *workspace, size_t ws_bytes, void *stream) {
+  Handle *h = reinterpret_cast<Handle *>(hh);
+  if (!h || !q || !weights) return TTKV_ERR_INVALID_ARG;
+  WeighPlan P{};
+  ttkv_status st = plan_weigh(c, h->check_tables, tier, seq, n_tokens, n_each, n_fresh, P);
+  if (st != TTKV_OK) return st;
+  if (q->fmt != TTKV_F16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;
+  if (c->tier[tier].k_fmt == TTKV_BF16 && q->fmt != TTKV_BF16) return TTKV_ERR_UNSUPPORTED;   // a bf16 tier takes bf16 queries
+  WeighArgs &a = P.a;
+  int64_t s[3];
+  uint8_t *data = nullptr;
+  if ((st = read_heads(q, seq < 0 ? c->batch : 1, n_tokens, false, s, &data)) != TTKV_OK) return st;
+  if (q->n_heads != c->n_q_heads || (P.queries && !lse)) return TTKV_ERR_INVALID_ARG;
+  if (P.n_slots == 0) return TTKV_OK;
+  a.q = data;
+  a.q_seq = s[0]; a.q_token = s[1]; a.q_head = s[2];
+  a.q_fmt = q->fmt;
+  a.lse = lse;
+  a.weights = weights;
+  const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
+  if (P.ws_bytes) {
+    if (!workspace || ws_bytes < mis + P.ws_bytes) return TTKV_ERR_WORKSPACE;
+    a.sums = (float *)((uint8_t *)workspace + mis);
+  }
+  int nk = 0;
+  TTKV_HIP(h, launch_weigh(a, P.most_rows, (hipStream_t)stream, &nk));
+  h->stats.kernels += nk;
   return TTKV_OK;
 }
 

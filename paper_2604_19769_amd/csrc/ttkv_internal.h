@@ -403,19 +403,22 @@ int64_t chunk_resident(const ChunkShape &s);      // workgroups on the chip at o
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
 hipError_t launch_chunk_merge(const ChunkArgs &a, int64_t n_rows, hipStream_t stream);   // rows of all heads
 
-// What the queries of a chunk give each token of one tier (weigh_kernel).
+// What the queries of a chunk give each token of one tier (weigh_kernel and its kin).
 struct WeighArgs {
   int32_t n_items, Hq, Hkv, G;
   uint32_t hkv_magic, g_magic;
   float scale;
   int32_t q_fmt;
   int32_t n_tokens, first_seq;     // lse's rows per entry; sequence of entry 0
+  int32_t chunk, n_split;          // tokens of an item; items that share a tile's rows
   const uint8_t *q;
   const float *lse;
   float *weights;
+  float *sums;                     // n_split > 1: [split][KV head][token], tokens of the slots one behind the other
+  int64_t n_sums;                  // tokens of all slots, each slot's rounded up to whole items
   int64_t q_seq, q_token, q_head;  // bytes
   TierView tv;
-  int32_t first_item[TTKV_MAX_BATCH];   // of the slot, INT32_MAX behind the last
+  int32_t first_item[TTKV_MAX_BATCH];   // of the slot (splits not counted), INT32_MAX behind the last
   int32_t count[TTKV_MAX_BATCH];
   int32_t sees[TTKV_MAX_BATCH];         // tokens of the tier that the slot's first query sees (less than none: below 0)
   int32_t first_tok[TTKV_MAX_BATCH], len[TTKV_MAX_BATCH];
@@ -423,7 +426,10 @@ struct WeighArgs {
   int32_t entry[TTKV_MAX_BATCH];
 };
 static_assert(sizeof(WeighArgs) <= 4096, "kernel arguments are passed by value");
-hipError_t launch_weigh(const WeighArgs &a, hipStream_t s);
+// How a launch is cut: tokens per item and items per tile's rows, for `most_rows` query rows per KV head, `tokens` of all slots (each rounded up to
+// 256) and their rows' steps.
+void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int k_fmt, int32_t &chunk, int32_t &n_split);
+hipError_t launch_weigh(const WeighArgs &a, int64_t most_rows, hipStream_t s, int *n_kernels);
 
 // The lightest tokens of a tier leave their places to tokens of its oldest blocks (light_select_kernel, light_move_kernel).
 struct LightArgs {

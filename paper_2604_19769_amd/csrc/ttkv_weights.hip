@@ -1,7 +1,8 @@
 // What a cache's tokens have been worth: the attention weight that queries give every token of a tier, added up, and the eviction of
 // the tokens that received least.
-#include "ttkv_shared_dev.h"
 #include "ttkv_chunk_dev.h"
+
+#include <algorithm>
 
 namespace ttkv {
 
@@ -13,114 +14,297 @@ using namespace chunk;
 
 // ---------------------------------------------------------------- weights
 // weight[token] += sum over rows that see it of e^(scale q.k - lse): the score product of the chunk's attention with the roles turned.  A
-// wave keeps the keys of 64 tokens in registers and takes the chunk's query rows 32 at a time from LDS; a lane has 16 scores of one row
-// from each 32 tokens, and adds the weights of its rows up by itself until the lanes meet at the end.  No two waves add to one token, so
+// wave keeps the keys of 32 tokens in registers and takes the chunk's query rows 32 at a time from LDS; a lane has 16 scores of one row,
+// and adds the weights of its rows up by itself until the lanes meet at the end.  No two waves add to one place, so
 // the order of a sum is fixed.
-constexpr int kWaves = 4, kTokens = 64 * kWaves;   // of a workgroup
-template <bool BF, int KF>
-__global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a) {
-  constexpr bool two = is_quant(KF);
-  __shared__ __align__(16) char s_q[2][32 * kRowK];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hh = lane >> 5;
-  const uint32_t id = blockIdx.x;
+constexpr int kWaves = 8, kTile = 32 * kWaves;   // tokens that a workgroup's waves take together
+constexpr int kFewRows = 256;
+
+// What an item works on.
+struct WeighItem {
+  int slot, entry, seq, hkv, rows, sees, len, t0, split;   // t0: the item's first token
+};
+__device__ __forceinline__ WeighItem weigh_item(const WeighArgs &a) {
+  // all that the look-ups read, asked for at once: a launch's arguments are in no cache when its first workgroups start
+  asm volatile("" ::"s"(a.Hkv), "s"(a.q), "s"(a.sums), "s"(a.tv.base), "s"(a.tv.bt), "s"(a.first_item[0]), "s"(a.count[0]), "s"(a.sees[0]),
+               "s"(a.first_tok[0]), "s"(a.len[0]), "s"(a.first_fresh[0]), "s"(a.entry[0]));
+  WeighItem w;
+  const int lane = threadIdx.x & 63;
+  uint32_t id = blockIdx.x;
+  w.split = 0;
+  if (a.n_split > 1) {
+    w.split = id % (uint32_t)a.n_split;
+    id /= (uint32_t)a.n_split;
+  }
   const int item = a.Hkv == 1 ? id : a.hkv_magic ? (int)mul_high(id, a.hkv_magic) : (int)(id / (uint32_t)a.Hkv);
-  const int hkv = id - item * a.Hkv;
-  const int slot = __popcll(__ballot(a.first_item[lane] <= item)) - 1;
-  const int entry = a.entry[slot], seq = a.first_seq + entry, rows = a.count[slot] * a.G, sees = a.sees[slot], len = a.len[slot];
-  const int tile = (item - a.first_item[slot]) * kTokens, t0 = tile + 64 * wave;
-  const bool idle = t0 >= len;
-  const Ring ring(a.tv, seq, hkv);
-  const Place at(ring, a.tv.bt_magic, a.first_tok[slot] + (idle ? tile : t0));
-  // keys as left operands: lane -> token 32 g + c, channels 16 kb + 8 hh .. + 7
-  u32x4 kf[2][8], kl[two ? 2 : 1][two ? 8 : 1];
-  const int last = max(min(63, len - t0 - 1), 0);
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
+  w.hkv = id - item * a.Hkv;
+  w.slot = __popcll(__ballot(a.first_item[lane] <= item)) - 1;
+  w.entry = a.entry[w.slot];
+  w.seq = a.first_seq + w.entry;
+  w.rows = a.count[w.slot] * a.G;
+  w.sees = a.sees[w.slot];
+  w.len = a.len[w.slot];
+  w.t0 = (item - a.first_item[w.slot]) * a.chunk;
+  return w;
+}
+// Keys of 32 tokens as left operands: lane -> token c, channels 16 kb + 8 hh .. + 7.
+template <int KF>
+struct Operands {
+  static constexpr bool two = is_quant(KF);
+  u32x4 hi[8], lo[two ? 8 : 1];
+  __device__ __forceinline__ void load(const Place &at, uint32_t meta, int left, int c, int hh) {   // left: live tokens from `at` on
+    const int row = at.row + min(c, left - 1);
 #pragma unroll
     for (int kb = 0; kb < 8; ++kb) {
-      const Piece<KF> x = load_piece<KF>(at.head, at.head + a.tv.k_meta_off, at.row + min(32 * g + c, last), 2 * kb + hh);
-      if constexpr (two) unpack_piece<KF, true>(x, kf[g][kb], kl[g][kb]);
-      else kf[g][kb] = x.w;
+      const Piece<KF> x = load_piece<KF>(at.head, at.head + meta, row, 2 * kb + hh);
+      if constexpr (two) unpack_piece<KF, true>(x, hi[kb], lo[kb]);
+      else hi[kb] = x.w;
     }
-  float acc[2][16];
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[g][i] = 0.0f;
-  const float cs = a.scale * kLog2e;
-  // rows in steps of 32, from the first that sees a token of the tile on
-  const int first_row = max(0, tile - sees + 1) * a.G;
-  const int s0 = min(first_row, rows) / 32, s1 = (rows + 31) / 32;
-  u32x4 qr[2];
-  const int qrow = threadIdx.x >> 4, qp = threadIdx.x & 15;
-  auto load = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int row = min(32 * s + qrow + 16 * i, rows - 1), token = token_of(a, row), hq = hkv * a.G + row - token * a.G;
-      qr[i] = *(const u32x4 *)(a.q + entry * a.q_seq + token * a.q_token + hq * a.q_head + 16 * qp);
-      if (!BF && a.q_fmt == TTKV_BF16) to_fp16(qr[i]);
-    }
-  };
-  auto put = [&](int s) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) *(u32x4 *)(s_q[s & 1] + (qrow + 16 * i) * kRowK + 16 * qp) = qr[i];
-  };
-  if (s0 < s1) {
-    load(s0);
-    put(s0);
-    if (s0 + 1 < s1) load(s0 + 1);
   }
-  for (int s = s0; s < s1; ++s) {
-    __syncthreads();   // the step's rows are there; everybody is done with those of the step before
-    if (s + 1 < s1) {
-      put(s + 1);
-      if (s + 2 < s1) load(s + 2);
+};
+// Scores of 32 rows (right operands at q_at) and the wave's 32 tokens.
+template <bool BF, int KF>
+__device__ __forceinline__ f16v score_rows(const Operands<KF> &k, const char *q_at) {
+  f16v sc = {};
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) {
+    const u32x4 q = *(const u32x4 *)(q_at + 32 * kb);
+    sc = mma<BF>(k.hi[kb], q, sc);
+    if constexpr (is_quant(KF)) sc = mma<BF>(k.lo[kb], q, sc);
+  }
+  return sc;
+}
+// lim: tokens of the wave's that the lane's row sees.
+__device__ __forceinline__ f16v mask_rows(f16v sc, int lim, int hh) {
+  if (!__all(lim >= 32)) mask_from(sc, lim, hh);
+  return sc;
+}
+// Their weights; off: -lse in the log2 domain.
+__device__ __forceinline__ f16v add_rows(f16v acc, const f16v sc, float cs, float off) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) acc[i] += __builtin_amdgcn_exp2f(fmaf(sc[i], cs, off));
+  return acc;
+}
+// The next step's products and this one's exponentials side by side: products of one chain wait for each other, and what stands behind a waiting one waits
+// as well.
+template <bool BF, int KF>
+__device__ __forceinline__ f16v side_by_side(const Operands<KF> &k, const char *q_at, f16v &sums, const f16v now, float cs, float off) {
+  constexpr bool two = is_quant(KF);
+  f16v then = {}, acc = sums;   // (elements are written of local variables only: of ones that a lambda holds they end in scratch)
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) {
+    const u32x4 q = *(const u32x4 *)(q_at + 32 * kb);
+    then = mma<BF>(k.hi[kb], q, then);
+    if constexpr (two) then = mma<BF>(k.lo[kb], q, then);
+    acc[2 * kb] += __builtin_amdgcn_exp2f(fmaf(now[2 * kb], cs, off));
+    acc[2 * kb + 1] += __builtin_amdgcn_exp2f(fmaf(now[2 * kb + 1], cs, off));
+  }
+  asm volatile("" : "+v"(acc));   // (kept here: wanted in the next step only, the sums would be worked out there)
+  __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, two ? 3 : 6, 0);
+    if constexpr (two) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
     }
-    if (idle) continue;
-    const int row = 32 * s + c, token = token_of(a, min(row, rows - 1)), hq = hkv * a.G + min(row, rows - 1) - token * a.G;
-    const float lse = a.lse[((int64_t)entry * a.n_tokens + token) * a.Hq + hq];
-    // tokens of the wave's that the row sees; a row whose log-sum-exp is not finite gives nothing
-    const int lim = row < rows && fabsf(lse) < INFINITY ? min(sees + token, len) - t0 : 0;
-    const float off = fabsf(lse) < INFINITY ? -lse * kLog2e : 0.0f;
-    u32x4 qf[8];
-    const char *const q_at = s_q[s & 1] + k_lane(lane);
+  }
+  sums = acc;
+  return then;
+}
+// Over the 32 lanes of a half; lane c < 16 of half hh then has token 8 (c / 4) + 4 hh + c % 4.
+__device__ __forceinline__ float gather(const f16v &acc, int c) {
+  float mine = 0.0f;
 #pragma unroll
-    for (int kb = 0; kb < 8; ++kb) qf[kb] = *(const u32x4 *)(q_at + 32 * kb);
-    const bool whole = __all(lim >= 64);
+  for (int i = 0; i < 16; ++i) {
+    float v = group_sum<16>(acc[i]);
+    const f2 both = both16(v);
+    v = both.x + both.y;
+    if (c == i) mine = v;
+  }
+  return mine;
+}
+__device__ __forceinline__ void store_weights(const WeighArgs &a, const WeighItem &w, const Ring &ring, const Place &at, int t0, float mine, int c, int hh) {
+  const int t = 8 * (c / 4) + 4 * hh + c % 4;
+  if (c >= 16 || t0 + t >= w.len) return;
+  const int64_t r = (int64_t)w.seq * ring.blocks + at.block, rec = a.tv.table ? (int64_t)a.tv.table[r] : r;
+  float *const x = a.weights + (rec * a.Hkv + w.hkv) * ring.bt + at.row + t;
+  *x = t0 + t >= a.first_fresh[w.slot] ? mine : *x + mine;
+}
+// A row's log-sum-exp as it lies, and the tokens of the tier that the row sees (rows behind the last: none).
+struct RawRow {
+  float lse;
+  int sees;
+};
+__device__ __forceinline__ RawRow raw_row(const WeighArgs &a, const WeighItem &w, int row) {
+  const int r = min(row, w.rows - 1), token = token_of(a, r), hq = w.hkv * a.G + r - token * a.G;
+  return {a.lse[((int64_t)w.entry * a.n_tokens + token) * a.Hq + hq], row < w.rows ? min(w.sees + token, w.len) : 0};
+}
+// The exponent's summand, and the tokens again: none where the log-sum-exp is not finite.
+struct RowOf {
+  float off;
+  int sees;
+};
+__device__ __forceinline__ RowOf row_of(const RawRow &x) {
+  const bool on = fabsf(x.lse) < INFINITY;
+  return {on ? -x.lse * kLog2e : 0.0f, on ? x.sees : 0};
+}
+template <bool BF>
+__device__ __forceinline__ u32x4 query_piece(const WeighArgs &a, const WeighItem &w, int row, int p) {
+  const int r = min(row, w.rows - 1), token = token_of(a, r), hq = w.hkv * a.G + r - token * a.G;
+  u32x4 x = *(const u32x4 *)(a.q + w.entry * a.q_seq + token * a.q_token + hq * a.q_head + 16 * p);
+  if (!BF && a.q_fmt == TTKV_BF16) to_fp16(x);
+  return x;
+}
+
+// Steps s .. n - 1 of rows that lie in LDS: the next one's products beside this one's exponentials.  row_at: the lane's of step 0; t: the wave's first token.
+template <bool BF, int KF>
+__device__ __forceinline__ f16v sum_steps(f16v acc, const Operands<KF> &ops, const char *q_at, const RowOf *row_at, int s, int n, int t, float cs, int hh) {
+  constexpr int kStep = 32 * kRowK;
+  if (s >= n) return acc;
+  f16v sc, nx;
+  RowOf r = row_at[32 * s], rn;
+  auto one = [&](f16v &now, f16v &then, const RowOf &of, RowOf &of_next) __attribute__((always_inline)) {
+    of_next = row_at[32 * s + 32];
+    then = mask_rows(side_by_side<BF, KF>(ops, q_at + (s + 1) * kStep, acc, now, cs, of.off), of_next.sees - t, hh);
+  };
+  sc = mask_rows(score_rows<BF, KF>(ops, q_at + s * kStep), r.sees - t, hh);
+  for (; s + 2 < n; ++s) {
+    one(sc, nx, r, rn);
+    ++s;
+    one(nx, sc, rn, r);
+  }
+  if (s + 1 == n) return add_rows(acc, sc, cs, r.off);
+  one(sc, nx, r, rn);
+  return add_rows(acc, nx, cs, rn.off);
+}
+
+// Few rows (a step's, the last queries of a prompt).  Bound: memory, and from some 200 rows on the vector unit's exponentials.  All rows lie in LDS; the waves take an item's tokens 32 at a time, the
+// next ones' keys on their way, and meet nobody.  Keys are loaded as whole lines and turned into operands through LDS of the wave's own (as
+// operands they are pieces of 32 bytes of 32 rows per instruction: a step of 48 x 4000 tokens of 32 / 8 heads 86 us).
+template <bool BF, int KF, int ROWS, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void weigh_few_kernel(const WeighArgs a) {
+  constexpr int kPart = 32 * kRowK, kOwn = (is_quant(KF) ? 2 : 1) * kPart;
+  __shared__ __align__(16) char s_all[ROWS * kRowK + NW * kOwn];
+  __shared__ RowOf s_row[ROWS];
+  char *const s_q = s_all, *const s_k = s_all + ROWS * kRowK;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hh = lane >> 5;
+  const WeighItem w = weigh_item(a);
+  const int end = min(w.t0 + a.chunk, w.len), steps = (w.rows + 31) / 32;
+  const Ring ring(a.tv, w.seq, w.hkv);
+  int t = w.t0 + 32 * wave;
+  Place next(ring, a.tv.bt_magic, a.first_tok[w.slot] + (t < end ? t : w.t0)), at = next;
+  Piece<KF> x[8];   // rows lane / 16 + 4 i, piece lane % 16
+  auto load = [&](int left) __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      f16v sc = {};
+    for (int i = 0; i < 8; ++i) x[i] = load_piece<KF>(next.head, next.head + a.tv.k_meta_off, next.row + min((lane >> 4) + 4 * i, min(31, left - 1)), lane & 15);
+  };
+  if (t < end) load(w.len - t);
+  for (int i = threadIdx.x; i < steps * 512; i += 64 * NW) *(u32x4 *)(s_q + (i >> 4) * kRowK + 16 * (i & 15)) = query_piece<BF>(a, w, i >> 4, i & 15);
+  for (int i = threadIdx.x; i < steps * 32; i += 64 * NW) s_row[i] = row_of(raw_row(a, w, i));
+  __syncthreads();
+  char *const own = s_k + wave * kOwn;
+  const char *const q_at = s_q + k_lane(lane);
+  const float cs = a.scale * kLog2e;
+  for (; t < end; t += 32 * NW) {
 #pragma unroll
-      for (int kb = 0; kb < 8; ++kb) {
-        sc = mma<BF>(kf[g][kb], qf[kb], sc);
-        if constexpr (two) sc = mma<BF>(kl[g][kb], qf[kb], sc);
-      }
-      if (!whole) mask_from(sc, lim - 32 * g, hh);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[g][i] += __builtin_amdgcn_exp2f(fmaf(sc[i], cs, off));
+    for (int i = 0; i < 8; ++i) {
+      char *const to = own + ((lane >> 4) + 4 * i) * kRowK + 16 * (lane & 15);
+      put_piece<BF, KF, true>(x[i], to, to + kPart);
     }
+    at = next;
+    if (t + 32 * NW < end) {
+      next.advance(ring, 32 * NW);
+      load(w.len - t - 32 * NW);
+    }
+    Operands<KF> ops;
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) {
+      ops.hi[kb] = *(const u32x4 *)(own + k_lane(lane) + 32 * kb);
+      if constexpr (is_quant(KF)) ops.lo[kb] = *(const u32x4 *)(own + kPart + k_lane(lane) + 32 * kb);
+    }
+    // from the first row that sees one of the tokens on
+    const f16v acc = sum_steps<BF, KF>(f16v{}, ops, q_at, s_row + c, max(0, t - w.sees + 1) * a.G / 32, steps, t, cs, hh);
+    store_weights(a, w, ring, at, t, gather(acc, c), c, hh);
+  }
+}
+
+// Many rows (a prompt's).  Bound: the vector unit's exponentials.  A wave keeps its tokens, the rows come through LDS; where there are few tokens, several
+// items share a tile's rows, and weigh_sum_kernel adds their sums in order.
+// (128 rows between two barriers: with 32 a step's rows were asked for one step ahead, less than they take; 2047 queries of 28 / 4 heads 52 us.)
+template <bool BF, int KF>
+__global__ __launch_bounds__(64 * kWaves, 1) void weigh_kernel(const WeighArgs a) {
+  constexpr int kRows = 128, kSteps = kRows / 32, kStage = kRows * kRowK, NL = kRows * 16 / (64 * kWaves);
+  __shared__ __align__(16) char s_q[2 * kStage];   // two stages' rows
+  __shared__ RowOf s_row[2 * kRows];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, hh = lane >> 5;
+  const WeighItem w = weigh_item(a);
+  const int t0 = w.t0 + 32 * wave;
+  const bool idle = t0 >= w.len;
+  const Ring ring(a.tv, w.seq, w.hkv);
+  const Place at(ring, a.tv.bt_magic, a.first_tok[w.slot] + (idle ? w.t0 : t0));
+  // rows in steps of 32, from the first that sees a token of the tile on; this item's share of them
+  const int all1 = (w.rows + 31) / 32, all0 = min(max(0, w.t0 - w.sees + 1) * a.G / 32, all1);
+  const int per = (all1 - all0 + a.n_split - 1) / a.n_split;
+  const int s0 = min(all0 + w.split * per, all1), s1 = min(s0 + per, all1);
+  const int qrow = threadIdx.x >> 4, qp = threadIdx.x & 15;
+  u32x4 qr[NL];
+  RawRow raw = {};
+  auto load = [&](int s) __attribute__((always_inline)) {   // rows of the stage that begins with step s
+#pragma unroll
+    for (int i = 0; i < NL; ++i) qr[i] = query_piece<BF>(a, w, 32 * s + qrow + 4 * kWaves * i, qp);
+    if (threadIdx.x < kRows) raw = raw_row(a, w, 32 * s + threadIdx.x);
+  };
+  auto put = [&](int buffer) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) *(u32x4 *)(s_q + buffer * kStage + (qrow + 4 * kWaves * i) * kRowK + 16 * qp) = qr[i];
+    if (threadIdx.x < kRows) s_row[buffer * kRows + threadIdx.x] = row_of(raw);
+  };
+  if (s0 < s1) load(s0);
+  Operands<KF> ops;
+  ops.load(at, a.tv.k_meta_off, max(w.len - t0, 1), c, hh);
+  f16v acc = {};
+  const float cs = a.scale * kLog2e;
+  if (s0 < s1) put(0);
+  if (s0 + kSteps < s1) load(s0 + kSteps);
+  int now = 0;
+  for (int s = s0; s < s1; s += kSteps) {
+    __syncthreads();   // the stage's rows are there; everybody is done with those of the one before
+    if (s + kSteps < s1) put(1 - now);
+    if (s + 2 * kSteps < s1) load(s + 2 * kSteps);
+    if (!idle)
+      acc = sum_steps<BF, KF>(acc, ops, s_q + now * kStage + k_lane(lane), s_row + now * kRows + c, 0, min(kSteps, s1 - s), t0, cs, hh);
+    now = 1 - now;
   }
   if (idle) return;
-  // over the 32 lanes of a half; lane c of half hh then stores token 32 g + 8 (c / 4) + 4 hh + c % 4 (c < 16)
-  float mine[2] = {0.0f, 0.0f};
+  const float mine = gather(acc, c);
+  if (a.n_split == 1) return store_weights(a, w, ring, at, t0, mine, c, hh);
+  if (c < 16) a.sums[((int64_t)w.split * a.Hkv + w.hkv) * a.n_sums + (int64_t)a.first_item[w.slot] * kTile + t0 + 8 * (c / 4) + 4 * hh + c % 4] = mine;
+}
+// The sums of a tile's items, a thread per token.
+__global__ __launch_bounds__(kTile) void weigh_sum_kernel(const WeighArgs a) {
+  const int item = blockIdx.x, hkv = blockIdx.y;
+  const int slot = __popcll(__ballot(a.first_item[threadIdx.x & 63] <= item)) - 1;
+  const int t = (item - a.first_item[slot]) * kTile + threadIdx.x;
+  if (t >= a.len[slot]) return;
+  const float *const sums = a.sums + (int64_t)hkv * a.n_sums + (int64_t)a.first_item[slot] * kTile + t;
+  float v = 0.0f;
+  const int64_t stride = (int64_t)a.Hkv * a.n_sums;
+  for (int i = 0; i < a.n_split; i += 8) {   // eight asked for at once
+    float x[8];
 #pragma unroll
-  for (int g = 0; g < 2; ++g)
+    for (int j = 0; j < 8; ++j) x[j] = i + j < a.n_split ? sums[(i + j) * stride] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = group_sum<16>(acc[g][i]);
-      const f2 both = both16(v);
-      v = both.x + both.y;
-      if (c == i) mine[g] = v;
-    }
-  if (c >= 16) return;
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const int t = 32 * g + 8 * (c / 4) + 4 * hh + c % 4;
-    if (t0 + t >= len) continue;
-    const int64_t r = (int64_t)seq * ring.blocks + at.block, rec = a.tv.table ? (int64_t)a.tv.table[r] : r;
-    float *const w = a.weights + (rec * a.Hkv + hkv) * ring.bt + at.row + t;
-    *w = t0 + t >= a.first_fresh[slot] ? mine[g] : *w + mine[g];
+    for (int j = 0; j < 8; ++j) v += x[j];
   }
+  int tok = a.first_tok[slot] + t;
+  if (tok >= a.tv.ring_blocks * a.tv.bt) tok -= a.tv.ring_blocks * a.tv.bt;
+  const int block = div_bt(tok, a.tv.bt, a.tv.bt_magic);
+  const int64_t r = (int64_t)(a.first_seq + a.entry[slot]) * a.tv.ring_blocks + block, rec = a.tv.table ? (int64_t)a.tv.table[r] : r;
+  float *const x = a.weights + (rec * a.Hkv + hkv) * a.tv.bt + tok - block * a.tv.bt;
+  *x = t >= a.first_fresh[slot] ? v : *x + v;
 }
 
 // ---------------------------------------------------------------- the lightest tokens go
@@ -264,14 +448,42 @@ __global__ __launch_bounds__(256) void light_move_kernel(const LightArgs a) {
 
 }  // namespace
 
-hipError_t launch_weigh(const WeighArgs &a, hipStream_t s) {
-  const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv), block(64 * kWaves);
-  switch (a.tv.k_fmt) {
-    case TTKV_F16: hipLaunchKernelGGL((weigh_kernel<false, TTKV_F16>), grid, block, 0, s, a); break;
-    case TTKV_BF16: hipLaunchKernelGGL((weigh_kernel<true, TTKV_BF16>), grid, block, 0, s, a); break;
-    case TTKV_I8_SYM_G32: hipLaunchKernelGGL((weigh_kernel<false, TTKV_I8_SYM_G32>), grid, block, 0, s, a); break;
-    default: hipLaunchKernelGGL((weigh_kernel<false, TTKV_I4_ASYM_G64>), grid, block, 0, s, a);
+void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int k_fmt, int32_t &chunk, int32_t &n_split) {
+  n_split = 1;
+  chunk = kTile;
+  const int64_t resident = 256;
+  if (most_rows <= kFewRows) {   // as many tokens per item as leave every workgroup that fits on the chip, one per CU, one
+    const int64_t want = most_rows <= 64 ? 2048 : 256;
+    chunk = (int32_t)(kTile * std::max<int64_t>(1, std::min<int64_t>(64, (tiles * Hkv + want - 1) / want)));
+    return;
   }
+  // several items per tile where the tiles alone leave CUs idle: steps of 32 rows, eight at least
+  n_split = (int32_t)std::max<int64_t>(1, std::min((2 * resident + tiles * Hkv - 1) / (tiles * Hkv), (most_rows + 255) / 256));
+  if (tiles * Hkv >= resident) n_split = 1;
+}
+
+template <bool BF, int KF>
+hipError_t start_weigh(const WeighArgs &a, int64_t most_rows, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv * (unsigned)a.n_split);
+  constexpr int mid = is_quant(KF) ? 4 : 8;
+  if (most_rows <= 64) hipLaunchKernelGGL((weigh_few_kernel<BF, KF, 64, 4>), grid, dim3(256), 0, s, a);
+  else if (most_rows <= kFewRows) hipLaunchKernelGGL((weigh_few_kernel<BF, KF, kFewRows, mid>), grid, dim3(64 * mid), 0, s, a);
+  else hipLaunchKernelGGL((weigh_kernel<BF, KF>), grid, dim3(64 * kWaves), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_weigh(const WeighArgs &a, int64_t most_rows, hipStream_t s, int *n_kernels) {
+  hipError_t e;
+  switch (a.tv.k_fmt) {
+    case TTKV_F16: e = start_weigh<false, TTKV_F16>(a, most_rows, s); break;
+    case TTKV_BF16: e = start_weigh<true, TTKV_BF16>(a, most_rows, s); break;
+    case TTKV_I8_SYM_G32: e = start_weigh<false, TTKV_I8_SYM_G32>(a, most_rows, s); break;
+    default: e = start_weigh<false, TTKV_I4_ASYM_G64>(a, most_rows, s);
+  }
+  *n_kernels += 1;
+  if (e != hipSuccess || a.n_split == 1) return e;
+  hipLaunchKernelGGL(weigh_sum_kernel, dim3((unsigned)a.n_items, (unsigned)a.Hkv), dim3(kTile), 0, s, a);
+  *n_kernels += 1;
   return hipGetLastError();
 }
 

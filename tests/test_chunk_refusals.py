@@ -87,13 +87,13 @@ def test_chunk_prefixes(h):  # noqa: F811
 
 
 def weigh(h, c, q=None, lse=ADDR, T=4, each=None, fresh=None, tier=0, seq=-1, w=ADDR):  # noqa: F811
-    return status(B.ttkv_add_weights, h, c, tier, seq, q or heads(**Q), lse, T, each, fresh, w, None)
+    return status(B.ttkv_add_weights, h, c, tier, seq, q or heads(**Q), lse, T, each, fresh, w, None, 0, None)
 
 
 def test_weight_refusals(h):  # noqa: F811
     c = cache()
-    assert status(B.ttkv_add_weights, None, c, 0, -1, heads(**Q), ADDR, 4, None, None, ADDR, None) == B.ERR_INVALID_ARG
-    assert status(B.ttkv_add_weights, h, c, 0, -1, None, ADDR, 4, None, None, ADDR, None) == B.ERR_INVALID_ARG
+    assert status(B.ttkv_add_weights, None, c, 0, -1, heads(**Q), ADDR, 4, None, None, ADDR, None, 0, None) == B.ERR_INVALID_ARG
+    assert status(B.ttkv_add_weights, h, c, 0, -1, None, ADDR, 4, None, None, ADDR, None, 0, None) == B.ERR_INVALID_ARG
     assert weigh(h, c, lse=None) == B.ERR_INVALID_ARG and weigh(h, c, w=None) == B.ERR_INVALID_ARG
     assert weigh(h, c, T=0) == B.OK and weigh(h, c, each=i64(0, 0)) == B.OK and weigh(h, cache(lens=(0, 0))) == B.OK
     for kw in (dict(tier=1), dict(tier=-1), dict(seq=2), dict(seq=-2), dict(T=-1), dict(each=i64(5, 0)), dict(each=i64(0, -1)), dict(fresh=i64(-1, 0)),

@@ -324,126 +324,231 @@ __device__ __forceinline__ TokenPlace token_place(const TierView &tv, int seq, i
   const int64_t r = (int64_t)seq * tv.ring_blocks + block;
   return {tv.table ? (int64_t)tv.table[r] : r, tok - block * tv.bt};
 }
-// One row, by 32 lanes: keys (lanes 0 .. 15), values, what decompresses them, the weight.
-__device__ __forceinline__ void move_row(const LightArgs &a, int slot, int hkv, int from, int to, int lane) {
-  const TokenPlace f = token_place(a.tv, a.seq[slot], a.first_tok[slot] + from), t = token_place(a.tv, a.seq[slot], a.first_tok[slot] + to);
-  uint8_t *const fh = a.tv.base + f.rec * a.tv.rec_bytes + (int64_t)hkv * a.tv.head_bytes, *const th = a.tv.base + t.rec * a.tv.rec_bytes + (int64_t)hkv * a.tv.head_bytes;
-  const int side = lane >> 4, p = lane & 15;
-  const int width = side ? a.vc : a.kc, off = side ? a.tv.v_off : 0;
-  if (16 * p < width) {
-    u32x4 *const x = (u32x4 *)(fh + off + (int64_t)f.row * width + 16 * p), *const y = (u32x4 *)(th + off + (int64_t)t.row * width + 16 * p);
-    const u32x4 v = *x;
-    if (a.swap) *x = *y;
-    *y = v;
+// What a lane of 32 has to do with a row that moves: lanes 0 .. 15 its keys, 16 .. 31 its values (16 bytes each), lanes 0 and 16 what decompresses
+// them, lane 1 the weight.
+struct RowMove {
+  u32x4 *x, *y;       // from, to
+  u32x2 *mx, *my;
+  float *wx, *wy;
+  u32x4 v, u;
+  u32x2 mv, mu;
+  float wv, wu;
+  bool on, meta, weight;
+  __device__ __forceinline__ void begin(const LightArgs &a, int slot, int hkv, int from, int to, int lane, bool valid) {   // asks for what moves
+    const TokenPlace f = token_place(a.tv, a.seq[slot], a.first_tok[slot] + from), t = token_place(a.tv, a.seq[slot], a.first_tok[slot] + to);
+    const int64_t head = (int64_t)hkv * a.tv.head_bytes;
+    uint8_t *const fh = a.tv.base + f.rec * a.tv.rec_bytes + head, *const th = a.tv.base + t.rec * a.tv.rec_bytes + head;
+    const int side = lane >> 4, p = lane & 15, width = side ? a.vc : a.kc, off = side ? a.tv.v_off : 0, m = side ? a.tv.v_meta_off : a.tv.k_meta_off;
+    on = valid && 16 * p < width;
+    meta = valid && p == 0 && (side ? a.vm : a.km);
+    weight = valid && lane == 1;
+    x = (u32x4 *)(fh + off + (int64_t)f.row * width + 16 * p);
+    y = (u32x4 *)(th + off + (int64_t)t.row * width + 16 * p);
+    mx = (u32x2 *)(fh + m + (int64_t)f.row * 8);
+    my = (u32x2 *)(th + m + (int64_t)t.row * 8);
+    wx = a.weights + (f.rec * a.Hkv + hkv) * a.tv.bt + f.row;
+    wy = a.weights + (t.rec * a.Hkv + hkv) * a.tv.bt + t.row;
+    if (on) v = *x;
+    if (meta) mv = *mx;
+    if (weight) wv = *wx;
+    if (!a.swap) return;
+    if (on) u = *y;
+    if (meta) mu = *my;
+    if (weight) wu = *wy;
   }
-  if (p == 0 && (side ? a.vm : a.km)) {
-    const int meta = side ? a.tv.v_meta_off : a.tv.k_meta_off;
-    u32x2 *const x = (u32x2 *)(fh + meta + (int64_t)f.row * 8), *const y = (u32x2 *)(th + meta + (int64_t)t.row * 8);
-    const u32x2 v = *x;
-    if (a.swap) *x = *y;
-    *y = v;
+  __device__ __forceinline__ void end(const LightArgs &a) const {
+    if (on) *y = v;
+    if (meta) *my = mv;
+    if (weight) *wy = wv;
+    if (!a.swap) return;
+    if (on) *x = u;
+    if (meta) *mx = mu;
+    if (weight) *wx = wu;
   }
-  if (lane == 1) {
-    const int Hkv = a.Hkv, bt = a.tv.bt;
-    float *const x = a.weights + (f.rec * Hkv + hkv) * bt + f.row, *const y = a.weights + (t.rec * Hkv + hkv) * bt + t.row;
-    const float v = *x;
-    if (a.swap) *x = *y;
-    *y = v;
-  }
-}
+};
 
-// A workgroup per (sequence, KV head): the (old - gone)-th largest weight by a radix select of its order, four passes of 8 bits; equal ones
-// stay from the oldest on.  Then the tokens in order, 1024 at a time: the i-th that stays among the first `gone` moves to the i-th place
-// behind them whose token goes.
-constexpr int kInPlace = 64;   // moves that the selecting workgroup makes by itself
-__global__ __launch_bounds__(1024) void light_select_kernel(const LightArgs a, int in_place) {
-  __shared__ uint32_t s_hist[256];
-  __shared__ int s_wave[16][3];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_left;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ int row_sum(int v) {   // over 16 lanes, in each of them
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, true);
+  return v;
+}
+// A workgroup per (sequence, KV head), each of its 16 waves a stretch of the tokens, 64 at a time; up to 64 IPT of them a wave keeps their orders in
+// registers, beyond (IPT 0) it reads the weights again.  The (old - gone)-th largest order is found by a radix select, 11, 11 and 10 bits of it at a time:
+// the first ones are exponent and two bits of the mantissa, so that tokens whose weights share an exponent do not all count on one of
+// LDS's counters.  (Counting the tokens above three candidates by ballots, two bits at a time: 4 x 32768 tokens 76 us.)  Then each wave
+// knows the places of its tokens from the counts of the waves before it: the i-th token that stays among the first `gone` moves to the i-th
+// place behind them whose token goes.
+constexpr int kInPlace = 256;   // moves that the selecting workgroup makes by itself
+template <int IPT>
+__global__ __launch_bounds__(1024, IPT > 12 ? 1 : 2) void light_select_kernel(const LightArgs a, int in_place) {
+  __shared__ i32x2 s_count[2][16];
+  __shared__ int s_hist[2][2048], s_total[16], s_pick[2];
+  __shared__ int32_t s_list[2 * kInPlace];
   const int hkv = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int old = a.old[slot], gone = a.gone[slot], keep = old - gone, seq = a.seq[slot], first = a.first_tok[slot];
-  int32_t *const list = a.moves + 2 * (a.move_base[slot] + (int64_t)hkv * a.most_moves[slot]);
-  auto weight = [&](int i) __attribute__((always_inline)) {
-    const TokenPlace p = token_place(a.tv, seq, first + i);
-    return order_of(a.weights[(p.rec * a.Hkv + hkv) * a.tv.bt + p.row]);
+  const int steps = (old + 1023) / 1024;            // of 64 tokens, of each wave
+  const int begin = wave * steps * 64;
+  int32_t *const list = in_place ? s_list : a.moves + 2 * (a.move_base[slot] + (int64_t)hkv * a.most_moves[slot]);
+  // 64 tokens lie in one block: the weights of the wave's c-th ones; behind the last token: what lies beside it, or its own 64 again
+  auto weights_at = [&](int c) __attribute__((always_inline)) -> const float * {
+    const TokenPlace p = token_place(a.tv, seq, first + min(begin + 64 * c, (old - 1) & ~63));
+    return a.weights + (p.rec * a.Hkv + hkv) * a.tv.bt + p.row;
   };
-  uint32_t prefix = 0;
-  int left = keep;   // of the tokens whose order begins with the prefix, so many stay
-  for (int shift = 24; shift >= 0 && keep > 0; shift -= 8) {
-    if (threadIdx.x < 256) s_hist[threadIdx.x] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < old; i += 1024) {
-      const uint32_t u = weight(i);
-      if (shift == 24 || u >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&s_hist[u >> shift & 255], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {   // lane -> bins 255 - 4 lane .. 252 - 4 lane
-      int n[4], sum = 0;
+  auto order_at = [&](int c, float w) __attribute__((always_inline)) { return begin + 64 * c + lane < old ? order_of(w) : 0u; };
+  uint32_t u[IPT ? IPT : 1];
+  if constexpr (IPT > 0) {   // each lane looks one up, then all are asked for at once
+    const uint64_t at = (uint64_t)weights_at(lane);
+    const int lo = (int)at, hi = (int)(at >> 32);
+    float x[IPT];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += n[j] = s_hist[255 - 4 * lane - j];
-      int before = sum;
+    for (int c = 0; c < IPT; ++c) {
+      const uint64_t p = (uint32_t)__builtin_amdgcn_readlane(lo, c) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, c) << 32;
+      x[c] = ((const __attribute__((address_space(1))) float *)p)[lane];
+    }
+#pragma unroll
+    for (int c = 0; c < IPT; ++c) u[c] = order_at(c, x[c]);
+  }
+  auto each = [&](auto f) __attribute__((always_inline)) {   // f(step, order), tokens behind the last one's: order 0
+    if constexpr (IPT > 0) {
+#pragma unroll
+      for (int c = 0; c < IPT; ++c)
+        if (c < steps) f(c, u[c]);   // (what follows is the next wave's)
+    } else {
+      for (int c = 0; c < steps; c += 4) {   // four asked for at once
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = weights_at(c + j)[lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (c + j < steps) f(c + j, order_at(c + j, x[j]));
+      }
+    }
+  };
+  int buffer = 0;
+  // Counts of the wave for everybody: lane v < 16 then has wave v's, and the sums over all waves (before: over the waves before this one) come
+  // from lanes 0 .. 15 of each row.
+  auto meet = [&](const int (&n)[2], int (&before)[2], int (&all)[2]) __attribute__((always_inline)) {
+    if (lane == 0) s_count[buffer][wave] = i32x2{n[0], n[1]};
+    __syncthreads();
+    const i32x2 x = s_count[buffer][lane & 15];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      all[j] = __builtin_amdgcn_readfirstlane(row_sum(x[j]));
+      before[j] = __builtin_amdgcn_readfirstlane(row_sum((lane & 15) < wave ? x[j] : 0));
+    }
+    buffer ^= 1;   // written again after the next meeting only
+  };
+  int before[2], all[2];
+  uint32_t least = 0;   // the largest order that `keep` tokens have at least
+  int left = keep;      // of the tokens that begin like it so many stay (the oldest)
+  if (keep > 0) {
+    for (int i = threadIdx.x; i < 2048; i += 1024) s_hist[0][i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      int *const hist = s_hist[pass & 1];
+      each([&](int c, uint32_t x) __attribute__((always_inline)) {
+        const bool on = begin + 64 * c + lane < old && (pass == 0 || (pass == 1 ? x >> 21 == least >> 21 : x >> 10 == least >> 10));
+        const int digit = x >> shift & 2047;
+        const uint64_t who = __ballot(on);
+        if (!who) return;
+        const int one = __builtin_amdgcn_readlane(digit, __builtin_ctzll(who));
+        if (__ballot(on && digit != one) == 0) {   // one counter: added to once
+          if (lane == 0) atomicAdd(&hist[one], __popcll(who));
+        } else if (on) {
+          atomicAdd(&hist[digit], 1);
+        }
+      });
+      __syncthreads();
+      if (pass < 2)
+        for (int i = threadIdx.x; i < 2048; i += 1024) s_hist[1 - (pass & 1)][i] = 0;
+      // thread t: counters 2047 - 2 t and 2046 - 2 t
+      const int h1 = hist[2047 - 2 * threadIdx.x], h0 = hist[2046 - 2 * threadIdx.x];
+      int sum = h1 + h0;
 #pragma unroll
       for (int d = 1; d < 64; d *= 2) {
-        const int x = __shfl_up(before, d);
-        if (lane >= d) before += x;
+        const int x = __shfl_up(sum, d);
+        if (lane >= d) sum += x;
       }
-      before -= sum;
-      if (before < left && before + sum >= left) {
-        int j = 0;
-        while (before + n[j] < left) before += n[j++];
-        s_prefix = prefix | (uint32_t)(255 - 4 * lane - j) << shift;
-        s_left = left - before;
+      if (lane == 63) s_total[wave] = sum;
+      __syncthreads();
+      const int mine = s_total[lane & 15];
+      const int above = sum - h1 - h0 + __builtin_amdgcn_readfirstlane(row_sum((lane & 15) < wave ? mine : 0));   // counted in higher counters
+      if (above < left && above + h1 + h0 >= left) {
+        const bool upper = above + h1 >= left;
+        s_pick[0] = 2047 - 2 * threadIdx.x - !upper;
+        s_pick[1] = left - above - (upper ? 0 : h1);
       }
+      __syncthreads();
+      least |= (uint32_t)s_pick[0] << shift;
+      left = s_pick[1];
     }
-    __syncthreads();
-    prefix = s_prefix;
-    left = s_left;
   }
-  int n_equal = 0, n_from = 0, n_to = 0;   // of the tokens before
-  for (int i0 = 0; i0 < old; i0 += 1024) {
-    const int i = i0 + threadIdx.x;
-    const uint32_t u = i < old ? weight(i) : 0;
-    const bool equal = keep > 0 && i < old && u == prefix;
-    const uint64_t me = (1ull << lane) - 1, be = __ballot(equal);
-    if (lane == 0) s_wave[wave][0] = __popcll(be);
-    __syncthreads();
-    int rank = n_equal + __popcll(be & me);
-    for (int w = 0; w < wave; ++w) rank += s_wave[w][0];
-    for (int w = 0; w < 16; ++w) n_equal += s_wave[w][0];
-    const bool stays = keep > 0 && i < old && (u > prefix || (equal && rank < left));
-    const bool from = stays && i < gone, to = !stays && i >= gone && i < old;
-    const uint64_t bf = __ballot(from), bt = __ballot(to);
-    if (lane == 0) {
-      s_wave[wave][1] = __popcll(bf);
-      s_wave[wave][2] = __popcll(bt);
-    }
-    __syncthreads();
-    int rf = n_from + __popcll(bf & me), rt = n_to + __popcll(bt & me);
-    for (int w = 0; w < wave; ++w) {
-      rf += s_wave[w][1];
-      rt += s_wave[w][2];
-    }
-    for (int w = 0; w < 16; ++w) {
-      n_from += s_wave[w][1];
-      n_to += s_wave[w][2];
-    }
-    if (from) list[2 * rf] = i;
-    if (to) list[2 * rt + 1] = i;
-  }
-  if (threadIdx.x == 0) a.count[slot * a.Hkv + hkv] = n_from;
+  // 64 tokens in order stay or go together before or behind `gone`, which is whole blocks.  f(step, is in front of it, bits of those that stay, of
+  // those that are live)
+  const uint64_t lower = (1ull << lane) - 1;
+  int n[2] = {0, 0};
+  each([&](int c, uint32_t x) __attribute__((always_inline)) { n[0] += __popcll(__ballot(x == least && begin + 64 * c + lane < old)); });
+  meet(n, before, all);
+  const int equal_before = before[0];
+  auto each_group = [&](auto f) __attribute__((always_inline)) {
+    int rank = equal_before;
+    each([&](int c, uint32_t x) __attribute__((always_inline)) {
+      const int i0 = begin + 64 * c;
+      const uint64_t live = old - i0 >= 64 ? ~0ull : old > i0 ? (1ull << (old - i0)) - 1 : 0;
+      const uint64_t equal = __ballot(x == least) & live;
+      uint64_t stays = __ballot(x > least) & live;
+      if (equal) {
+        const bool me = equal >> lane & 1;
+        stays |= __ballot(me && rank + __popcll(equal & lower) < left);
+        rank += __popcll(equal);
+      }
+      if (keep == 0) stays = 0;
+      f(c, i0 < gone, stays, live);
+    });
+  };
+  n[0] = n[1] = 0;
+  each_group([&](int, bool front, uint64_t stays, uint64_t live) __attribute__((always_inline)) {
+    if (front) n[0] += __popcll(stays);
+    else n[1] += __popcll(live & ~stays);
+  });
+  meet(n, before, all);
+  int rank[2] = {before[0], before[1]};
+  each_group([&](int c, bool front, uint64_t stays, uint64_t live) __attribute__((always_inline)) {
+    const uint64_t who = front ? stays : live & ~stays;
+    int &at = front ? rank[0] : rank[1];
+    if (who >> lane & 1) list[2 * (at + __popcll(who & lower)) + !front] = begin + 64 * c + lane;
+    at += __popcll(who);
+  });
+  if (threadIdx.x == 0) a.count[slot * a.Hkv + hkv] = all[0];
   if (!in_place) return;
-  __threadfence_block();
   __syncthreads();
-  for (int i = threadIdx.x >> 5; i < n_from; i += 32) move_row(a, slot, hkv, list[2 * i], list[2 * i + 1], threadIdx.x & 31);
+  const int moves = all[0], group = threadIdx.x >> 5;
+  for (int i = group; i < moves; i += 32) {
+    RowMove m;
+    m.begin(a, slot, hkv, s_list[2 * i], s_list[2 * i + 1], threadIdx.x & 31, true);
+    m.end(a);
+  }
 }
+// Two rows per 32 lanes.
 __global__ __launch_bounds__(256) void light_move_kernel(const LightArgs a) {
   const int hkv = blockIdx.y % a.Hkv, slot = blockIdx.y / a.Hkv;
-  const int i = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (i >= a.count[slot * a.Hkv + hkv]) return;
+  const int moves = a.count[slot * a.Hkv + hkv], i = blockIdx.x * 16 + (threadIdx.x >> 5);
+  if (i >= moves) return;
   const int32_t *const list = a.moves + 2 * (a.move_base[slot] + (int64_t)hkv * a.most_moves[slot]);
-  move_row(a, slot, hkv, list[2 * i], list[2 * i + 1], threadIdx.x & 31);
+  RowMove m[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int k = min(i + 8 * j, moves - 1);
+    m[j].begin(a, slot, hkv, list[2 * k], list[2 * k + 1], threadIdx.x & 31, i + 8 * j < moves);
+  }
+#pragma unroll
+  for (int j = 0; j < 2; ++j) m[j].end(a);
 }
 
 }  // namespace
@@ -489,11 +594,16 @@ hipError_t launch_weigh(const WeighArgs &a, int64_t most_rows, hipStream_t s, in
 
 hipError_t launch_light(const LightArgs &a, int32_t most_moves, hipStream_t s, int *n_kernels) {
   const bool in_place = most_moves <= kInPlace;
-  hipLaunchKernelGGL(light_select_kernel, dim3((unsigned)(a.n_slots * a.Hkv)), dim3(1024), 0, s, a, (int)in_place);
+  const dim3 grid((unsigned)(a.n_slots * a.Hkv)), block(1024);
+  const int most_old = *std::max_element(a.old, a.old + a.n_slots);
+  if (most_old <= 4 * 1024) hipLaunchKernelGGL(light_select_kernel<4>, grid, block, 0, s, a, (int)in_place);
+  else if (most_old <= 12 * 1024) hipLaunchKernelGGL(light_select_kernel<12>, grid, block, 0, s, a, (int)in_place);
+  else if (most_old <= 32 * 1024) hipLaunchKernelGGL(light_select_kernel<32>, grid, block, 0, s, a, (int)in_place);
+  else hipLaunchKernelGGL(light_select_kernel<0>, grid, block, 0, s, a, (int)in_place);
   *n_kernels += 1;
   hipError_t e = hipGetLastError();
   if (in_place || e != hipSuccess) return e;
-  hipLaunchKernelGGL(light_move_kernel, dim3((unsigned)((most_moves + 7) / 8), (unsigned)(a.n_slots * a.Hkv)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(light_move_kernel, dim3((unsigned)((most_moves + 15) / 16), (unsigned)(a.n_slots * a.Hkv)), dim3(256), 0, s, a);
   *n_kernels += 1;
   return hipGetLastError();
 }

@@ -19,6 +19,10 @@ SOURCES = {
     "ttkv_rope.hip": [],
     "ttkv_shared.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_shared_quant.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ttkv_chunk_mixed.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ttkv_chunk_i8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ttkv_chunk_i4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ttkv_chunk_k8v4.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_chunk.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_weights.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "ttkv_probe.hip": [],
@@ -36,7 +40,7 @@ def _compile(item):
 
 
 def build(verbose=False):
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, SOURCES.items()))
     subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs], check=True)
     if verbose:

@@ -1705,14 +1705,14 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
   a.members = 0;
   a.n_prefix = prefix ? prefix->n_tiers : 0;
   a.n_tiers = a.n_prefix + c->n_tiers;
-  bool quantized = false;
+  int quantized = 0;
   int64_t lead = 0;
   for (int i = 0; i < a.n_prefix; ++i) {   // oldest first
     const ttkv_tier &T = prefix->tier[prefix->n_tiers - 1 - i];
     a.tv[i] = make_view(T, make_layout(T, c->n_kv_heads));
     a.prefix_tok[i] = (int32_t)(T.start[0] % ring_tokens(T));
     a.prefix_len[i] = (int32_t)T.len[0];
-    quantized |= T.len[0] > 0 && !is_fp(T.k_fmt);
+    if (T.len[0] > 0) quantized |= quantized_kind(T.k_fmt, T.v_fmt);
     lead += T.len[0];
   }
   for (int i = 0; i < c->n_tiers; ++i) {
@@ -1736,7 +1736,8 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
     const int64_t total = held_tokens(c, b) + (in ? lead : 0);
     if (total >= (1ll << 31) - (1 << 24)) return TTKV_ERR_UNSUPPORTED;   // places are counted in 32 bits
     if (n == 0) continue;
-    for (int t = 0; t < c->n_tiers; ++t) quantized |= c->tier[t].len[b] > 0 && !is_fp(c->tier[t].k_fmt);
+    for (int t = 0; t < c->n_tiers; ++t)
+      if (c->tier[t].len[b] > 0) quantized |= quantized_kind(c->tier[t].k_fmt, c->tier[t].v_fmt);
     slot[n_slots++] = Slot{j, b, n, total};
     P.rows += n * a.G;
     most_rows = std::max(most_rows, n * a.G);

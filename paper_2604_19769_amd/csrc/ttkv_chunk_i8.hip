@@ -1,0 +1,8 @@
+// Chunk attention over int8 tiers, beside fp16 or bf16 ones.
+#include "ttkv_chunk_kernels.h"
+
+namespace ttkv {
+
+void start_chunk_i8(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream) { chunk::start_quantized<kInt8>(a, s, stream); }
+
+}  // namespace ttkv

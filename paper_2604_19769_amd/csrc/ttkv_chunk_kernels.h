@@ -1,0 +1,639 @@
+// Attention of a chunk of new tokens over the tiers that hold them and everything before them: what a prompt, a part of one, or a few
+// drafted tokens ask of the cache.  The query rows of a KV head are its G query heads in every new token, row r = (token r / G, head r % G),
+// and a row sees the tokens up to its own:
+//       S^T[token][row] = sum_d K[token][d] Q[row][d],     O^T[d][row] += sum_token V[token][d] P[token][row]
+// with the running maximum and sum of the softmax in between.  Both products are v_mfma_f32_32x32x16 with tokens (channels) as rows and query
+// rows as columns, so a lane has 16 scores of ONE row and the scores' registers are the second product's operand as they lie.
+//
+// Outputs are 16 bits wide, so the weights are rounded once to the product's type; their sum, the maximum and the log-sum-exp stay fp32.
+// Quantized tiers are worked on in fp16 whatever the others' type, in front of them.  Their rows are decompressed on their way into LDS, keys
+// into two numbers each (22 bits: the log-sum-exp is an fp32 number), values into two where the outputs are fp16, into one where bf16 outputs
+// end far above what that rounds.
+//
+// A kernel knows the formats that it meets (Q: none, one, or all of the quantized ones): with the loops of all of them in every kernel, registers end in
+// scratch (20001 int8 tokens 1423 us instead of 1193, int4 turns 106 instead of 95).
+#pragma once
+#include "ttkv_chunk_dev.h"
+
+#include <algorithm>
+
+namespace ttkv {
+namespace chunk {
+
+// Weights are 2^unit times e^(score - reference), and the reference moves only when a score is `room` above it (powers of two): over
+// bf16 values no weight is above 1, over fp16 values they stay below 2^16 and keep 11 bits down to 2^-22 of the reference.
+template <bool BF>
+constexpr float unit16() { return BF ? -7.0f : 8.0f; }
+constexpr float kRoom16 = 7.0f;
+
+// ---------------------------------------------------------------- items
+struct ChunkItem {
+  int slot, entry, seq, hkv, row_tile, split, n_split;
+  int count, rows;   // new tokens, query rows
+};
+__device__ __forceinline__ ChunkItem chunk_item(const ChunkArgs &a, int rows_per_tile) {
+  ChunkItem it;
+  const uint32_t id = blockIdx.x;
+  const int item = a.Hkv == 1 ? id : a.hkv_magic ? (int)mul_high(id, a.hkv_magic) : (int)(id / (uint32_t)a.Hkv);
+  it.hkv = id - item * a.Hkv;
+  it.slot = __popcll(__ballot(a.first_item[threadIdx.x & 63] <= item)) - 1;
+  it.entry = a.entry[it.slot];
+  it.seq = a.first_seq + it.entry;
+  it.count = a.count[it.slot];
+  it.rows = it.count * a.G;
+  it.n_split = a.n_split[it.slot];
+  const int local = item - a.first_item[it.slot], x = local / it.n_split;
+  it.split = local - x * it.n_split;
+  it.row_tile = (it.rows + rows_per_tile - 1) / rows_per_tile - 1 - x;   // those that see most first
+  return it;
+}
+struct ChunkTier {
+  int tok, len;
+};
+__device__ __forceinline__ ChunkTier chunk_tier(const ChunkArgs &a, const ChunkItem &it, int t) {
+  if (t < a.n_prefix) return {a.prefix_tok[t], a.members >> it.seq & 1 ? a.prefix_len[t] : 0};
+  return {a.first_tok[t - a.n_prefix][it.slot], a.len[t - a.n_prefix][it.slot]};
+}
+// ---------------------------------------------------------------- rows
+struct ChunkRows {
+  float cs, inv_cs;
+  float m, l, mcs, far;   // as in Rows
+  float rounded;          // l of the rounded weights, where it is kept (0: it is not)
+  int token, hq, pos;     // new token, query head, place behind the oldest token
+  bool on;
+};
+__device__ __forceinline__ ChunkRows begin_chunk_rows(const ChunkArgs &a, const ChunkItem &it, int total, int row) {
+  ChunkRows r;
+  r.on = row < it.rows;
+  row = min(row, it.rows - 1);
+  r.token = token_of(a, row);
+  r.hq = it.hkv * a.G + row - r.token * a.G;
+  r.pos = total - it.count + r.token;
+  r.cs = a.scale * kLog2e;
+  r.inv_cs = 1.0f / r.cs;
+  r.m = r.far = -INFINITY;
+  r.l = r.mcs = r.rounded = 0.0f;
+  return r;
+}
+// The row's channels 16 kb + 8 hh .. + 7 in qf[kb], in the product's type.
+template <bool BF>
+__device__ __forceinline__ void load_query(const ChunkArgs &a, const ChunkItem &it, const ChunkRows &r, int hh, u32x4 (&qf)[8]) {
+  const u32x4 *qp = (const u32x4 *)(a.q + it.entry * a.q_seq + r.token * a.q_token + r.hq * a.q_head);
+#pragma unroll
+  for (int kb = 0; kb < 8; ++kb) qf[kb] = qp[2 * kb + hh];
+  if (!BF && a.q_fmt == TTKV_BF16)
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) to_fp16(qf[kb]);
+}
+template <bool BF>
+__device__ __forceinline__ void move_chunk_reference(ChunkRows &r, float mt, f16v (&o)[4]) {
+#pragma clang fp contract(off)
+  const float mn = fmaxf(r.m, mt), at = __builtin_rintf(mn * r.cs), was = r.mcs;
+  const bool unit = fabsf(at) < kFar;
+  r.mcs = mn == -INFINITY ? 0.0f : (unit ? unit16<BF>() : 0.0f) - at;
+  const float alpha = r.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(r.mcs - was);
+  r.l *= alpha;
+  r.rounded *= alpha;
+  rescale(o, alpha);
+  r.m = mn;
+  r.far = unit ? (at + kRoom16) * r.inv_cs : mn;
+}
+// Where a row is kept from a token whose value is infinite or no number, a weight of 0 would still make a NaN of it.  So in steps that not every row
+// of a tile sees such values go into LDS as 0 and into a list of bits, a byte for eight channels of a token, and a row that does see one gets
+// a NaN in that channel.
+struct Wild {
+  int step[2];                 // per buffer: the last step with such a value
+  __align__(16) uint8_t bits[2][32][16];
+};
+// Step's tokens below lim, by lane.
+__device__ __forceinline__ void spoil(f16v (&o)[4], const uint8_t (&bits)[32][16], int lim, int hh) {
+  u32x4 all = {0, 0, 0, 0};
+#pragma unroll 1
+  for (int t = 0; t < 32; ++t) {
+    const u32x4 w = *(const u32x4 *)bits[t];
+    if (t < lim) all |= w;
+  }
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)   // channel 32 d + 8 (i / 4) + 4 hh + i % 4
+      if (all[d] >> (8 * (i / 4) + 4 * hh + i % 4) & 1) o[d][i] = __builtin_nanf("");
+}
+
+// ---------------------------------------------------------------- a workgroup's part
+// RW waves of 32 rows each share the tokens' tiles, TW such teams take the steps of 32 tokens in turn.
+template <int RW, int TW>
+struct Share {
+  ChunkItem it;
+  int lane, tw, rw, c, hh, tid;      // tid: of the team
+  int row0;                          // of the wave
+  bool idle;                         // a wave without rows only helps with the tiles
+  int total, base;                   // tokens that the sequence attends; place of the first new one
+  int sees, tile_sees;               // tokens that the tile's last row sees, its first one
+  int first_sees, last_sees;         // of the wave's rows
+  int s0, s1;                        // this item's steps, tiers one behind the other
+  __device__ __forceinline__ explicit Share(const ChunkArgs &a) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63;
+    tw = wave / RW;
+    rw = wave % RW;
+    c = lane & 31;
+    hh = lane >> 5;
+    tid = threadIdx.x & (64 * RW - 1);
+    it = chunk_item(a, 32 * RW);
+    total = 0;
+    for (int t = 0; t < a.n_tiers; ++t) total += chunk_tier(a, it, t).len;
+    row0 = it.row_tile * 32 * RW + rw * 32;
+    idle = row0 >= it.rows;
+    base = total - it.count;
+    sees = max(0, base + 1 + token_of(a, min(it.row_tile * 32 * RW + 32 * RW, it.rows) - 1));
+    tile_sees = base + 1 + token_of(a, it.row_tile * 32 * RW);
+    first_sees = base + 1 + token_of(a, min(row0, it.rows - 1));
+    last_sees = base + 1 + token_of(a, min(row0 + 31, it.rows - 1));
+    int n_steps = 0, before = 0;
+    for (int t = 0; t < a.n_tiers; ++t) {
+      const int len = chunk_tier(a, it, t).len, n = min(max(sees - before, 0), len);
+      n_steps += (n + 31) / 32;
+      before += len;
+    }
+    const int per = ((n_steps + it.n_split - 1) / it.n_split + TW - 1) / TW * TW;
+    s0 = min(it.split * per, n_steps);
+    s1 = min(s0 + per, n_steps);
+  }
+  // f(tier, its run, its sequence, steps lo .. hi - 1 of it, tokens before it) for every quantized (or every other) tier that the item has
+  // steps of
+  template <typename F>
+  __device__ __forceinline__ void tiers(const ChunkArgs &a, bool quantized, F &&f) const {
+    int at = 0, before = 0;
+    for (int t = 0; t < a.n_tiers; ++t) {
+      const ChunkTier T = chunk_tier(a, it, t);
+      const int n = (min(max(sees - before, 0), T.len) + 31) / 32;
+      const int lo = max(s0 - at, 0), hi = min(s1 - at, n);
+      if (lo < hi && quantized == is_quant(a.tv[t].k_fmt)) f(a.tv[t], T, t < a.n_prefix ? 0 : it.seq, lo, hi, before);
+      at += n;
+      before += T.len;
+    }
+  }
+};
+
+// A team's rows of one tier on their way: steps mine, mine + TW, .. below hi; keys and values apart.
+template <int F, int RW, int TW>
+struct Stream {
+  static constexpr int NL = 8 / RW;   // pieces per thread and step
+  const Ring &ring;
+  Place at;
+  int step, hi, len, tid;
+  uint32_t codes, meta;               // offsets of the sections in the head's part
+  Piece<F> x[NL];
+  __device__ __forceinline__ Stream(const Ring &g, const Place &from, int mine, int hi_, int len_, int tid_, uint32_t codes_, uint32_t meta_)
+      : ring(g), at(from), step(mine), hi(hi_), len(len_), tid(tid_), codes(codes_), meta(meta_) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) x[i] = Piece<F>{};
+  }
+  __device__ __forceinline__ void load() {   // the next step, if there is one; behind the tier's end its last row
+    if (step >= hi) return;
+    const int last = min(31, len - 32 * step - 1);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) x[i] = load_piece<F>(at.head + codes, at.head + meta, at.row + min((tid >> 4) + 4 * RW * i, last), tid & 15);
+    step += TW;
+    if (step < hi) at.advance(ring, 32 * TW);
+  }
+  template <bool BF, bool TWO>
+  __device__ __forceinline__ void put(char *to, int row_bytes, int part_bytes) const {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      char *const p = to + ((tid >> 4) + 4 * RW * i) * row_bytes + (tid & 15) * 16;
+      put_piece<BF, F, TWO>(x[i], p, p + part_bytes);
+    }
+  }
+  // Values of step `of`; all_see: tokens of the tier that every row of the tile sees.
+  template <bool BF, bool TWO>
+  __device__ __forceinline__ void put_values(char *to, int part_bytes, int of, int all_see, Wild &wild, int buffer) const {
+    if (32 * of + 32 <= all_see) return put<BF, TWO>(to, kRowV, part_bytes);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = (tid >> 4) + 4 * RW * i;
+      char *const p = to + row * kRowV + (tid & 15) * 16;
+      const uint32_t bits = put_piece<BF, F, TWO, true>(x[i], p, p + part_bytes);
+      wild.bits[buffer][row][tid & 15] = (uint8_t)bits;
+      if (bits) wild.step[buffer] = of;
+    }
+  }
+};
+
+// The rounded weights 2 i and 2 i + 1 of a step.
+template <bool BF>
+__device__ __forceinline__ void weigh2(ChunkRows &r, const f16v &sc, int i, u32x4 (&p)[2]) {
+  const float w0 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i], r.cs, r.mcs)), w1 = __builtin_amdgcn_exp2f(fmaf(sc[2 * i + 1], r.cs, r.mcs));
+  r.l += w0 + w1;
+  p[i / 4][i % 4] = pack2<BF>(w0, w1);
+}
+
+// The sum of a step's weights as the values meet them.
+template <bool BF>
+__device__ __forceinline__ float rounded_sum(const u32x4 (&p)[2], float sum) {
+  constexpr uint32_t ones = BF ? 0x3f803f80u : 0x3c003c00u;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (BF) sum = __builtin_amdgcn_fdot2_f32_bf16(as_b2(p[i / 4][i % 4]), as_b2(ones), sum, false);
+    else sum = __builtin_amdgcn_fdot2(as_h2(p[i / 4][i % 4]), as_h2(ones), sum, false);
+  }
+  return sum;
+}
+
+// What the workgroup's rows come to: the teams' results meet, each wave ends with 128 / TW channels of its rows and stores them.
+template <bool ROUNDED, int RW, int TW>
+__device__ __forceinline__ void finish(const ChunkArgs &a, const Share<RW, TW> &w, ChunkRows &r, f16v (&o)[4], char *s_tile, float (*s_m)[32], float (*s_l)[32]) {
+  const int lane = w.lane, tw = w.tw, rw = w.rw, c = w.c, hh = w.hh;
+  const ChunkItem &it = w.it;
+  const int row0 = w.row0;
+  const f2 both = both32(r.l);
+  r.l = both.x + both.y;
+  float top = r.m == -INFINITY ? -INFINITY : -r.mcs, l = r.l;
+  if constexpr (ROUNDED) {
+    const f2 halves = both32(r.rounded);
+    if (halves.x + halves.y > 0.0f) rescale(o, l / (halves.x + halves.y));
+  }
+  constexpr int OWN = 4 / TW > 0 ? 4 / TW : 1;                   // blocks of 32 channels that a wave stores (TW <= 4)
+  if constexpr (TW > 1) {
+    __syncthreads();
+    if (hh == 0) {
+      s_m[tw * RW + rw][c] = top;
+      s_l[tw * RW + rw][c] = l;
+    }
+    auto place = [&](int giver, int taker, int e, int k) __attribute__((always_inline)) -> float4 * {   // [giver][taker but the giver][block][piece][lane]
+      const int slot = taker - (taker > giver);
+      return (float4 *)(s_tile + (((((giver * RW + rw) * (TW - 1) + slot) * OWN + e) * 4 + k) * 64 + lane) * 16);
+    };
+#pragma unroll
+    for (int t = 0; t < TW; ++t)
+      if (t != tw)
+#pragma unroll
+        for (int e = 0; e < OWN; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *place(tw, t, e, k) = float4{o[t * OWN + e][4 * k], o[t * OWN + e][4 * k + 1], o[t * OWN + e][4 * k + 2], o[t * OWN + e][4 * k + 3]};
+    __syncthreads();
+    top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < TW; ++u) top = fmaxf(top, s_m[u * RW + rw][c]);
+    float by[TW];
+    l = 0.0f;
+#pragma unroll
+    for (int u = 0; u < TW; ++u) {
+      const float mu = s_m[u * RW + rw][c];
+      by[u] = mu == -INFINITY ? (s_l[u * RW + rw][c] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(mu - top);   // (a sum that is no number stays none)
+      l = fmaf(s_l[u * RW + rw][c], by[u], l);
+    }
+#pragma unroll
+    for (int w = 0; w < TW; ++w) {
+      if (w != tw) continue;
+#pragma unroll
+      for (int e = 0; e < OWN; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          f16v &x = o[w * OWN + e];
+          float y[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y[j] = x[4 * k + j] * by[w];
+#pragma unroll
+          for (int u = 0; u < TW; ++u) {
+            if (u == w) continue;
+            const float4 z = *place(u, w, e, k);
+            y[0] = fmaf(z.x, by[u], y[0]);
+            y[1] = fmaf(z.y, by[u], y[1]);
+            y[2] = fmaf(z.z, by[u], y[2]);
+            y[3] = fmaf(z.w, by[u], y[3]);
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[4 * k + j] = y[j];
+        }
+    }
+  }
+  if (!r.on) return;
+  // channels 32 d + 8 k + 4 hh .. + 3 of the row lie in registers 4 k .. + 3 of block d
+  if (a.part_stride) {
+    const int64_t at_part = (((int64_t)a.row_base[it.slot] + row0 + c) * a.Hkv + it.hkv) * a.part_stride + it.split;
+    float *const po = a.pacc + at_part * 128 + 4 * hh;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      if (TW > 1 && d / OWN != tw) continue;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) *(float4 *)(po + 32 * d + 8 * k) = float4{o[d][4 * k], o[d][4 * k + 1], o[d][4 * k + 2], o[d][4 * k + 3]};
+    }
+    if (hh == 0 && tw == 0) {
+      a.pm[at_part] = top;     // weights are exp2(score cs - this)
+      a.pl[at_part] = l;
+    }
+    return;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  uint8_t *const out = a.out + it.entry * a.o_seq + r.token * a.o_token + r.hq * a.o_head + 8 * hh;
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if (TW > 1 && d / OWN != tw) continue;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      u32x2 w;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const float x = o[d][4 * k + 2 * j] * inv, y = o[d][4 * k + 2 * j + 1] * inv;
+        w[j] = a.out_fmt == TTKV_BF16 ? pack2<true>(x, y) : pack2<false>(x, y);
+      }
+      *(u32x2 *)(out + 64 * d + 16 * k) = w;
+    }
+  }
+  if (a.lse && hh == 0 && tw == 0)
+    a.lse[((int64_t)it.entry * a.n_tokens + r.token) * a.Hq + r.hq] = l == 0.0f ? -INFINITY : (__builtin_amdgcn_logf(l) + top) * kLn2;
+}
+
+// run(key format, value format, ..) for every tier that the item has steps of, the quantized ones first.  Their weights are fp16 numbers and carry that
+// type's power of two; beside bf16 tiers it changes in between.
+template <bool BF, int Q, int RW, int TW, typename R>
+__device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW> &w, ChunkRows &r, f16v (&o)[4], u32x4 (&qf)[8], R &run) {
+  constexpr int FP = BF ? TTKV_BF16 : TTKV_F16;
+  if constexpr (Q != 0) {
+    load_query<false>(a, w.it, r, w.hh, qf);
+    w.tiers(a, true, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+      if constexpr ((Q & kInt4) != 0)
+        if (Q == kInt4 || tv.k_fmt == TTKV_I4_ASYM_G64) return run(num<TTKV_I4_ASYM_G64>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
+      if constexpr ((Q & kInt84) != 0)
+        if (Q == kInt84 || tv.v_fmt == TTKV_I4_ASYM_G64) return run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I4_ASYM_G64>{}, tv, T, seq, lo, hi, ahead);
+      if constexpr ((Q & kInt8) != 0) run(num<TTKV_I8_SYM_G32>{}, num<TTKV_I8_SYM_G32>{}, tv, T, seq, lo, hi, ahead);
+    });
+    if constexpr (BF) {
+      constexpr float step = unit16<true>() - unit16<false>();
+      if (fabsf(r.mcs) < kFar) {   // (a reference beyond carries none)
+        const float by = __builtin_amdgcn_exp2f(step);
+        if (r.m != -INFINITY) r.mcs += step;
+        r.l *= by;
+        rescale(o, by);
+      }
+    }
+  }
+  if constexpr (BF || Q == 0) load_query<BF>(a, w.it, r, w.hh, qf);
+  w.tiers(a, false, [&](const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    run(num<FP>{}, num<FP>{}, tv, T, seq, lo, hi, ahead);
+  });
+}
+
+// ---------------------------------------------------------------- few rows
+// Bound: memory.  Keys of one step and values of the one before are on their way while one is computed.  The outputs are divided by the sum of the
+// weights as they were rounded: where a token or two have most of the weight, their rounding then cancels.  With quantized tiers LDS holds one step
+// only, so that a CU has two workgroups: one decompresses while the other computes.
+template <bool BF, int Q, bool V2, int RW, int TW>
+__global__ __launch_bounds__(64 * RW * TW, Q ? 2 : 1) void chunk_kernel(const ChunkArgs a) {
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kStep = kPartsK * kKeys + kPartsV * kValues;
+  constexpr int kBuffers = Q ? 1 : 2;
+  __shared__ __align__(16) char s_tile[TW * kBuffers * kStep];   // per team: keys and values of two steps (one); at the end what the waves exchange
+  static_assert(TW * kBuffers * kStep >= TW * RW * (16 - 16 / TW) * 1024, "room for what the waves exchange");
+  __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
+  __shared__ Wild s_wild[TW];
+  const Share<RW, TW> w(a);
+  u32x4 qf[8];
+  ChunkRows r = begin_chunk_rows(a, w.it, w.total, w.row0 + w.c);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) o[d] = f16v{};
+  char *const team = s_tile + w.tw * kBuffers * kStep;
+  const char *const k_at = team + k_lane(w.lane), *const v_at = team + kPartsK * kKeys + v_lane(w.lane);
+
+  auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF) && V2, BT = BF && !is_quant(KF);   // the product's type: quantized tiers in fp16
+    const int mine = lo + w.tw;
+    const Ring ring(tv, seq, w.it.hkv);
+    const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    Wild &wild = s_wild[w.tw];
+    auto put_values = [&](int at, int step) __attribute__((always_inline)) {
+      values.template put_values<BT, two_v>(team + at + kPartsK * kKeys, kValues, step, w.tile_sees - ahead, wild, at != 0);
+    };
+    auto put_keys = [&](int at) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + at, kRowK, kKeys); };
+    auto works = [&](int s) __attribute__((always_inline)) { return s < hi && !w.idle && 32 * s < w.last_sees - ahead; };   // (wave-uniform)
+    auto scores = [&](int at, f16v &sc) __attribute__((always_inline)) {
+#pragma unroll
+      for (int kb = 0; kb < 8; ++kb) {
+        sc = mma<BT>(*(const u32x4 *)(k_at + at + 32 * kb), qf[kb], sc);
+        if constexpr (two_k) sc = mma<BT>(*(const u32x4 *)(k_at + at + kKeys + 32 * kb), qf[kb], sc);
+      }
+    };
+    auto attend = [&](int at, int s, f16v &sc) __attribute__((always_inline)) {
+      const int lim = min(r.pos + 1 - ahead, T.len) - 32 * s;
+      if (32 * s + 32 > min(w.first_sees - ahead, T.len)) mask_from(sc, lim, w.hh);
+      const float mt = step_max(sc);
+      if (__any(mt > r.far)) move_chunk_reference<BT>(r, mt, o);
+      u32x4 p[2];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) weigh2<BT>(r, sc, i, p);
+      if constexpr (Q == 0) r.rounded = rounded_sum<BT>(p, r.rounded);
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          o[d] = mma<BT>(value_operand(v_at + at, d, b), p[b], o[d]);
+          if constexpr (two_v) o[d] = mma<BT>(value_operand(v_at + at + kValues, d, b), p[b], o[d]);
+        }
+      if (32 * s + 32 > w.tile_sees - ahead && wild.step[at != 0] == s) spoil(o, wild.bits[at != 0], lim, w.hh);
+    };
+    __syncthreads();   // everybody is done with the tier before
+    keys.load();
+    values.load();
+    if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
+    __syncthreads();
+    const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
+    if constexpr (Q != 0) {
+      for (int t = 0; t < n_it; ++t) {
+        const int s = mine + TW * t;
+        put_keys(0);
+        put_values(0, s);
+        keys.load();
+        values.load();
+        __syncthreads();
+        if (works(s)) {
+          f16v sc = {};
+          scores(0, sc);
+          attend(0, s, sc);
+        }
+        __syncthreads();
+      }
+    } else {
+      put_keys(0);
+      keys.load();
+      put_values(0, mine);
+      values.load();
+      int now = 0;
+      for (int t = 0; t < n_it; ++t) {
+        __syncthreads();   // the step is in its buffer; everybody is done with the other one
+        const int next = kStep - now, s = mine + TW * t;
+        const bool on = works(s);
+        f16v sc = {};
+        if (on) scores(now, sc);
+        put_keys(next);
+        keys.load();
+        if (on) attend(now, s, sc);
+        put_values(next, s + TW);
+        values.load();
+        now = next;
+      }
+    }
+  };
+  each_tier<BF, Q>(a, w, r, o, qf, run);
+  finish<Q == 0>(a, w, r, o, s_tile, s_m, s_l);
+}
+
+// Keeps a step's products and its softmax side by side: after every product some vector instructions and the next operands' loads.
+template <bool TWO_K, bool TWO_V>
+__device__ __forceinline__ void interleave() {
+  constexpr int pairs = 1 + (TWO_K && TWO_V), vector = 6 / (2 * pairs);
+  __builtin_amdgcn_sched_group_barrier(0x100, 9, 0);
+#pragma unroll
+  for (int i = 0; i < 8 * pairs; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, vector, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, vector, 0);
+  }
+}
+
+// ---------------------------------------------------------------- many rows
+// Bound: the matrix cores and the vector unit alike.  The steps overlap inside a wave: while the softmax of step s runs on the vector
+// unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  LDS holds two steps' keys and values (s + 1 and
+// s + 2; s - 1 and s), one barrier per step.
+template <bool BF, int Q, bool V2, int RW, int TW>
+__global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
+  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 2 * (kPartsK * kKeys + kPartsV * kValues);
+  __shared__ __align__(16) char s_tile[TW * kTeam];              // per team: keys of even and odd steps, values of even and odd steps
+  __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
+  __shared__ Wild s_wild[TW];
+  const Share<RW, TW> w(a);
+  u32x4 qf[8];
+  ChunkRows r = begin_chunk_rows(a, w.it, w.total, w.row0 + w.c);
+  f16v o[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) o[d] = f16v{};
+  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 2 * kPartsK * kKeys;
+  const char *const k_at = team + k_lane(w.lane), *const v_at = team_v + v_lane(w.lane);
+
+  auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
+    constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
+    constexpr bool two_k = is_quant(KF), two_v = is_quant(VF) && V2, BT = BF && !is_quant(KF);   // the product's type: quantized tiers in fp16
+    const int mine = lo + w.tw;
+    const Ring ring(tv, seq, w.it.hkv);
+    const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
+    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    const int seen_by_all = min(w.first_sees - ahead, T.len), seen = w.idle ? 0 : min(32 * hi, w.last_sees - ahead);   // by the wave's rows
+    const int lim = min(r.pos + 1 - ahead, T.len);
+    auto put_keys = [&](int odd) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + odd * kPartsK * kKeys, kRowK, kKeys); };
+    Wild &wild = s_wild[w.tw];
+    auto put_values = [&](int odd, int step) __attribute__((always_inline)) {
+      values.template put_values<BT, two_v>(team_v + odd * kPartsV * kValues, kValues, step, w.tile_sees - ahead, wild, odd);
+    };
+    auto score = [&](f16v &x, int odd, int kb) __attribute__((always_inline)) {
+      const char *const k = k_at + odd * kPartsK * kKeys + 32 * kb;
+      x = mma<BT>(*(const u32x4 *)k, qf[kb], x);
+      if constexpr (two_k) x = mma<BT>(*(const u32x4 *)(k + kKeys), qf[kb], x);
+    };
+    auto value = [&](int odd, int d, int b, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+      const char *const v = v_at + odd * kPartsV * kValues;
+      o[d] = mma<BT>(value_operand(v, d, b), p[b], o[d]);
+      if constexpr (two_v) o[d] = mma<BT>(value_operand(v + kValues, d, b), p[b], o[d]);
+    };
+    // The weights of step s meet its values, by themselves.
+    auto flush = [&](int odd, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) value(odd, d, b, p);
+    };
+    auto spoil_by = [&](int odd, int s) __attribute__((always_inline)) {
+      if (32 * s + 32 > w.tile_sees - ahead && wild.step[odd] == s) spoil(o, wild.bits[odd], lim - 32 * s, w.hh);
+    };
+    // Step s, in buffers ODD: sc its scores, p the weights of the step before (zeros where its values are added already); next and pn receive
+    // the next step's scores and its own weights.
+    auto body = [&](int s, auto odd_tag, f16v &sc, f16v &next, u32x4 (&p)[2], u32x4 (&pn)[2], bool &pending) __attribute__((always_inline)) {
+      constexpr int ODD = decltype(odd_tag)::value;
+      __syncthreads();   // keys of the next step and values of the one before are there; everybody is done with those of this one and the one before that
+      if (pending) spoil_by(1 - ODD, s - TW);
+      const bool works = 32 * s < seen;   // (wave-uniform)
+      const float mt = step_max(sc);
+      const bool moves = works && __any(mt > r.far);
+      if (moves || !works) {
+        if (pending) flush(1 - ODD, p);
+        p[0] = p[1] = u32x4{0, 0, 0, 0};
+        if (moves) move_chunk_reference<BT>(r, mt, o);
+      }
+      put_keys(ODD);
+      put_values(ODD, s);
+      keys.load();
+      values.load();
+      if (works) {
+        f16v nx = {};
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
+          value(1 - ODD, g / 2, g % 2, p);
+          score(nx, 1 - ODD, g);
+          weigh2<BT>(r, sc, g, pn);
+        }
+        // (kept here: the weights are wanted in the next step only, and would be worked out there, behind the products)
+        asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(r.l));
+        interleave<two_k, two_v>();
+        if (32 * (s + TW) + 32 > seen_by_all) mask_from(nx, lim - 32 * (s + TW), w.hh);
+        next = nx;
+      }
+      pending = works;
+    };
+    u32x4 p0[2], p1[2];
+    p0[0] = p0[1] = u32x4{0, 0, 0, 0};
+    __syncthreads();   // everybody is done with the tier before
+    // there is no step before the first: weights of zero meet zeros
+    for (int i = w.tid; i < kPartsV * kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + kPartsV * kValues))[i] = u32x4{0, 0, 0, 0};
+    if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
+    keys.load();
+    put_keys(0);
+    keys.load();
+    put_keys(1);
+    keys.load();
+    values.load();
+    __syncthreads();
+    f16v s0 = {}, s1 = {};
+#pragma unroll
+    for (int kb = 0; kb < 8; ++kb) score(s0, 0, kb);
+    if (32 * mine + 32 > seen_by_all) mask_from(s0, lim - 32 * mine, w.hh);
+    bool pending = false;
+    const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
+    for (int t = 0; t < n_it; t += 2) {
+      body(mine + TW * t, num<0>{}, s0, s1, p0, p1, pending);
+      body(mine + TW * (t + 1), num<1>{}, s1, s0, p1, p0, pending);
+    }
+    __syncthreads();
+    if (pending) {
+      spoil_by(1, mine + TW * ((n_it + 1) / 2 * 2 - 1));
+      flush(1, p0);
+    }
+  };
+  each_tier<BF, Q>(a, w, r, o, qf, run);
+  finish<false>(a, w, r, o, s_tile, s_m, s_l);
+}
+
+template <bool BF, int Q, bool V2>
+void start(const ChunkArgs &a, int rows, hipStream_t s) {
+  const dim3 grid((unsigned)a.n_items * (unsigned)a.Hkv);
+  if (rows == 256) hipLaunchKernelGGL((chunk_rows_kernel<BF, Q, V2, 8, 1>), grid, dim3(512), 0, s, a);
+  else if (rows == 128) hipLaunchKernelGGL((chunk_rows_kernel<BF, Q, V2, 4, 2>), grid, dim3(512), 0, s, a);
+  else if constexpr (Q != 0) hipLaunchKernelGGL((chunk_kernel<BF, Q, V2, 2, 2>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((chunk_kernel<BF, Q, V2, 2, 4>), grid, dim3(512), 0, s, a);
+}
+// Values in two numbers for fp16 outputs.
+template <int Q>
+void start_quantized(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream) {
+  const bool fine = a.out_fmt == TTKV_F16;
+  if (s.bf) fine ? start<true, Q, true>(a, s.rows, stream) : start<true, Q, false>(a, s.rows, stream);
+  else fine ? start<false, Q, true>(a, s.rows, stream) : start<false, Q, false>(a, s.rows, stream);
+}
+
+}  // namespace chunk
+}  // namespace ttkv

@@ -393,11 +393,18 @@ struct ChunkArgs {
 };
 static_assert(sizeof(ChunkArgs) <= 4096, "kernel arguments are passed by value");
 // Query rows per workgroup, and the kernels that a launch takes.
+constexpr int kInt8 = 1, kInt4 = 2, kInt84 = 4;   // formats of quantized tiers: K / V int8 / int8, int4 / int4, int8 / int4
+inline int quantized_kind(int k_fmt, int v_fmt) { return is_fp(k_fmt) ? 0 : k_fmt == TTKV_I4_ASYM_G64 ? kInt4 : v_fmt == TTKV_I4_ASYM_G64 ? kInt84 : kInt8; }
 struct ChunkShape {
   int rows;
-  bool bf, quantized;
+  bool bf;
+  int quantized;   // the formats of the tiers that hold tokens
 };
-ChunkShape chunk_shape(int64_t most_rows, bool bf, bool quantized);
+ChunkShape chunk_shape(int64_t most_rows, bool bf, int quantized);
+void start_chunk_i8(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+void start_chunk_i4(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+void start_chunk_k8v4(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
+void start_chunk_mixed(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
 int64_t chunk_least_steps(const ChunkShape &s);   // of 32 tokens, that an item should have
 int64_t chunk_resident(const ChunkShape &s);      // workgroups on the chip at once
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);

@@ -32,6 +32,9 @@ struct ChunkItem {
   int count, rows;   // new tokens, query rows
 };
 __device__ __forceinline__ ChunkItem chunk_item(const ChunkArgs &a, int rows_per_tile) {
+  // all that the look-ups read, asked for at once: a launch's arguments are in no cache when its first workgroups start
+  asm volatile("" ::"s"(a.Hkv), "s"(a.n_tiers), "s"(a.q), "s"(a.q_seq), "s"(a.tv[0].base), "s"(a.tv[0].bt), "s"(a.first_item[0]), "s"(a.count[0]),
+               "s"(a.row_base[0]), "s"(a.n_split[0]), "s"(a.entry[0]), "s"(a.first_tok[0][0]), "s"(a.len[0][0]), "s"(a.prefix_len[0]));
   ChunkItem it;
   const uint32_t id = blockIdx.x;
   const int item = a.Hkv == 1 ? id : a.hkv_magic ? (int)mul_high(id, a.hkv_magic) : (int)(id / (uint32_t)a.Hkv);

@@ -411,7 +411,7 @@ ttkv_status ttkv_decode_step_shared(ttkv_handle h, ttkv_cache *c, const ttkv_cac
  *   prefix  a cache of batch 1 that the sequences with a non-zero entry in member [host] [batch] (NULL: all) attend in front of their own
  *           tokens, or NULL; conditions as in ttkv_decode_step_shared.
  *   Tiers   in device memory, fp16 or bf16 (not both in one call) and row-wise quantized (K / V int8 / int8, int4 / int4 or int8 / int4); keys
- *           grouped over tokens, values stored channel-major and host tiers: UNSUPPORTED.  Keys and values of quantized tiers are
+ *           grouped over tokens, values stored channel-major, host tiers and blocks of more than 2^21 tokens: UNSUPPORTED.  Keys and values of quantized tiers are
  *           worked on as fp16 numbers: they end at 131008 (values for bf16 outputs at 65504).
  *   q       [entry][token][n_q_heads][128], F16 or BF16 (a BF16 tier needs BF16; otherwise |q| below 65504);
  *   out     the same shape, F16 or BF16: rounded once from fp32.  Softmax weights meet the values rounded to the product's type (fp16; bf16
@@ -436,7 +436,7 @@ size_t ttkv_chunk_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t se
  *   n_fresh [host] per entry: so many of the sequence's newest tokens begin at 0, whatever their places hold (NULL: the chunk's own).
  *   weights [device] fp32 [pool_blocks][n_kv_heads][block_tokens], beside the tier's records.
  *   workspace [device], ttkv_weights_workspace_bytes (0: invalid arguments): partial sums, where many rows meet few tokens.
- * Tiers in device memory whose keys are fp16, bf16, int8 or int4 (UNSUPPORTED otherwise).  The order of each sum is fixed. */
+ * Tiers in device memory whose keys are fp16, bf16, int8 or int4, blocks of up to 2^21 tokens (UNSUPPORTED otherwise).  The order of each sum is fixed. */
 ttkv_status ttkv_add_weights(ttkv_handle h, const ttkv_cache *c, int32_t tier, int32_t seq, const ttkv_heads *q, const float *lse,
                              int64_t n_tokens, const int64_t *n_each, const int64_t *n_fresh, float *weights, void *workspace,
                              size_t ws_bytes, void *stream);
@@ -452,7 +452,7 @@ size_t ttkv_weights_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t 
  *   swap 0: the freed blocks leave the tier (start[], len[]).  swap != 0: rows change places and nothing leaves: the tier's oldest blocks
  *   then hold the lightest tokens, which ttkv_tier_demote / ttkv_evict take into the next tier.
  *   workspace [device], ttkv_evict_light_workspace_bytes (0: invalid arguments).
- * Device tiers of formats stored by rows (fp16, bf16, int8, int4) without mean keys; UNSUPPORTED otherwise. */
+ * Device tiers of formats stored by rows (fp16, bf16, int8, int4) without mean keys, blocks of up to 2^21 tokens; UNSUPPORTED otherwise. */
 ttkv_status ttkv_evict_light(ttkv_handle h, ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent, int32_t swap, float *weights,
                              void *workspace, size_t ws_bytes, void *stream);
 size_t ttkv_evict_light_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent);

@@ -1662,6 +1662,8 @@ struct ChunkPlan {
   int64_t rows;        // query rows per KV head, all sequences
   size_t ws_bytes;     // partials
 };
+// Offsets inside a KV head's part of a block are counted in 32 bits.
+constexpr int32_t kLargestBlock = 1 << 21;
 int64_t held_tokens(const ttkv_cache *c, int b) {
   int64_t n = 0;
   for (int t = 0; t < c->n_tiers; ++t) n += c->tier[t].len[b];
@@ -1672,7 +1674,7 @@ ttkv_status check_chunk_tiers(const ttkv_cache *c, bool &f16, bool &bf16) {
   for (int t = 0; t < c->n_tiers; ++t) {
     const ttkv_tier &T = c->tier[t];
     const bool fp = is_fp(T.k_fmt) && T.k_fmt == T.v_fmt;
-    if (T.mem != TTKV_MEM_DEVICE || !(fp || shared_quant_fits(T.k_fmt, T.v_fmt))) return TTKV_ERR_UNSUPPORTED;
+    if (T.block_tokens > kLargestBlock || T.mem != TTKV_MEM_DEVICE || !(fp || shared_quant_fits(T.k_fmt, T.v_fmt))) return TTKV_ERR_UNSUPPORTED;
     f16 |= T.k_fmt == TTKV_F16;
     bf16 |= T.k_fmt == TTKV_BF16;
   }
@@ -1868,7 +1870,8 @@ ttkv_status plan_weigh(const ttkv_cache *c, bool check_tables, int32_t tier, int
   if (tier < 0 || tier >= c->n_tiers || seq < -1 || seq >= c->batch || n_tokens < 0) return TTKV_ERR_INVALID_ARG;
   if (n_tokens > TTKV_MAX_CHUNK_TOKENS) return TTKV_ERR_UNSUPPORTED;
   const ttkv_tier &T = c->tier[tier];
-  if (T.mem != TTKV_MEM_DEVICE || !(is_fp(T.k_fmt) || T.k_fmt == TTKV_I8_SYM_G32 || T.k_fmt == TTKV_I4_ASYM_G64)) return TTKV_ERR_UNSUPPORTED;
+  if (T.block_tokens > kLargestBlock || T.mem != TTKV_MEM_DEVICE) return TTKV_ERR_UNSUPPORTED;
+  if (!is_fp(T.k_fmt) && T.k_fmt != TTKV_I8_SYM_G32 && T.k_fmt != TTKV_I4_ASYM_G64) return TTKV_ERR_UNSUPPORTED;
   const int b0 = seq < 0 ? 0 : seq, n_seq = seq < 0 ? c->batch : 1;
   WeighArgs &a = P.a;
   a.Hq = c->n_q_heads;
@@ -1969,7 +1972,7 @@ ttkv_status plan_light(const ttkv_cache *c, bool check_tables, int32_t tier, int
   if (tier < 0 || tier >= c->n_tiers || recent < 0 || keep < recent) return TTKV_ERR_INVALID_ARG;
   const ttkv_tier &T = c->tier[tier];
   auto by_row = [](int f) { return is_fp(f) || f == TTKV_I8_SYM_G32 || f == TTKV_I4_ASYM_G64; };
-  if (T.mem != TTKV_MEM_DEVICE || !by_row(T.k_fmt) || !by_row(T.v_fmt) || T.k_sum) return TTKV_ERR_UNSUPPORTED;
+  if (T.block_tokens > kLargestBlock || T.mem != TTKV_MEM_DEVICE || !by_row(T.k_fmt) || !by_row(T.v_fmt) || T.k_sum) return TTKV_ERR_UNSUPPORTED;
   const Layout L = make_layout(T, c->n_kv_heads);
   a.Hkv = c->n_kv_heads;
   a.kc = L.kc; a.km = L.km; a.vc = L.vc; a.vm = L.vm;

@@ -126,3 +126,12 @@ def test_eviction_refusals(h):  # noqa: F811
     c.tier[0].k_sum = c.tier[0].k_summary = None
     c.tier[0].mem = B.MEM_HOST_PINNED
     assert light(h, c) == B.ERR_UNSUPPORTED and B.ttkv_evict_light_workspace_bytes(h, c, 0, 64, 8) == 0
+
+
+def test_blocks_beyond_32_bits(h):  # noqa: F811
+    """A KV head's part of a block of 2^22 tokens has more bytes than 31 bits count."""
+    c = cache(lens=(0, 0))
+    c.tier[0].block_tokens, c.tier[0].ring_blocks, c.tier[0].pool_blocks, c.tier[0].capacity_tokens = 1 << 22, 2, 4, 1 << 23
+    assert chunk(h, c, T=0) == B.ERR_UNSUPPORTED and weigh(h, c, T=0) == B.ERR_UNSUPPORTED and light(h, c) == B.ERR_UNSUPPORTED
+    c.tier[0].block_tokens = c.tier[0].capacity_tokens = 1 << 21
+    assert chunk(h, c, T=0) == B.OK and weigh(h, c, T=0) == B.OK and light(h, c) == B.OK

@@ -266,6 +266,7 @@ class TieredCache:
         n = k.shape[-2]
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
+        self._unweighed(tier)
         if self.cfg[tier].mem == "host" and self.host_append_direct:
             # no staging: the conversion kernels store into the pinned records
             B.ttkv_quantize_append_host(self.h, self.c, tier, seq, k, v, fmt, n, int(through_tiers), None, 0, self._compute())
@@ -297,9 +298,11 @@ class TieredCache:
         if first_pos is None and positions is None and (self.prefix is not None or self.evicted.any()):
             first_pos = sum(self.len) + self.evicted
             if self.prefix is not None:
-                first_pos = first_pos + (1 if self.members is None else self.members) * int(sum(x[0] for x in self.prefix.len))
+                ahead = int(sum(x[0] for x in self.prefix.len) + self.prefix.evicted[0])
+                first_pos = first_pos + (1 if self.members is None else self.members) * ahead
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
         shape = (n, T, self.Hkv, 128)
+        self._unweighed(tier)
         B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, shape, dev), _heads(v, shape, dev), T, _host_int64(counts, n),
                            _host_int64(first_pos, n), _device_positions(positions, n, T, dev), self._compute())
         self._parts_age = None            # lengths jump: count the parts again at the next step
@@ -329,6 +332,8 @@ class TieredCache:
     def decode(self, q, selected=None, overlap=True, new=None):
         """q [B][Hq][128] f16/bf16 on the device.  selected: None or (sel_blocks, sel_count) pinned int32 tensors.
         new: None, or (k_new, v_new) [B][Hkv][1][128] of the step's token, appended to tier 0 by the same call."""
+        if new is not None:
+            self._unweighed(0)
         if self.prefix is not None:
             assert selected is None, "blocks are not selected behind a prefix"
             return self._decode_shared(q, new)
@@ -517,6 +522,11 @@ class TieredCache:
         return out, lse
 
     # ------------------------------------------------------------------ weights of tokens
+    def _unweighed(self, tier):
+        """Before tokens are appended: what lies behind the newest token held has not been weighed (tokens may have been taken back)."""
+        if self.weights[tier] is not None:
+            np.minimum(self._weighed[tier], self.start[tier] + self.len[tier], out=self._weighed[tier])
+
     @_on_own_device
     def add_weights(self, q, lse, counts=None, fresh=None, tier=0, seq=-1):
         """Adds to self.weights[tier] what the newest tokens' queries give each token (ttkv_add_weights): q [B][T][Hq][128] (or [B][Hq][128]
@@ -541,7 +551,7 @@ class TieredCache:
     @_on_own_device
     def evict_light(self, keep, recent, tier=0, swap=False):
         """Frees the tier's oldest blocks, as many as leave every sequence at least `keep` tokens: per KV head the tokens of least weight go, the
-        `recent` newest stay (ttkv_evict_light).  swap: nothing goes; the light tokens lie in the oldest blocks afterwards, for demote()."""
+        `recent` newest stay, the others have been weighed (ttkv_evict_light).  swap: nothing goes; the light tokens lie in the oldest blocks afterwards, for demote()."""
         assert self.weights[tier] is not None, "the tier keeps no weights"
         held, stream = self.len[tier].copy(), self._compute()
         self._with_workspace("light", lambda ws, size: B.ttkv_evict_light(self.h, self.c, tier, keep, recent, swap, self.weights[tier], ws, size, stream),
@@ -573,6 +583,7 @@ class TieredCache:
         assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
         assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128)
         stride = self._select_buffers(k)
+        self._unweighed(0)
         # The split of a selection is planned inside the call, which refuses a workspace that is too small for it before
         # anything is enqueued: the workspace is sized once from a dense plan's parts and grows when it is refused (no
         # run is cut finer than into items of 128 tokens, which bounds it).

@@ -258,3 +258,64 @@ def test_a_refused_chunk_leaves_the_cache_as_it_was():
         c.prefill(rotary, q, k, v, dtype=torch.float32)           # results are 16 bits wide
     assert e.value.status == B.ERR_UNSUPPORTED and (c.len[0] == held).all()
     c.close()
+
+
+@pytest.mark.parametrize("T", [3, 30, 100])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_every_format_at_once(T, dtype):
+    """All quantized formats in one call, some of them a prefix's."""
+    p = make_cache(1, (8, 2), [("i4", [100]), ("k8v4", [65])], seed=40)
+    c = make_cache(3, (8, 2), [(dtype, [T, 1, 70]), ("i8", [0, T, 300]), ("i4", [200, 0, 31])], prefix=p, members=[1, 0, 1], paged=True)
+    q = rnd(4, 3, T, 8, 128, dtype=dtype)
+    counts = [T, T, T - 1]
+    check(c, q, *attend(c, q, counts), counts=counts, untouched=7.0)
+    c.close()
+    p.close()
+
+
+def test_places_beyond_32_bits():
+    """Rows of the pool, of the queries and of the results more than 4 GiB apart; a run that begins at the pool's end."""
+    c = make_cache(1, (8, 8), [("f16", [300])], spare=20000)
+    assert c.pool[0].numel() > 1 << 32
+    far = torch.empty(2, 2 ** 31 + 1024, dtype=torch.float16, device=DEV)
+    few, many = rnd(1, 1, 3, 8, 128), rnd(2, 1, 270, 8, 128)
+    for q in (few, many):
+        check(c, q, *attend(c, q))
+    c.close()
+    c = make_cache(2, (8, 2), [("f16", [300, 200])])
+    for T in (3, 100):
+        n = T * 8 * 128
+        q, out = far[:, :n].view(2, T, 8, 128), far[:, n:2 * n].view(2, T, 8, 128)
+        q.copy_(rnd(3, 2, T, 8, 128))
+        o, lse = c.attend_chunk(q, out=out)
+        check(c, q, o, lse)
+    c.close()
+
+
+def test_blocks_that_are_divided_by():
+    """Rings so long, blocks so large that places are found by a division."""
+    c = make_cache(1, (2, 1), [("i4", [9000])], block=1 << 20, spare=8)
+    assert c.cfg[0].ring_blocks * 2 ** 20 // 64 * 2 ** 14 >= 1 << 31
+    for T in (2, 200):
+        q = rnd(T, 1, T, 2, 128)
+        check(c, q, *attend(c, q))
+    c.close()
+
+
+def test_positions_behind_a_prefix_that_was_thinned_out():
+    from paper_2604_19769_amd.cache import Rotary, TierConfig, TieredCache
+    p = TieredCache(1, 8, 2, [TierConfig("f16", "f16", 10 ** 9, 64, 6, weights=True)])
+    c = TieredCache(2, 8, 2, [TierConfig("f16", "f16", 10 ** 9, 64, 6)], prefix=p, members=[True, False])
+    rotary = Rotary(Rotary.frequencies(128))
+    q, k, v = rnd(1, 1, 300, 8, 128), rnd(2, 1, 300, 2, 128), rnd(3, 1, 300, 2, 128)
+    _, lse = p.prefill(rotary, q, k, v)
+    p.add_weights(rotary.apply(q)[0], lse)
+    p.evict_light(100, 20)
+    assert p.len[0][0] == 108 and p.evicted[0] == 192
+    q, k, v = rnd(4, 2, 9, 8, 128), rnd(5, 2, 9, 2, 128), rnd(6, 2, 9, 2, 128)
+    turned, _ = rotary.apply(q, first_pos=[300, 0])
+    out, lse = c.prefill(rotary, q, k, v)
+    torch.cuda.synchronize()
+    check(c, turned, out, lse)
+    c.close()
+    p.close()

@@ -157,6 +157,97 @@ def test_step_after_step():
     c.close()
 
 
+@pytest.mark.parametrize("fmt", ["f16", "bf16", "i8", "i4"])
+@pytest.mark.parametrize("heads,T,lens", [((8, 8), 2, [70000, 100]), ((8, 4), 60, [17000, 300]), ((4, 1), 100, [300, 1000]), ((4, 4), 270, [17000, 1])])
+def test_every_way_to_cut_it(fmt, heads, T, lens):
+    """Few rows with several tiles of tokens to an item, a hundred rows, many rows that items share, many rows over many tokens."""
+    dtype = "bf16" if fmt == "bf16" else "f16"
+    c = make_cache(2, heads, [(fmt, lens)], weights=True, paged=True)
+    q = rnd(2, 2, T, heads[0], 128, dtype=dtype)
+    _, lse = c.attend_chunk(q)
+    before = start_weights(c)
+    c.add_weights(q, lse, fresh=[5, lens[1]])
+    check_added(c, before, q, lse, None, [5, lens[1]], part=dtype)
+    c.close()
+
+
+def test_places_beyond_32_bits():
+    c = make_cache(1, (8, 8), [("f16", [300])], spare=20000, weights=True)
+    assert c.pool[0].numel() > 1 << 32
+    for T in (3, 270):
+        q = rnd(T, 1, T, 8, 128)
+        _, lse = c.attend_chunk(q)
+        before = start_weights(c)
+        c.add_weights(q, lse, fresh=[0])
+        check_added(c, before, q, lse, None, [0])
+    evict_and_check(c, 100, 20)
+    c.close()
+
+
+def test_places_that_are_divided_for():
+    c = make_cache(1, (2, 1), [("i4", [9000])], block=1 << 20, spare=8, weights=True)
+    assert c.cfg[0].ring_blocks * 2 ** 20 // 64 * 2 ** 14 >= 1 << 31
+    for T in (3, 270):
+        q = rnd(T, 1, T, 2, 128)
+        _, lse = c.attend_chunk(q)
+        before = start_weights(c)
+        c.add_weights(q, lse, fresh=[0])
+        check_added(c, before, q, lse, None, [0])
+    fill_weights(c, "plain")
+    evict_and_check(c, 300, 20)
+    c.close()
+
+
+def test_tokens_that_were_taken_back():
+    """Drafted tokens that were refused: those that come in their places begin at 0, also where a step brings them."""
+    c = make_cache(1, (8, 2), [("f16", [100])], weights=True)
+    q = rnd(1, 1, 8, 8, 128)
+    _, lse = c.attend_chunk(q)
+    c.add_weights(q, lse)
+    for bring in ("append", "step"):
+        c.len[0] -= 3
+        before = [weights_of(c, 0, 0)]
+        n = 4 if bring == "append" else 1
+        k, v, q = rnd(2, 1, 2, n, 128), rnd(3, 1, 2, n, 128), rnd(4, 1, n, 8, 128)
+        if bring == "append":
+            c.append(0, k, v)
+            _, lse = c.attend_chunk(q)
+        else:
+            _, lse = c.decode(q[:, 0].contiguous(), new=(k, v))
+        before = [torch.cat([before[0], torch.full((2, n), 9.0, device=DEV)], 1)]
+        c.add_weights(q, lse.view(1, n, 8))
+        check_added(c, before, q, lse.view(1, n, 8), None, [n])
+    c.close()
+
+
+def test_two_streams_with_workspaces_that_grow():
+    """Calls of two caches' kind at once: each stream has its own partial sums."""
+    cs = [make_cache(1, (8, 2), [("f16", [n])], weights=True) for n in (600, 900)]
+    cs[1]._streams_ws = cs[0]._streams_ws                         # one table of workspaces for both
+    qs = [[rnd(10 * i + T, 1, T, 8, 128) for T in (70, 300, 100, 500)] for i in range(2)]
+    lses = [[c.attend_chunk(q)[1].clone() for q in x] for c, x in zip(cs, qs)]
+    want = []
+    for c, x, ls in zip(cs, qs, lses):
+        c.weights[0].zero_()
+        for q, lse in zip(x, ls):
+            c.add_weights(q, lse, fresh=[0])
+        want.append(c.weights[0].clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cs]
+    for _ in range(5):
+        for c in cs:
+            c.weights[0].zero_()
+        torch.cuda.synchronize()
+        for j in range(4):
+            for c, x, ls, s in zip(cs, qs, lses, streams):
+                with torch.cuda.stream(s):
+                    c.add_weights(x[j], ls[j], fresh=[0])
+        torch.cuda.synchronize()
+        assert all(torch.equal(c.weights[0], w) for c, w in zip(cs, want))
+    for c in cs:
+        c.close()
+
+
 # ------------------------------------------------------------------ eviction
 
 def rows_of(c, t, b):
@@ -258,6 +349,16 @@ def test_long_tier():
     c = make_cache(1, (2, 1), [("f16", [70000])], weights=True, block=256)
     fill_weights(c, "ties")
     evict_and_check(c, 3000, 256)
+    c.close()
+
+
+@pytest.mark.parametrize("lens", [[4160, 9000], [12345, 500], [31000, 4096], [32833, 64]])
+@pytest.mark.parametrize("swap", [False, True])
+@pytest.mark.parametrize("kind", ["plain", "ties", "wild"])
+def test_lengths_that_waves_hold(lens, swap, kind):
+    c = make_cache(2, (2, 1), [("i4", lens)], weights=True, paged=True)
+    fill_weights(c, kind)
+    evict_and_check(c, 2000, 65, swap)
     c.close()
 
 

@@ -51,14 +51,15 @@ __device__ __forceinline__ Piece<F> load_piece(uint64_t codes, uint64_t meta, in
 // Which of eight numbers are infinite or none, a bit each; they become 0.
 template <bool BF>
 __device__ __forceinline__ uint32_t take_wild(u32x4 &w) {
-  constexpr uint32_t exp1 = BF ? 0x7f80u : 0x7c00u;
+  constexpr uint32_t exps = BF ? 0x7f807f80u : 0x7c007c00u, one = BF ? 0x00800080u : 0x04000400u;
   uint32_t bits = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool low = (w[i] & exp1) == exp1, high = (w[i] >> 16 & exp1) == exp1;
-    bits |= (low ? 1u << 2 * i : 0u) | (high ? 2u << 2 * i : 0u);
-    w[i] &= ~((low ? 0xffffu : 0u) | (high ? 0xffff0000u : 0u));
+    const uint32_t t = ((w[i] & exps) + one) >> 15 & 0x10001u;   // an exponent of ones runs over into the sign's place
+    bits |= (t | t >> 15) << 2 * i;
+    w[i] &= ~(t * 0xffffu);
   }
+  bits &= 0xffu;
   return bits;
 }
 // Eight decompressed channels as fp16 numbers and what those leave (22 bits; the first ones end at 65504, the others have the rest).  Codes

@@ -26,6 +26,8 @@ template <bool BF>
 constexpr float unit16() { return BF ? -7.0f : 8.0f; }
 constexpr float kRoom16 = 7.0f;
 
+typedef __attribute__((address_space(3))) char *las_char;
+
 // ---------------------------------------------------------------- items
 struct ChunkItem {
   int slot, entry, seq, hkv, row_tile, split, n_split;
@@ -117,10 +119,14 @@ __device__ __forceinline__ void spoil(f16v (&o)[4], const uint8_t (&bits)[32][16
     if (t < lim) all |= w;
   }
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d) {   // (without comparisons: 64 conditions at once took the loop's scalar registers, 7-10 % of the time)
+    const uint32_t w = all[d] >> 4 * hh;
+    f16v x = o[d];
 #pragma unroll
     for (int i = 0; i < 16; ++i)   // channel 32 d + 8 (i / 4) + 4 hh + i % 4
-      if (all[d] >> (8 * (i / 4) + 4 * hh + i % 4) & 1) o[d][i] = __builtin_nanf("");
+      x[i] = __uint_as_float(__float_as_uint(x[i]) | ((uint32_t)__builtin_amdgcn_sbfe(w, 8 * (i / 4) + i % 4, 1) & 0x7fc00000u));
+    o[d] = x;
+  }
 }
 
 // ---------------------------------------------------------------- a workgroup's part
@@ -179,8 +185,21 @@ struct Share {
   }
 };
 
+// Where piece p (16 bytes) of a step's row lies in LDS.  Padded: rows begin in other banks each.  Swizzled: rows of 256 bytes whose pieces are exchanged
+// by the row, so that sixteen rows' pieces (four rows' blocks of 64 bytes, for the transposed reads) lie in banks of their own; what the loads
+// without registers ask for, which write 1024 bytes in order.
+struct Padded {
+  static __device__ __forceinline__ int key(int row, int p) { return row * kRowK + 16 * p; }
+  static __device__ __forceinline__ int value(int row, int p) { return row * kRowV + 16 * p; }
+};
+struct Swizzled {
+  static __device__ __forceinline__ int key(int row, int p) { return row * 256 + 16 * (p ^ (row & 15)); }
+  static __device__ __forceinline__ int value(int row, int p) { return row * 256 + 16 * (p ^ (row & 3) << 2); }
+};
+constexpr int kSlot = 32 * 256;   // a step's keys or values there
+
 // A team's rows of one tier on their way: steps mine, mine + TW, .. below hi; keys and values apart.
-template <int F, int RW, int TW>
+template <int F, typename AT, int RW, int TW>
 struct Stream {
   static constexpr int NL = 8 / RW;   // pieces per thread and step
   const Ring &ring;
@@ -202,27 +221,66 @@ struct Stream {
     if (step < hi) at.advance(ring, 32 * TW);
   }
   template <bool BF, bool TWO>
-  __device__ __forceinline__ void put(char *to, int row_bytes, int part_bytes) const {
+  __device__ __forceinline__ void put_keys(char *to, int part_bytes) const {
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-      char *const p = to + ((tid >> 4) + 4 * RW * i) * row_bytes + (tid & 15) * 16;
+      char *const p = to + AT::key((tid >> 4) + 4 * RW * i, tid & 15);
       put_piece<BF, F, TWO>(x[i], p, p + part_bytes);
     }
   }
   // Values of step `of`; all_see: tokens of the tier that every row of the tile sees.
   template <bool BF, bool TWO>
   __device__ __forceinline__ void put_values(char *to, int part_bytes, int of, int all_see, Wild &wild, int buffer) const {
-    if (32 * of + 32 <= all_see) return put<BF, TWO>(to, kRowV, part_bytes);
+    const bool all = 32 * of + 32 <= all_see;
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = (tid >> 4) + 4 * RW * i;
-      char *const p = to + row * kRowV + (tid & 15) * 16;
+      char *const p = to + AT::value(row, tid & 15);
+      if (all) {
+        put_piece<BF, F, TWO>(x[i], p, p + part_bytes);
+        continue;
+      }
       const uint32_t bits = put_piece<BF, F, TWO, true>(x[i], p, p + part_bytes);
       wild.bits[buffer][row][tid & 15] = (uint8_t)bits;
       if (bits) wild.step[buffer] = of;
     }
   }
 };
+
+// fp rows of one tier on their way into LDS without registers: a wave's four rows at a time, 1024 bytes in order.
+template <int RW, int TW>
+struct Direct {
+  static constexpr int NL = 8 / RW;   // per wave and step
+  const Ring &ring;
+  Place at;
+  int step, hi, len;
+  uint32_t codes;
+  __device__ __forceinline__ Direct(const Ring &g, const Place &from, int mine, int lo, int hi_, int len_, uint32_t codes_)
+      : ring(g), at(from), step(mine < hi_ ? mine : lo), hi(hi_), len(len_), codes(codes_) {}
+  // The next step's rows (behind the last step: its own again, so that as many loads are always under way); to: LDS address of the step, piece_of: the
+  // lane's piece in row 4 rw + lane / 16, which is the same in every fourth row and, of keys, exchanged by 4 RW i too.
+  template <bool KEYS>
+  __device__ __forceinline__ void issue(uint32_t to, int rw, int lane) {
+    const int last = min(31, len - 32 * step - 1);
+    const uint64_t base = at.head + codes + (uint64_t)((int64_t)at.row * 256);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = 4 * (rw + RW * i) + (lane >> 4), p = (lane & 15) ^ (KEYS ? row & 15 : (row & 3) << 2);
+      const uint32_t off = min(row, last) * 256 + 16 * p, m0 = to + 1024 * (rw + RW * i);
+      // (not the builtin: the compiler waits for every such load of its own in front of every read of LDS.  Five wait states: the vector unit may have
+      // written the base just before.  Nothing else here uses m0.)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
+    }
+    if (step + TW < hi) {
+      step += TW;
+      at.advance(ring, 32 * TW);
+    }
+  }
+};
+template <int N>
+__device__ __forceinline__ void wait_loads() {   // until N at most are under way
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 // The rounded weights 2 i and 2 i + 1 of a step.
 template <bool BF>
@@ -406,13 +464,13 @@ __global__ __launch_bounds__(64 * RW * TW, Q ? 2 : 1) void chunk_kernel(const Ch
     const int mine = lo + w.tw;
     const Ring ring(tv, seq, w.it.hkv);
     const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
-    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
-    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    Stream<KF, Padded, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    Stream<VF, Padded, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
     Wild &wild = s_wild[w.tw];
     auto put_values = [&](int at, int step) __attribute__((always_inline)) {
       values.template put_values<BT, two_v>(team + at + kPartsK * kKeys, kValues, step, w.tile_sees - ahead, wild, at != 0);
     };
-    auto put_keys = [&](int at) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + at, kRowK, kKeys); };
+    auto put_keys = [&](int at) __attribute__((always_inline)) { keys.template put_keys<BT, two_k>(team + at, kKeys); };
     auto works = [&](int s) __attribute__((always_inline)) { return s < hi && !w.idle && 32 * s < w.last_sees - ahead; };   // (wave-uniform)
     auto scores = [&](int at, f16v &sc) __attribute__((always_inline)) {
 #pragma unroll
@@ -502,13 +560,13 @@ __device__ __forceinline__ void interleave() {
 }
 
 // ---------------------------------------------------------------- many rows
-// Bound: the matrix cores and the vector unit alike.  The steps overlap inside a wave: while the softmax of step s runs on the vector
-// unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  LDS holds two steps' keys and values (s + 1 and
-// s + 2; s - 1 and s), one barrier per step.
+// Bound: the matrix cores, and the power they take.  The steps overlap inside a wave: while the softmax of step s runs on the vector
+// unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  One barrier per step.  fp rows come into LDS without
+// registers, three steps ahead, into four slots each of keys and values; codes through registers, into two.
 template <bool BF, int Q, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
-  constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 2 * (kPartsK * kKeys + kPartsV * kValues);
-  __shared__ __align__(16) char s_tile[TW * kTeam];              // per team: keys of even and odd steps, values of even and odd steps
+  constexpr int kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 8 * kSlot;
+  __shared__ __align__(1024) char s_tile[TW * kTeam];            // per team: four slots of keys, four of values
   __shared__ float s_m[TW * RW][32], s_l[TW * RW][32];
   __shared__ Wild s_wild[TW];
   const Share<RW, TW> w(a);
@@ -517,68 +575,115 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
   f16v o[4];
 #pragma unroll
   for (int d = 0; d < 4; ++d) o[d] = f16v{};
-  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 2 * kPartsK * kKeys;
-  const char *const k_at = team + k_lane(w.lane), *const v_at = team_v + v_lane(w.lane);
+  char *const team = s_tile + w.tw * kTeam, *const team_v = team + 4 * kSlot;
+  const uint32_t team_at = (uint32_t)(uintptr_t)(las_char)team;
+  const int k_at = w.tw * kTeam + Swizzled::key(w.c, w.hh);                      // in s_tile; block kb of 16 channels: ^ 32 kb
+  const int v_row = 4 * w.hh + ((w.lane & 15) >> 2);
+  const int v_at = w.tw * kTeam + 4 * kSlot + Swizzled::value(v_row, 2 * (w.lane >> 4 & 1) + (w.lane >> 1 & 1)) + 8 * (w.lane & 1);   // block d of 32 channels: ^ 64 d
 
   auto run = [&](auto kf, auto vf, const TierView &tv, const ChunkTier &T, int seq, int lo, int hi, int ahead) __attribute__((always_inline)) {
     constexpr int KF = decltype(kf)::value, VF = decltype(vf)::value;
     constexpr bool two_k = is_quant(KF), two_v = is_quant(VF) && V2, BT = BF && !is_quant(KF);   // the product's type: quantized tiers in fp16
+    constexpr bool direct = !is_quant(KF);
+    constexpr int kSlots = direct ? 4 : 2, kKeys = direct ? kSlot : kPartsK * kSlot, kValues = direct ? kSlot : kPartsV * kSlot;
     const int mine = lo + w.tw;
     const Ring ring(tv, seq, w.it.hkv);
     const Place from(ring, tv.bt_magic, T.tok + 32 * (mine < hi ? mine : lo));
-    Stream<KF, RW, TW> keys(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
-    Stream<VF, RW, TW> values(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    auto keys = [&] __attribute__((always_inline)) {
+      if constexpr (direct) return Direct<RW, TW>(ring, from, mine, lo, hi, T.len, 0);
+      else return Stream<KF, Swizzled, RW, TW>(ring, from, mine, hi, T.len, w.tid, 0, tv.k_meta_off);
+    }();
+    auto values = [&] __attribute__((always_inline)) {
+      if constexpr (direct) return Direct<RW, TW>(ring, from, mine, lo, hi, T.len, tv.v_off);
+      else return Stream<VF, Swizzled, RW, TW>(ring, from, mine, hi, T.len, w.tid, tv.v_off, tv.v_meta_off);
+    }();
     const int seen_by_all = min(w.first_sees - ahead, T.len), seen = w.idle ? 0 : min(32 * hi, w.last_sees - ahead);   // by the wave's rows
     const int lim = min(r.pos + 1 - ahead, T.len);
-    auto put_keys = [&](int odd) __attribute__((always_inline)) { keys.template put<BT, two_k>(team + odd * kPartsK * kKeys, kRowK, kKeys); };
     Wild &wild = s_wild[w.tw];
-    auto put_values = [&](int odd, int step) __attribute__((always_inline)) {
-      values.template put_values<BT, two_v>(team_v + odd * kPartsV * kValues, kValues, step, w.tile_sees - ahead, wild, odd);
+    auto bring_keys = [&](int slot) __attribute__((always_inline)) {
+      if constexpr (direct) keys.template issue<true>(team_at + slot * kKeys, w.rw, w.lane);
+      else {
+        keys.template put_keys<BT, two_k>(team + slot * kKeys, kSlot);
+        keys.load();
+      }
     };
-    auto score = [&](f16v &x, int odd, int kb) __attribute__((always_inline)) {
-      const char *const k = k_at + odd * kPartsK * kKeys + 32 * kb;
+    auto bring_values = [&](int slot, int step) __attribute__((always_inline)) {
+      if constexpr (direct) values.template issue<false>(team_at + 4 * kSlot + slot * kValues, w.rw, w.lane);
+      else {
+        values.template put_values<BT, two_v>(team_v + slot * kValues, kSlot, step, w.tile_sees - ahead, wild, slot);
+        values.load();
+      }
+    };
+    // The wave's own part of a step's values, when it has come: see Wild.
+    auto check_values = [&](int slot, int step) __attribute__((always_inline)) {
+      if (32 * step + 32 <= w.tile_sees - ahead) return;
+#pragma unroll
+      for (int i = 0; i < 8 / RW; ++i) {
+        const int row = 4 * (w.rw + RW * i) + (w.lane >> 4), p = w.lane & 15;
+        u32x4 *const at = (u32x4 *)(team_v + slot * kValues + Swizzled::value(row, p));
+        u32x4 x = *at;
+        const uint32_t bits = take_wild<BT>(x);
+        if (bits) *at = x;
+        wild.bits[slot & 1][row][p] = (uint8_t)bits;
+        if (bits) wild.step[slot & 1] = step;
+      }
+    };
+    auto score = [&](f16v &x, int slot, int kb) __attribute__((always_inline)) {
+      const char *const k = s_tile + (k_at ^ 32 * kb) + slot * kKeys;
       x = mma<BT>(*(const u32x4 *)k, qf[kb], x);
-      if constexpr (two_k) x = mma<BT>(*(const u32x4 *)(k + kKeys), qf[kb], x);
+      if constexpr (two_k) x = mma<BT>(*(const u32x4 *)(k + kSlot), qf[kb], x);
     };
-    auto value = [&](int odd, int d, int b, const u32x4 (&p)[2]) __attribute__((always_inline)) {
-      const char *const v = v_at + odd * kPartsV * kValues;
-      o[d] = mma<BT>(value_operand(v, d, b), p[b], o[d]);
-      if constexpr (two_v) o[d] = mma<BT>(value_operand(v + kValues, d, b), p[b], o[d]);
+    auto operand = [&](const char *v, int b) __attribute__((always_inline)) -> u32x4 {
+      u32x4 va;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((las_s4)(v + (16 * b + 8 * j) * 256)));
+        va[2 * j] = y.x;
+        va[2 * j + 1] = y.y;
+      }
+      return va;
+    };
+    auto value = [&](int slot, int d, int b, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+      const char *const v = s_tile + (v_at ^ 64 * d) + slot * kValues;
+      o[d] = mma<BT>(operand(v, b), p[b], o[d]);
+      if constexpr (two_v) o[d] = mma<BT>(operand(v + kSlot, b), p[b], o[d]);
     };
     // The weights of step s meet its values, by themselves.
-    auto flush = [&](int odd, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+    auto flush = [&](int slot, const u32x4 (&p)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) value(odd, d, b, p);
+        for (int b = 0; b < 2; ++b) value(slot, d, b, p);
     };
-    auto spoil_by = [&](int odd, int s) __attribute__((always_inline)) {
-      if (32 * s + 32 > w.tile_sees - ahead && wild.step[odd] == s) spoil(o, wild.bits[odd], lim - 32 * s, w.hh);
+    auto spoil_by = [&](int slot, int s) __attribute__((always_inline)) {
+      if (32 * s + 32 > w.tile_sees - ahead && wild.step[slot & 1] == s) spoil(o, wild.bits[slot & 1], lim - 32 * s, w.hh);
     };
-    // Step s, in buffers ODD: sc its scores, p the weights of the step before (zeros where its values are added already); next and pn receive
+    // Step s, in slot NOW: sc its scores, p the weights of the step before (zeros where its values are added already); next and pn receive
     // the next step's scores and its own weights.
-    auto body = [&](int s, auto odd_tag, f16v &sc, f16v &next, u32x4 (&p)[2], u32x4 (&pn)[2], bool &pending) __attribute__((always_inline)) {
-      constexpr int ODD = decltype(odd_tag)::value;
+    auto body = [&](int s, auto slot_tag, f16v &sc, f16v &next, u32x4 (&p)[2], u32x4 (&pn)[2], bool &pending) __attribute__((always_inline)) {
+      constexpr int NOW = decltype(slot_tag)::value, BEFORE = (NOW + kSlots - 1) % kSlots, NEXT = (NOW + 1) % kSlots;
+      if constexpr (direct) {
+        wait_loads<4 * (8 / RW)>();   // all but those of the last two steps
+        check_values(BEFORE, s - TW);
+      }
       __syncthreads();   // keys of the next step and values of the one before are there; everybody is done with those of this one and the one before that
-      if (pending) spoil_by(1 - ODD, s - TW);
+      if (pending) spoil_by(BEFORE, s - TW);
       const bool works = 32 * s < seen;   // (wave-uniform)
       const float mt = step_max(sc);
       const bool moves = works && __any(mt > r.far);
       if (moves || !works) {
-        if (pending) flush(1 - ODD, p);
+        if (pending) flush(BEFORE, p);
         p[0] = p[1] = u32x4{0, 0, 0, 0};
         if (moves) move_chunk_reference<BT>(r, mt, o);
       }
-      put_keys(ODD);
-      put_values(ODD, s);
-      keys.load();
-      values.load();
+      bring_keys(NOW);                                     // (of the fourth step behind this one; of the second)
+      bring_values(direct ? (NOW + 2) % kSlots : NOW, s);  // (of the second behind it; its own)
       if (works) {
         f16v nx = {};
 #pragma unroll
         for (int g = 0; g < 8; ++g) {   // a product of the values, one of the scores, an eighth of the softmax
-          value(1 - ODD, g / 2, g % 2, p);
-          score(nx, 1 - ODD, g);
+          value(BEFORE, g / 2, g % 2, p);
+          score(nx, NEXT, g);
           weigh2<BT>(r, sc, g, pn);
         }
         // (kept here: the weights are wanted in the next step only, and would be worked out there, behind the products)
@@ -593,14 +698,22 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
     p0[0] = p0[1] = u32x4{0, 0, 0, 0};
     __syncthreads();   // everybody is done with the tier before
     // there is no step before the first: weights of zero meet zeros
-    for (int i = w.tid; i < kPartsV * kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + kPartsV * kValues))[i] = u32x4{0, 0, 0, 0};
+    for (int i = w.tid; i < kValues / 16; i += 64 * RW) ((u32x4 *)(team_v + (kSlots - 1) * kValues))[i] = u32x4{0, 0, 0, 0};
     if (w.tid == 0) wild.step[0] = wild.step[1] = -1;
-    keys.load();
-    put_keys(0);
-    keys.load();
-    put_keys(1);
-    keys.load();
-    values.load();
+    if constexpr (direct) {
+      bring_keys(0);
+      bring_keys(1);
+      bring_keys(2);
+      bring_values(0, 0);
+      bring_keys(3);
+      bring_values(1, 0);
+      wait_loads<5 * (8 / RW)>();
+    } else {
+      keys.load();
+      bring_keys(0);
+      bring_keys(1);
+      values.load();
+    }
     __syncthreads();
     f16v s0 = {}, s1 = {};
 #pragma unroll
@@ -608,14 +721,24 @@ __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const Chunk
     if (32 * mine + 32 > seen_by_all) mask_from(s0, lim - 32 * mine, w.hh);
     bool pending = false;
     const int n_it = (hi - lo + TW - 1) / TW;      // of the first team: all take as many barriers
-    for (int t = 0; t < n_it; t += 2) {
+    int t = 0;
+    for (; t < n_it; t += kSlots) {
       body(mine + TW * t, num<0>{}, s0, s1, p0, p1, pending);
       body(mine + TW * (t + 1), num<1>{}, s1, s0, p1, p0, pending);
+      if constexpr (direct) {
+        body(mine + TW * (t + 2), num<2>{}, s0, s1, p0, p1, pending);
+        body(mine + TW * (t + 3), num<3>{}, s1, s0, p1, p0, pending);
+      }
+    }
+    const int last = mine + TW * (t - 1);
+    if constexpr (direct) {
+      wait_loads<0>();
+      check_values(kSlots - 1, last);
     }
     __syncthreads();
     if (pending) {
-      spoil_by(1, mine + TW * ((n_it + 1) / 2 * 2 - 1));
-      flush(1, p0);
+      spoil_by(kSlots - 1, last);
+      flush(kSlots - 1, p0);
     }
   };
   each_tier<BF, Q>(a, w, r, o, qf, run);

@@ -21,13 +21,24 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int
   for (int i = lane; i < n; i += 64) top = fmaxf(top, a.pm[at + i]);
   top = wave_max(top);
   float l = 0.0f, x = 0.0f, y = 0.0f;
-  for (int i = 0; i < n; ++i) {
-    const float m = a.pm[at + i], li = a.pl[at + i];
-    const float by = m == -INFINITY ? (li != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m - top);
-    const float2 v = *(const float2 *)(a.pacc + (at + i) * 128 + 2 * lane);
-    l = fmaf(li, by, l);
-    x = fmaf(v.x, by, x);
-    y = fmaf(v.y, by, y);
+  for (int i = 0; i < n; i += 8) {   // eight asked for at once
+    float m[8], ls[8];
+    float2 v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int64_t k = at + min(i + j, n - 1);
+      m[j] = a.pm[k];
+      ls[j] = a.pl[k];
+      v[j] = *(const float2 *)(a.pacc + k * 128 + 2 * lane);
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (i + j >= n) continue;
+      const float by = m[j] == -INFINITY ? (ls[j] != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m[j] - top);
+      l = fmaf(ls[j], by, l);
+      x = fmaf(v[j].x, by, x);
+      y = fmaf(v[j].y, by, y);
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   *(uint32_t *)(a.out + entry * a.o_seq + token * a.o_token + hq * a.o_head + 4 * lane) =

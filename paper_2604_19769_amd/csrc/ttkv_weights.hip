@@ -558,7 +558,7 @@ void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int k_fmt, int32
   chunk = kTile;
   const int64_t resident = 256;
   if (most_rows <= kFewRows) {   // as many tokens per item as leave every workgroup that fits on the chip, one per CU, one
-    const int64_t want = most_rows <= 64 ? 2048 : 256;
+    const int64_t want = most_rows <= 64 ? 768 : 256;
     chunk = (int32_t)(kTile * std::max<int64_t>(1, std::min<int64_t>(64, (tiles * Hkv + want - 1) / want)));
     return;
   }

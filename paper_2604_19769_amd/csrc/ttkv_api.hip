@@ -1907,7 +1907,7 @@ ttkv_status plan_weigh(const ttkv_cache *c, bool check_tables, int32_t tier, int
   P.ws_bytes = 0;
   if (P.n_slots == 0) return TTKV_OK;
   if (P.most_rows >= 1ll << 28) return TTKV_ERR_UNSUPPORTED;
-  weigh_shape(P.most_rows, tiles, a.Hkv, T.k_fmt, a.chunk, a.n_split);
+  weigh_shape(P.most_rows, tiles, a.Hkv, a.chunk, a.n_split);
   int64_t items = 0;
   for (int i = 0; i < P.n_slots; ++i) {
     a.first_item[i] = (int32_t)items;

@@ -438,9 +438,10 @@ __device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW
 }
 
 // ---------------------------------------------------------------- few rows
-// Bound: memory.  Keys of one step and values of the one before are on their way while one is computed.  The outputs are divided by the sum of the
+// Bound: memory (32 sequences of 4000 to 6000 bf16 tokens, 32 / 8 heads, 16 rows per KV head: 522 MB in 107 us, 4.9 TB/s where a large copy reaches 5.1).  A workgroup has
+// all rows of a KV head and a part of its tokens, four teams of two waves; keys of one step and values of the one before are on their way while one is computed.  The outputs are divided by the sum of the
 // weights as they were rounded: where a token or two have most of the weight, their rounding then cancels.  With quantized tiers LDS holds one step
-// only, so that a CU has two workgroups: one decompresses while the other computes.
+// only, so that a CU has two workgroups: one decompresses while the other computes (int4 histories of 8192 tokens, 48 rows: 89 us; with one workgroup of eight waves 250).
 template <bool BF, int Q, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, Q ? 2 : 1) void chunk_kernel(const ChunkArgs a) {
   constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kStep = kPartsK * kKeys + kPartsV * kValues;
@@ -560,9 +561,11 @@ __device__ __forceinline__ void interleave() {
 }
 
 // ---------------------------------------------------------------- many rows
-// Bound: the matrix cores, and the power they take.  The steps overlap inside a wave: while the softmax of step s runs on the vector
+// Bound: the matrix cores and the power limit, then what the rows' way into LDS costs: 2048 fp16 rows of 32 / 8 heads behind 32768 tokens 1150 us, 0.98 PFLOP/s where a large
+// library product reaches 1.36; 980 without the loads, 870 with the products alone (builds for the measurement).  The steps overlap inside a wave: while the softmax of step s runs on the vector
 // unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  One barrier per step.  fp rows come into LDS without
-// registers, three steps ahead, into four slots each of keys and values; codes through registers, into two.
+// registers, three steps ahead, into four slots each of keys and values (through registers, one step ahead: 1205); codes through registers, into two.  256 rows per
+// workgroup, so that the CUs read an XCD's KV head from its L2 half as often as with 128; two workgroups of four waves per CU 1356.
 template <bool BF, int Q, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
   constexpr int kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 8 * kSlot;

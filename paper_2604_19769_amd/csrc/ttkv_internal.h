@@ -433,9 +433,8 @@ struct WeighArgs {
   int32_t entry[TTKV_MAX_BATCH];
 };
 static_assert(sizeof(WeighArgs) <= 4096, "kernel arguments are passed by value");
-// How a launch is cut: tokens per item and items per tile's rows, for `most_rows` query rows per KV head, `tokens` of all slots (each rounded up to
-// 256) and their rows' steps.
-void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int k_fmt, int32_t &chunk, int32_t &n_split);
+// How a launch is cut: tokens per item and items per tile's rows, for `most_rows` query rows per KV head and `tiles` of 256 tokens of all slots.
+void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int32_t &chunk, int32_t &n_split);
 hipError_t launch_weigh(const WeighArgs &a, int64_t most_rows, hipStream_t s, int *n_kernels);
 
 // The lightest tokens of a tier leave their places to tokens of its oldest blocks (light_select_kernel, light_move_kernel).

@@ -181,7 +181,8 @@ __device__ __forceinline__ f16v sum_steps(f16v acc, const Operands<KF> &ops, con
   return add_rows(acc, nx, cs, rn.off);
 }
 
-// Few rows (a step's, the last queries of a prompt).  Bound: memory, and from some 200 rows on the vector unit's exponentials.  All rows lie in LDS; the waves take an item's tokens 32 at a time, the
+// Few rows (a step's, the last queries of a prompt).  Bound: memory (a step of 48 x 2000 to 4000 fp16 tokens, 32 / 8 heads: 305 MB in 57-62 us, 5 TB/s), and from some 200 rows
+// on the vector unit's exponentials (256 rows x 4 x 16384 bf16 tokens 51 us; its bytes alone 28).  All rows lie in LDS; the waves take an item's tokens 32 at a time, the
 // next ones' keys on their way, and meet nobody.  Keys are loaded as whole lines and turned into operands through LDS of the wave's own (as
 // operands they are pieces of 32 bytes of 32 rows per instruction: a step of 48 x 4000 tokens of 32 / 8 heads 86 us).
 template <bool BF, int KF, int ROWS, int NW>
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(64 * NW, 1) void weigh_few_kernel(const WeighArgs a
   }
 }
 
-// Many rows (a prompt's).  Bound: the vector unit's exponentials.  A wave keeps its tokens, the rows come through LDS; where there are few tokens, several
+// Many rows (a prompt's).  Bound: the vector unit's exponentials, and in short prompts the launch's start (2047 queries of 28 / 4 heads 33 us, the sums 4).  A wave keeps its tokens, the rows come through LDS; where there are few tokens, several
 // items share a tile's rows, and weigh_sum_kernel adds their sums in order.
 // (128 rows between two barriers: with 32 a step's rows were asked for one step ahead, less than they take; 2047 queries of 28 / 4 heads 52 us.)
 template <bool BF, int KF>
@@ -381,7 +382,10 @@ __device__ __forceinline__ int row_sum(int v) {   // over 16 lanes, in each of t
 // LDS's counters.  (Counting the tokens above three candidates by ballots, two bits at a time: 4 x 32768 tokens 76 us.)  Then each wave
 // knows the places of its tokens from the counts of the waves before it: the i-th token that stays among the first `gone` moves to the i-th
 // place behind them whose token goes.
-constexpr int kInPlace = 256;   // moves that the selecting workgroup makes by itself
+// Bound: the instructions of the CUs that work, for an item is a sequence's KV head (32 heads of up to 32768 tokens 37 us, 384 heads of 4096 16; orders read again
+// instead of kept 91 and 28; registers for 32768 tokens where 4096 are 27).
+// Moves that the selecting workgroup makes by itself: a launch less (384 heads of 4096 tokens that free a block 16.4 us, in two launches 16.7 + 3.9).
+constexpr int kInPlace = 256;
 template <int IPT>
 __global__ __launch_bounds__(1024, IPT > 12 ? 1 : 2) void light_select_kernel(const LightArgs a, int in_place) {
   __shared__ i32x2 s_count[2][16];
@@ -535,7 +539,7 @@ __global__ __launch_bounds__(1024, IPT > 12 ? 1 : 2) void light_select_kernel(co
     m.end(a);
   }
 }
-// Two rows per 32 lanes.
+// Two rows per 32 lanes.  Bound: memory's latency and rate (32 heads, up to 1800 rows of 516 bytes each: 11 us).
 __global__ __launch_bounds__(256) void light_move_kernel(const LightArgs a) {
   const int hkv = blockIdx.y % a.Hkv, slot = blockIdx.y / a.Hkv;
   const int moves = a.count[slot * a.Hkv + hkv], i = blockIdx.x * 16 + (threadIdx.x >> 5);
@@ -553,11 +557,13 @@ __global__ __launch_bounds__(256) void light_move_kernel(const LightArgs a) {
 
 }  // namespace
 
-void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int k_fmt, int32_t &chunk, int32_t &n_split) {
+void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int32_t &chunk, int32_t &n_split) {
   n_split = 1;
   chunk = kTile;
   const int64_t resident = 256;
-  if (most_rows <= kFewRows) {   // as many tokens per item as leave every workgroup that fits on the chip, one per CU, one
+  // Up to 256 rows, all in LDS: 256 rows x 4 x 16384 tokens 54 us, 75 in the kernel for many; 256 x 4096 tokens 10.5 and 10.9.  One round of the workgroups that a CU
+  // holds: three with 64 rows (8 x 8192 tokens 24.8 us, 28.5 with 2048 items; in the kernel for 256 rows 24.9, but 48 x 4000 98 instead of 82), one with 256.
+  if (most_rows <= kFewRows) {
     const int64_t want = most_rows <= 64 ? 768 : 256;
     chunk = (int32_t)(kTile * std::max<int64_t>(1, std::min<int64_t>(64, (tiles * Hkv + want - 1) / want)));
     return;

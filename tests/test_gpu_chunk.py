@@ -319,3 +319,38 @@ def test_positions_behind_a_prefix_that_was_thinned_out():
     check(c, turned, out, lse)
     c.close()
     p.close()
+
+
+@pytest.mark.parametrize("fmt,codes,group", [("i8", 128, 32), ("i4", 64, 64)])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [3, 20, 70, 200])
+def test_wild_scales_of_tokens_that_a_query_does_not_see(fmt, codes, group, dtype, T):
+    """A value scale that is no number in a quantized tier's newer token: as above, in the channels of its group."""
+    n = T + 70
+    c = make_cache(1, (8, 2), [(fmt, [n])], wrap=False)
+    q = rnd(6, 1, T, 8, 128, dtype=dtype)
+    clean = attend(c, q)
+    row = n - (T + 1) // 2
+    at = (row // 64 * 2 + 1) * 64 * (2 * codes + 16) + 64 * (2 * codes + 8) + row % 64 * 8   # KV head 1, the row's first value scale
+    c.pool[0].view(-1)[at:at + 2] = 255
+    wild = attend(c, q)
+    seen = T - (n - row)
+    assert torch.equal(wild[0][:, :seen], clean[0][:, :seen]) and torch.equal(wild[1], clean[1])
+    assert torch.isnan(wild[0][:, seen:, 4:, :group]).all()
+    assert torch.equal(wild[0][:, :, 4:, group:], clean[0][:, :, 4:, group:]) and torch.equal(wild[0][:, :, :4], clean[0][:, :, :4])
+    c.close()
+
+
+@pytest.mark.parametrize("T", [20, 70])
+def test_wild_values_behind_a_quantized_tier(T):
+    """The step where a tier ends, and the fp tier behind it, whose first token nobody but the newest query sees."""
+    c = make_cache(1, (8, 2), [("f16", [1]), ("i8", [T + 44])], wrap=False)
+    q = rnd(6, 1, T, 8, 128)
+    clean = attend(c, q)
+    c.pool[0].view(torch.float16).view(-1, 2, 2, 64, 128)[0, 1, 1, 0, 100] = float("inf")
+    wild = attend(c, q)
+    assert torch.equal(wild[0][:, :-1], clean[0][:, :-1]) and torch.equal(wild[1], clean[1])
+    assert not torch.isfinite(wild[0][:, -1, 4:, 100]).any()
+    others = torch.arange(128, device=DEV) != 100
+    assert torch.equal(wild[0][..., others], clean[0][..., others])
+    c.close()

@@ -166,6 +166,7 @@ class TieredCache:
         self.start, self.len, self.pool, self.table = [], [], [], []
         self.weights = []                 # per tier None, or fp32 [record][KV head][block token] beside the tier's records
         self._weighed = [np.zeros(batch, np.int64) for _ in self.cfg]   # lifetime ordinal behind the newest token weighed
+        self._weighted = [t for t, cfg in enumerate(self.cfg) if cfg.weights]
         self.evicted = np.zeros(batch, np.int64)   # tokens of each sequence that evict_light dropped (they still count as positions)
         for t, cfg in enumerate(self.cfg):
             T = c.tier[t]
@@ -266,7 +267,7 @@ class TieredCache:
         n = k.shape[-2]
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
-        self._unweighed(tier)
+        self._unweighed()
         if self.cfg[tier].mem == "host" and self.host_append_direct:
             # no staging: the conversion kernels store into the pinned records
             B.ttkv_quantize_append_host(self.h, self.c, tier, seq, k, v, fmt, n, int(through_tiers), None, 0, self._compute())
@@ -302,7 +303,7 @@ class TieredCache:
                 first_pos = first_pos + (1 if self.members is None else self.members) * ahead
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
         shape = (n, T, self.Hkv, 128)
-        self._unweighed(tier)
+        self._unweighed()
         B.ttkv_rope_append(self.h, self.c, tier, seq, rotary.r, qv, qo, _heads(k, shape, dev), _heads(v, shape, dev), T, _host_int64(counts, n),
                            _host_int64(first_pos, n), _device_positions(positions, n, T, dev), self._compute())
         self._parts_age = None            # lengths jump: count the parts again at the next step
@@ -316,6 +317,7 @@ class TieredCache:
         need = 0 if self.host_demote_direct else self._demote_need
         if need and (self.demote_ws is None or self.demote_ws.numel() < need):
             self.demote_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self._unweighed()
         B.ttkv_evict(self.h, self.c, self.demote_ws if need else None, need, self._compute(), self._copy(overlap))
 
     def _workspace(self, parts):
@@ -333,7 +335,7 @@ class TieredCache:
         """q [B][Hq][128] f16/bf16 on the device.  selected: None or (sel_blocks, sel_count) pinned int32 tensors.
         new: None, or (k_new, v_new) [B][Hkv][1][128] of the step's token, appended to tier 0 by the same call."""
         if new is not None:
-            self._unweighed(0)
+            self._unweighed()
         if self.prefix is not None:
             assert selected is None, "blocks are not selected behind a prefix"
             return self._decode_shared(q, new)
@@ -522,10 +524,11 @@ class TieredCache:
         return out, lse
 
     # ------------------------------------------------------------------ weights of tokens
-    def _unweighed(self, tier):
-        """Before tokens are appended: what lies behind the newest token held has not been weighed (tokens may have been taken back)."""
-        if self.weights[tier] is not None:
-            np.minimum(self._weighed[tier], self.start[tier] + self.len[tier], out=self._weighed[tier])
+    def _unweighed(self):
+        """Before tokens come into a tier, from outside or down the cascade: what lies behind the newest token that each tier holds has not been
+        weighed (tokens may have been taken back, a sequence may have ended)."""
+        for t in self._weighted:
+            np.minimum(self._weighed[t], self.start[t] + self.len[t], out=self._weighed[t])
 
     @_on_own_device
     def add_weights(self, q, lse, counts=None, fresh=None, tier=0, seq=-1):
@@ -583,7 +586,7 @@ class TieredCache:
         assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
         assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128)
         stride = self._select_buffers(k)
-        self._unweighed(0)
+        self._unweighed()
         # The split of a selection is planned inside the call, which refuses a workspace that is too small for it before
         # anything is enqueued: the workspace is sized once from a dense plan's parts and grows when it is refused (no
         # run is cut finer than into items of 128 tokens, which bounds it).

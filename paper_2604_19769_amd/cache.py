@@ -167,7 +167,8 @@ class TieredCache:
         self.weights = []                 # per tier None, or fp32 [record][KV head][block token] beside the tier's records
         self._weighed = [np.zeros(batch, np.int64) for _ in self.cfg]   # lifetime ordinal behind the newest token weighed
         self._weighted = [t for t, cfg in enumerate(self.cfg) if cfg.weights]
-        self.evicted = np.zeros(batch, np.int64)   # tokens of each sequence that evict_light dropped (they still count as positions)
+        self.evicted = np.zeros(batch, np.int64)   # tokens of each sequence that evict_light dropped since it began (they still count as positions)
+        self._thinned = False             # some of `evicted` may not be 0
         for t, cfg in enumerate(self.cfg):
             T = c.tier[t]
             T.k_fmt, T.v_fmt = B.FMT_NAMES[cfg.k_fmt], B.FMT_NAMES[cfg.v_fmt]
@@ -267,6 +268,7 @@ class TieredCache:
         n = k.shape[-2]
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
+        self._ended()
         self._unweighed()
         if self.cfg[tier].mem == "host" and self.host_append_direct:
             # no staging: the conversion kernels store into the pinned records
@@ -284,7 +286,8 @@ class TieredCache:
         """Keys normed and rotated on their way into an fp16 / bf16 tier, values beside them, the queries normed and rotated in the
         same launch (ttkv_rope_append).  k, v [B][T][Hkv][128], q [B][T][Hq][128], any strides but the last, f16 / bf16 / f32;
         seq >= 0: one sequence's, B = 1.  counts: tokens of each sequence (host integers; None: T).  Positions as in
-        Rotary.apply; neither given: behind the tokens held (prefix included) and those that evict_light dropped.  Returns q_out (a new tensor unless given; rows behind a
+        Rotary.apply; neither given: behind the tokens held (prefix included) and those that evict_light dropped; a sequence that holds none begins anew
+        (begin_anew).  Returns q_out (a new tensor unless given; rows behind a
         sequence's count are not written, a new tensor's hold anything)."""
         n, T = (self.B, k.shape[1]) if seq < 0 else (1, k.shape[1])
         assert rotary.device == self.device or _on(rotary, self.device)
@@ -296,9 +299,11 @@ class TieredCache:
                                          memory_format=torch.contiguous_format)
             shape = (n, T, self.Hq, 128)
             qv, qo = _heads(q, shape, dev), _heads(q_out, shape, dev)
-        if first_pos is None and positions is None and (self.prefix is not None or self.evicted.any()):
+        self._ended()
+        if first_pos is None and positions is None and (self.prefix is not None or self._thinned):
             first_pos = sum(self.len) + self.evicted
             if self.prefix is not None:
+                self.prefix._ended()
                 ahead = int(sum(x[0] for x in self.prefix.len) + self.prefix.evicted[0])
                 first_pos = first_pos + (1 if self.members is None else self.members) * ahead
             first_pos = first_pos if seq < 0 else first_pos[seq:seq + 1]
@@ -309,6 +314,23 @@ class TieredCache:
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
         return q_out
+
+    def begin_anew(self, seq=-1):
+        """Sequence seq (-1: every one) ends: no tier holds a token of it any more, and the next ones begin at position 0, or right behind the prefix.
+        (Setting its lengths in all tiers to 0 by hand comes to the same.)"""
+        assert -1 <= seq < self.B
+        rows = slice(None) if seq < 0 else slice(seq, seq + 1)
+        for held in self.len:
+            held[rows] = 0
+        self._ended()
+        self._parts_age = None            # lengths jump: count the parts again at the next step
+        self._until_evict = 0
+
+    def _ended(self):
+        """Before tokens are appended: of a sequence that holds none evict_light has dropped none."""
+        if self._thinned:
+            self.evicted[sum(self.len) == 0] = 0
+            self._thinned = bool(self.evicted.any())
 
     def demote(self, overlap=True):
         """Cascade eviction through all tiers (Alg. 1, last lines)."""
@@ -335,6 +357,7 @@ class TieredCache:
         """q [B][Hq][128] f16/bf16 on the device.  selected: None or (sel_blocks, sel_count) pinned int32 tensors.
         new: None, or (k_new, v_new) [B][Hkv][1][128] of the step's token, appended to tier 0 by the same call."""
         if new is not None:
+            self._ended()
             self._unweighed()
         if self.prefix is not None:
             assert selected is None, "blocks are not selected behind a prefix"
@@ -560,6 +583,7 @@ class TieredCache:
         self._with_workspace("light", lambda ws, size: B.ttkv_evict_light(self.h, self.c, tier, keep, recent, swap, self.weights[tier], ws, size, stream),
                              lambda: B.ttkv_evict_light_workspace_bytes(self.h, self.c, tier, keep, recent))
         self.evicted += held - self.len[tier]
+        self._thinned = bool(self.evicted.any())
         self._parts_age = None            # lengths jump: count the parts again at the next step
         self._until_evict = 0
 
@@ -586,6 +610,7 @@ class TieredCache:
         assert q.is_contiguous() and k_new.is_contiguous() and v_new.is_contiguous()
         assert k_new.shape == v_new.shape == (self.B, self.Hkv, 1, 128)
         stride = self._select_buffers(k)
+        self._ended()
         self._unweighed()
         # The split of a selection is planned inside the call, which refuses a workspace that is too small for it before
         # anything is enqueued: the workspace is sized once from a dense plan's parts and grows when it is refused (no

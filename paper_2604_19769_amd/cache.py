@@ -167,6 +167,7 @@ class TieredCache:
         self.weights = []                 # per tier None, or fp32 [record][KV head][block token] beside the tier's records
         self._weighed = [np.zeros(batch, np.int64) for _ in self.cfg]   # lifetime ordinal behind the newest token weighed
         self._weighted = [t for t, cfg in enumerate(self.cfg) if cfg.weights]
+        self._weighs = [False] * len(self.cfg)   # add_weights keeps the tier's weights (otherwise the caller does, who knows what they wrote)
         self.evicted = np.zeros(batch, np.int64)   # tokens of each sequence that evict_light dropped since it began (they still count as positions)
         self._thinned = False             # some of `evicted` may not be 0
         for t, cfg in enumerate(self.cfg):
@@ -573,12 +574,18 @@ class TieredCache:
         self._with_workspace("weights", lambda ws, size: B.ttkv_add_weights(self.h, self.c, tier, seq, qv, lse, T, each, begin, self.weights[tier], ws, size, stream),
                              lambda: B.ttkv_weights_workspace_bytes(self.h, self.c, tier, seq, T, each, begin))
         self._weighed[tier][rows] = end
+        self._weighs[tier] = True
 
     @_on_own_device
     def evict_light(self, keep, recent, tier=0, swap=False):
         """Frees the tier's oldest blocks, as many as leave every sequence at least `keep` tokens: per KV head the tokens of least weight go, the
-        `recent` newest stay, the others have been weighed (ttkv_evict_light).  swap: nothing goes; the light tokens lie in the oldest blocks afterwards, for demote()."""
+        `recent` newest stay, the others have been weighed (ttkv_evict_light; where add_weights keeps the tier's weights, tokens that came after it and
+        are not among the recent ones are refused).  swap: nothing goes; the light tokens lie in the oldest blocks afterwards, for demote()."""
         assert self.weights[tier] is not None, "the tier keeps no weights"
+        if self._weighs[tier]:            # tokens that were not weighed have what their places held before
+            held, bt = self.len[tier], self.cfg[tier].block_tokens
+            if ((held - keep >= bt) & (self.start[tier] + held - self._weighed[tier] > recent)).any():
+                raise B.TTKVError(B.ERR_INVALID_ARG, "ttkv_evict_light: tokens in front of the recent ones were not weighed")
         held, stream = self.len[tier].copy(), self._compute()
         self._with_workspace("light", lambda ws, size: B.ttkv_evict_light(self.h, self.c, tier, keep, recent, swap, self.weights[tier], ws, size, stream),
                              lambda: B.ttkv_evict_light_workspace_bytes(self.h, self.c, tier, keep, recent))

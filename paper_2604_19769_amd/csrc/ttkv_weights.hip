@@ -210,11 +210,14 @@ __global__ __launch_bounds__(64 * NW, 1) void weigh_few_kernel(const WeighArgs a
   const char *const q_at = s_q + k_lane(lane);
   const float cs = a.scale * kLog2e;
   for (; t < end; t += 32 * NW) {
+    // (LDS takes a wave's stores and reads in order; the compiler has to leave them so)
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       char *const to = own + ((lane >> 4) + 4 * i) * kRowK + 16 * (lane & 15);
       put_piece<BF, KF, true>(x[i], to, to + kPart);
     }
+    asm volatile("" ::: "memory");
     at = next;
     if (t + 32 * NW < end) {
       next.advance(ring, 32 * NW);

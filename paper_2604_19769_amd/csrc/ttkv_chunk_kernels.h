@@ -268,8 +268,8 @@ struct Direct {
       const int row = 4 * (rw + RW * i) + (lane >> 4), p = (lane & 15) ^ (KEYS ? row & 15 : (row & 3) << 2);
       const uint32_t off = min(row, last) * 256 + 16 * p, m0 = to + 1024 * (rw + RW * i);
       // (not the builtin: the compiler waits for every such load of its own in front of every read of LDS.  Five wait states: the vector unit may have
-      // written the base just before.  Nothing else here uses m0.)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory");
+      // written the base just before.)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(m0), "v"(off), "s"(base) : "memory", "m0");
     }
     if (step + TW < hi) {
       step += TW;

@@ -1658,9 +1658,11 @@ namespace {
 // One launch of the chunk's attention: what the cache, the prefix and the lengths decide.
 struct ChunkPlan {
   ChunkArgs a;
+  ChunkMergeArgs merge;
   ChunkShape shape;
-  int64_t rows;        // query rows per KV head, all sequences
-  size_t ws_bytes;     // partials
+  int64_t rows, cut_rows;   // query rows per KV head, all sequences; those whose tiles are cut
+  int64_t parts;            // partials that they leave
+  size_t ws_bytes;
 };
 // Offsets inside a KV head's part of a block are counted in 32 bits.
 constexpr int32_t kLargestBlock = 1 << 21;
@@ -1745,8 +1747,8 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
     most_rows = std::max(most_rows, n * a.G);
   }
   P.ws_bytes = 0;
+  P.cut_rows = P.parts = 0;
   a.n_items = 0;
-  a.part_stride = 0;
   if (n_slots == 0) return TTKV_OK;
   if (P.rows * a.Hkv >= 1ll << 28) return TTKV_ERR_UNSUPPORTED;   // a launch has 2^32 threads at most
   std::sort(slot, slot + n_slots, [](const Slot &x, const Slot &y) { return x.sees != y.sees ? x.sees > y.sees : x.entry < y.entry; });
@@ -1780,13 +1782,13 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
       }
     }
   }
-  int most = 1;
-  int64_t items = 0, rows = 0;
+  int64_t items = 0;
   for (int i = 0; i < n_slots; ++i) {
     const int n = (int)split_at(best_steps, i);
     a.first_item[i] = (int32_t)items;
     a.count[i] = (int32_t)slot[i].n;
-    a.row_base[i] = (int32_t)rows;
+    P.merge.row_base[i] = (int32_t)P.cut_rows;
+    a.part_base[i] = (int32_t)P.parts;   // (a workgroup leaves 256 at most, and there are fewer than 2^23)
     a.n_split[i] = n;
     a.entry[i] = slot[i].entry;
     for (int t = 0; t < c->n_tiers; ++t) {
@@ -1795,16 +1797,17 @@ ttkv_status plan_chunk(const ttkv_cache *c, bool check_tables, int32_t seq, cons
       a.len[t][i] = (int32_t)T.len[slot[i].b];
     }
     items += tiles[i] * n;
-    rows += slot[i].n * a.G;
-    most = std::max(most, n);
+    if (items * a.Hkv >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;
+    if (n > 1) {
+      P.cut_rows += slot[i].n * a.G;
+      P.parts += slot[i].n * a.G * a.Hkv * n;
+    }
   }
-  for (int i = n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = a.row_base[i] = INT32_MAX;
-  if (items * a.Hkv >= 1ll << 23) return TTKV_ERR_UNSUPPORTED;
+  for (int i = n_slots; i < TTKV_MAX_BATCH; ++i) a.first_item[i] = P.merge.row_base[i] = INT32_MAX;
   a.n_items = (int32_t)items;
-  a.part_stride = most > 1 ? most : 0;
   a.hkv_magic = a.Hkv > 1 && items * a.Hkv * a.Hkv < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.Hkv - 1) / a.Hkv) : 0;
   a.g_magic = a.G > 1 && most_rows * a.G < (1ll << 32) ? (uint32_t)(((1ll << 32) + a.G - 1) / a.G) : 0;
-  P.ws_bytes = (size_t)P.rows * a.Hkv * a.part_stride * 130 * sizeof(float);
+  P.ws_bytes = (size_t)P.parts * 130 * sizeof(float);
   return TTKV_OK;
 }
 }  // namespace
@@ -1842,16 +1845,26 @@ ttkv_status ttkv_chunk_attn(ttkv_handle hh, const ttkv_cache *c, int32_t seq, co
   a.lse = lse;
   const size_t mis = (256 - ((uintptr_t)workspace & 255)) & 255;
   if (P.ws_bytes && (!workspace || ws_bytes < mis + P.ws_bytes)) return TTKV_ERR_WORKSPACE;
-  const int64_t parts = P.rows * a.Hkv * a.part_stride;
-  if (parts) {
+  if (P.parts) {
     a.pacc = (float *)((uint8_t *)workspace + mis);
-    a.pm = a.pacc + parts * 128;
-    a.pl = a.pm + parts;
+    a.pm = a.pacc + P.parts * 128;
+    a.pl = a.pm + P.parts;
   }
   hipStream_t stream = (hipStream_t)stream_;
   TTKV_HIP(h, launch_chunk(a, P.shape, stream));
-  if (parts) TTKV_HIP(h, launch_chunk_merge(a, P.rows * a.Hkv, stream));
-  h->stats.kernels += parts ? 2 : 1;
+  if (P.parts) {
+    ChunkMergeArgs &m = P.merge;
+    m.Hq = a.Hq; m.Hkv = a.Hkv; m.G = a.G; m.g_magic = a.g_magic;
+    m.out_fmt = a.out_fmt; m.n_tokens = a.n_tokens;
+    m.out = a.out; m.lse = lse;
+    m.pm = a.pm; m.pl = a.pl; m.pacc = a.pacc;
+    m.o_seq = a.o_seq; m.o_token = a.o_token; m.o_head = a.o_head;
+    std::copy_n(a.part_base, TTKV_MAX_BATCH, m.part_base);
+    std::copy_n(a.n_split, TTKV_MAX_BATCH, m.n_split);
+    std::copy_n(a.entry, TTKV_MAX_BATCH, m.entry);
+    TTKV_HIP(h, launch_chunk_merge(m, P.cut_rows * a.Hkv, stream));
+  }
+  h->stats.kernels += P.parts ? 2 : 1;
   return TTKV_OK;
 }
 

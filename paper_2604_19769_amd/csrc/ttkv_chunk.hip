@@ -9,7 +9,7 @@ using namespace chunk;
 
 // The items of a row tile joined: a wave per query row, two channels per lane.  Bound: the parts' way from the L2s (512 rows of 32 parts 7.0 us; one part after
 // the other 11.1).
-__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int n_rows) {
+__global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkMergeArgs a, int n_rows) {
   const int lane = threadIdx.x & 63;
   const int id = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
   if (id >= n_rows) return;
@@ -17,7 +17,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a, int
   const int slot = __popcll(__ballot(a.row_base[lane] <= row_all)) - 1;
   const int row = row_all - a.row_base[slot], token = token_of(a, row), hq = hkv * a.G + row - token * a.G;
   const int n = a.n_split[slot], entry = a.entry[slot];
-  const int64_t at = (int64_t)id * a.part_stride;
+  const int64_t at = a.part_base[slot] + ((int64_t)row * a.Hkv + hkv) * n;
   float top = -INFINITY;
   for (int i = lane; i < n; i += 64) top = fmaxf(top, a.pm[at + i]);
   top = wave_max(top);
@@ -71,7 +71,7 @@ hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t str
   return hipGetLastError();
 }
 
-hipError_t launch_chunk_merge(const ChunkArgs &a, int64_t n_rows, hipStream_t stream) {
+hipError_t launch_chunk_merge(const ChunkMergeArgs &a, int64_t n_rows, hipStream_t stream) {
   hipLaunchKernelGGL(chunk_merge_kernel, dim3((unsigned)((n_rows + 3) / 4)), dim3(256), 0, stream, a, (int)n_rows);
   return hipGetLastError();
 }

@@ -36,7 +36,7 @@ struct ChunkItem {
 __device__ __forceinline__ ChunkItem chunk_item(const ChunkArgs &a, int rows_per_tile) {
   // all that the look-ups read, asked for at once: a launch's arguments are in no cache when its first workgroups start
   asm volatile("" ::"s"(a.Hkv), "s"(a.n_tiers), "s"(a.q), "s"(a.q_seq), "s"(a.tv[0].base), "s"(a.tv[0].bt), "s"(a.first_item[0]), "s"(a.count[0]),
-               "s"(a.row_base[0]), "s"(a.n_split[0]), "s"(a.entry[0]), "s"(a.first_tok[0][0]), "s"(a.len[0][0]), "s"(a.prefix_len[0]));
+               "s"(a.part_base[0]), "s"(a.n_split[0]), "s"(a.entry[0]), "s"(a.first_tok[0][0]), "s"(a.len[0][0]), "s"(a.prefix_len[0]));
   ChunkItem it;
   const uint32_t id = blockIdx.x;
   const int item = a.Hkv == 1 ? id : a.hkv_magic ? (int)mul_high(id, a.hkv_magic) : (int)(id / (uint32_t)a.Hkv);
@@ -372,8 +372,8 @@ __device__ __forceinline__ void finish(const ChunkArgs &a, const Share<RW, TW> &
   }
   if (!r.on) return;
   // channels 32 d + 8 k + 4 hh .. + 3 of the row lie in registers 4 k .. + 3 of block d
-  if (a.part_stride) {
-    const int64_t at_part = (((int64_t)a.row_base[it.slot] + row0 + c) * a.Hkv + it.hkv) * a.part_stride + it.split;
+  if (it.n_split > 1) {
+    const int64_t at_part = a.part_base[it.slot] + ((int64_t)(row0 + c) * a.Hkv + it.hkv) * it.n_split + it.split;
     float *const po = a.pacc + at_part * 128 + 4 * hh;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {

@@ -372,19 +372,18 @@ struct ChunkArgs {
   int32_t n_tiers, n_prefix;       // tiers, and how many of them are the prefix's
   float scale;
   int32_t q_fmt, out_fmt;
-  int32_t part_stride;             // partials per row; 0: every row tile is one item, which stores the result
   int32_t n_tokens, first_seq;     // lse's rows per entry; sequence of entry 0
   const uint8_t *q;
   uint8_t *out;
   float *lse;                      // nullable
-  float *pm, *pl, *pacc;
+  float *pm, *pl, *pacc;           // partials of the slots whose row tiles are several items (the others' items store the results)
   int64_t q_seq, q_token, q_head, o_seq, o_token, o_head;
   uint64_t members;                // sequences that attend the prefix
   TierView tv[2 * TTKV_MAX_TIERS];
   int32_t prefix_tok[TTKV_MAX_TIERS], prefix_len[TTKV_MAX_TIERS];
   int32_t first_item[TTKV_MAX_BATCH];   // of the slot, INT32_MAX behind the last
   int32_t count[TTKV_MAX_BATCH];        // new tokens
-  int32_t row_base[TTKV_MAX_BATCH];     // query rows per KV head of the slots before
+  int32_t part_base[TTKV_MAX_BATCH];    // the slot's first partial, [row][KV head][item of the row's tile]
   // (32 bits wide like the others: arrays of narrower numbers beside them made the compiler add an index in bytes to a scalar load's
   // base, whose two low bits the load leaves out)
   int32_t n_split[TTKV_MAX_BATCH];      // items per row tile
@@ -408,7 +407,19 @@ void start_chunk_mixed(const ChunkArgs &a, const ChunkShape &s, hipStream_t stre
 int64_t chunk_least_steps(const ChunkShape &s);   // of 32 tokens, that an item should have
 int64_t chunk_resident(const ChunkShape &s);      // workgroups on the chip at once
 hipError_t launch_chunk(const ChunkArgs &a, const ChunkShape &s, hipStream_t stream);
-hipError_t launch_chunk_merge(const ChunkArgs &a, int64_t n_rows, hipStream_t stream);   // rows of all heads
+// The join of the partials of the slots whose row tiles are several items.
+struct ChunkMergeArgs {
+  int32_t Hq, Hkv, G;
+  uint32_t g_magic;
+  int32_t out_fmt, n_tokens;
+  uint8_t *out;
+  float *lse;                      // nullable
+  const float *pm, *pl, *pacc;
+  int64_t o_seq, o_token, o_head;
+  int32_t row_base[TTKV_MAX_BATCH];     // rows per KV head that are joined of the slots before, INT32_MAX behind the last
+  int32_t part_base[TTKV_MAX_BATCH], n_split[TTKV_MAX_BATCH], entry[TTKV_MAX_BATCH];   // as in ChunkArgs
+};
+hipError_t launch_chunk_merge(const ChunkMergeArgs &a, int64_t n_rows, hipStream_t stream);   // rows of all heads
 
 // What the queries of a chunk give each token of one tier (weigh_kernel and its kin).
 struct WeighArgs {

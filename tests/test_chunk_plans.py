@@ -1,0 +1,35 @@
+"""How a chunk's launch is cut, as far as the workspace that it asks for tells (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+from paper_2604_19769_amd import binding as B
+from test_abi import host_cache
+from test_chunk_refusals import i64
+from test_operator_refusals import h  # noqa: F401
+
+PART = 520                                                        # a row's part: 128 sums, maximum, sum of weights
+
+
+def cache(lens, Hq=32, Hkv=8):
+    c = host_cache(batch=len(lens), Hq=Hq, Hkv=Hkv, fmts=(("f16", "f16"),), bt=(128,))
+    c.tier[0].ring_blocks = (1 << 24) // 128
+    c.tier[0].pool_blocks = len(lens) * c.tier[0].ring_blocks
+    for b, n in enumerate(lens):
+        C.cast(c.tier[0].len, C.POINTER(C.c_int64))[b] = n
+    return c
+
+
+def parts(h, lens, new, **kw):  # noqa: F811
+    """Parts of a launch, from its workspace."""
+    need = B.ttkv_chunk_workspace_bytes(h, cache(lens, **kw), -1, None, None, max(new), i64(*new))
+    assert need >= 256
+    return (need - 256) // PART
+
+
+@pytest.mark.parametrize("prompt,few,past", [(1024, 4, 100_000), (4096, 4, 500_000), (2000, 1, 2_000_000), (600, 16, 1_000_000)])
+def test_a_prompt_beside_a_long_sequence(h, prompt, few, past):  # noqa: F811
+    """The prompt's rows have as many parts as the prompt is cut into, not as many as the long sequence is: a workgroup leaves 256 parts at most, and
+    cutting adds 6 rounds of 256 workgroups at most to one per row tile and KV head."""
+    got = parts(h, [prompt, past + few], [prompt, few])
+    assert 0 < got <= 256 * (8 * (-(-prompt * 4 // 256) + 1) + 6 * 256)

@@ -1,0 +1,28 @@
+"""Chunks whose sequences are cut along the tokens differently: partials of some, results of the others."""
+import pytest
+
+from chunk_testlib import check, make_cache, rnd
+from paper_2604_19769_amd import binding as B
+from test_gpu_chunk import attend
+
+pytestmark = pytest.mark.gpu
+
+
+def parts(c, T, counts=None):
+    """Partials of a launch, from its workspace (520 bytes each)."""
+    each = None if counts is None else (B.C.c_int64 * len(counts))(*counts)
+    return (B.ttkv_chunk_workspace_bytes(c.h, c.c, -1, None, None, T, each) - 256) // 520
+
+
+@pytest.mark.parametrize("dtype,older", [("f16", None), ("bf16", None), ("f16", "i8"), ("bf16", "i4")])
+@pytest.mark.parametrize("heads,T,counts,past", [((8, 1), 300, [300, 5, 1, 0], [0, 20000, 700, 90]), ((8, 2), 20, [1, 20, 3, 20], [9000, 0, 0, 300]),
+                                                 ((28, 4), 40, [2, 40, 0, 40], [30000, 10, 64, 3000])])
+def test_batches_of_all_lengths(heads, T, counts, past, dtype, older):
+    """A long sequence's rows are many items' and meet in the merge, beside rows that one item answers."""
+    new = [p + n for p, n in zip(past, counts)]
+    tiers = [(dtype, new)] if older is None else [(dtype, counts), (older, past)]
+    c = make_cache(4, heads, tiers, paged=True)
+    q = rnd(5, 4, T, heads[0], 128, dtype=dtype)
+    assert parts(c, T, counts) > 0
+    check(c, q, *attend(c, q, counts), counts=counts, untouched=7.0)
+    c.close()

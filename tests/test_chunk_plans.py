@@ -33,3 +33,22 @@ def test_a_prompt_beside_a_long_sequence(h, prompt, few, past):  # noqa: F811
     cutting adds 6 rounds of 256 workgroups at most to one per row tile and KV head."""
     got = parts(h, [prompt, past + few], [prompt, few])
     assert 0 < got <= 256 * (8 * (-(-prompt * 4 // 256) + 1) + 6 * 256)
+
+
+@pytest.mark.parametrize("prompts,few,past", [([8192], 4, 500_000), ([8192], 1, 2_000_000), ([4000, 5000, 3000], 8, 300_000), ([20_000], 4, 900_000)])
+def test_a_long_sequence_beside_many_rows(h, prompts, few, past):  # noqa: F811
+    """As many row tiles as fill the chip several times: a sequence that would take longer than the rest of the batch by itself is cut all the
+    same, into items of no more than a fair share of the steps of 32 tokens; the prompts are not."""
+    new, lens = [*prompts, few], [*prompts, past + few]
+    tiles = [-(-n * 4 // 256) for n in new]
+    steps = [-(-n // 32) for n in lens]
+    assert sum(tiles) * 8 >= 1024
+    fair = sum(a * b for a, b in zip(tiles, steps)) * 8 // 256
+    cut, rest = divmod(parts(h, lens, new), few * 4 * 8)
+    assert rest == 0 and cut > 1 and steps[-1] <= cut * fair
+
+
+@pytest.mark.parametrize("lens,new", [([8192], None), ([8192] * 4, None), ([9000, 2000, 4000, 8000], None), ([32768], [8192]), ([40_000, 30_000], [4096, 4096])])
+def test_prompts_of_many_rows(h, lens, new):  # noqa: F811
+    """Their own row tiles are items enough: nothing is cut."""
+    assert parts(h, lens, new or lens) == 0

@@ -26,3 +26,17 @@ def test_batches_of_all_lengths(heads, T, counts, past, dtype, older):
     assert parts(c, T, counts) > 0
     check(c, q, *attend(c, q, counts), counts=counts, untouched=7.0)
     c.close()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_long_sequence_beside_many_rows(dtype):
+    """189 row tiles of prompts, and a sequence of few new tokens that is cut all the same."""
+    new = [130] * 63 + [4]
+    p = make_cache(1, (32, 8), [(dtype, [40_000])], seed=40)
+    c = make_cache(64, (32, 8), [(dtype, new)], prefix=p, members=[False] * 63 + [True])
+    each = (B.C.c_int64 * 64)(*new)
+    assert B.ttkv_chunk_workspace_bytes(c.h, c.c, -1, p.c, c.members.ctypes.data, 130, each) > 4 * 4 * 8 * 520 + 256
+    q = rnd(5, 64, 130, 32, 128, dtype=dtype)
+    check(c, q, *attend(c, q, new), counts=new, untouched=7.0)
+    c.close()
+    p.close()

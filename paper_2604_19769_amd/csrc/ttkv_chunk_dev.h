@@ -69,11 +69,13 @@ template <int F, bool TWO>
 __device__ __forceinline__ void unpack_piece(const Piece<F> &x, u32x4 &hi, u32x4 &lo) {
   h2 s2, z2 = {};
   uint32_t n[4];
+  float size;    // infinite where the scale is, or the zero point
   bool beyond;   // some value may
   if constexpr (F == TTKV_I8_SYM_G32) {
     const _Float16 s = __builtin_bit_cast(_Float16, x.s);
     s2 = h2{s, s};
-    beyond = !(fabsf((float)s) < 515.0f);
+    size = fabsf((float)s);
+    beyond = !(size < 515.0f);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const uint32_t w = x.w[i] ^ 0x80808080u;                                // code + 128
@@ -86,7 +88,8 @@ __device__ __forceinline__ void unpack_piece(const Piece<F> &x, u32x4 &hi, u32x4
     const h2 sz = as_h2(x.sz);
     s2 = h2{sz.x, sz.x};
     z2 = h2{sz.y, sz.y};
-    beyond = !(fmaf(15.0f, fabsf((float)sz.x), fabsf((float)sz.y)) < 65504.0f);
+    size = fmaf(15.0f, fabsf((float)sz.x), fabsf((float)sz.y));
+    beyond = !(size < 65504.0f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {                                             // nibbles 2 i and 2 i + 1
       const uint32_t w = x.w >> (8 * i);
@@ -101,7 +104,9 @@ __device__ __forceinline__ void unpack_piece(const Piece<F> &x, u32x4 &hi, u32x4
     hi[i] = __builtin_bit_cast(uint32_t, h);
   }
   if (__any(beyond)) {
-    auto end = [](_Float16 v) { return v != v ? v : (_Float16)fminf(fmaxf((float)v, -65504.0f), 65504.0f); };
+    // (what is infinite stays so: of two numbers the other one is)
+    const float top = TWO || size < INFINITY ? 65504.0f : INFINITY;
+    auto end = [&](_Float16 v) { return v != v ? v : (_Float16)fminf(fmaxf((float)v, -top), top); };
 #pragma unroll
     for (int i = 0; i < 4; ++i) hi[i] = __builtin_bit_cast(uint32_t, h2{end(as_h2(hi[i]).x), end(as_h2(hi[i]).y)});
   }

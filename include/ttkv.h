@@ -452,7 +452,8 @@ size_t ttkv_weights_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t 
  *   swap 0: the freed blocks leave the tier (start[], len[]).  swap != 0: rows change places and nothing leaves: the tier's oldest blocks
  *   then hold the lightest tokens, which ttkv_tier_demote / ttkv_evict take into the next tier.
  *   workspace [device], ttkv_evict_light_workspace_bytes (0: invalid arguments).
- * Device tiers of formats stored by rows (fp16, bf16, int8, int4) without mean keys, blocks of up to 2^21 tokens; UNSUPPORTED otherwise. */
+ * Device tiers of formats stored by rows (fp16, bf16, int8, int4) without mean keys, blocks of up to 2^21 tokens, up to 2^28 - 16 tokens of a
+ * sequence that may move (the fewer of those that go and of those that may stay in front of `recent`); UNSUPPORTED otherwise. */
 ttkv_status ttkv_evict_light(ttkv_handle h, ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent, int32_t swap, float *weights,
                              void *workspace, size_t ws_bytes, void *stream);
 size_t ttkv_evict_light_workspace_bytes(ttkv_handle h, const ttkv_cache *c, int32_t tier, int64_t keep, int64_t recent);

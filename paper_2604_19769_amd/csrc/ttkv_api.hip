@@ -2012,6 +2012,7 @@ ttkv_status plan_light(const ttkv_cache *c, bool check_tables, int32_t tier, int
     moves += (int64_t)a.most_moves[i] * a.Hkv;
     most_moves = std::max(most_moves, a.most_moves[i]);
   }
+  if (most_moves > (1 << 28) - 16) return TTKV_ERR_UNSUPPORTED;   // a launch has 2^32 threads at most, 256 for every 16 moves
   ws_bytes = align256((size_t)a.n_slots * a.Hkv * 4) + (size_t)moves * 8;
   return TTKV_OK;
 }

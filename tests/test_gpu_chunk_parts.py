@@ -1,7 +1,7 @@
 """Chunks whose sequences are cut along the tokens differently: partials of some, results of the others."""
 import pytest
 
-from chunk_testlib import check, make_cache, rnd
+from chunk_testlib import all_tokens, check, make_cache, rnd
 from paper_2604_19769_amd import binding as B
 from test_gpu_chunk import attend
 
@@ -40,3 +40,30 @@ def test_a_long_sequence_beside_many_rows(dtype):
     check(c, q, *attend(c, q, new), counts=new, untouched=7.0)
     c.close()
     p.close()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "bf16", "i8", "i4"])
+@pytest.mark.parametrize("T", [1, 5])
+def test_more_parts_than_a_wave_has_lanes(T, fmt):
+    """A row's parts are more than 64: what has the largest score lies in one of the first, of the last, or nowhere in particular."""
+    dtype = "bf16" if fmt == "bf16" else "f16"
+    c = make_cache(1, (8, 1), [(fmt, [30_000 + T])])
+    assert parts(c, T) > 64 * T * 8
+    keys, _ = all_tokens(c, 0)
+    q = rnd(5, 1, T, 8, 128, dtype=dtype)
+    check(c, q, *attend(c, q))
+    for at in (700, 29_000):                                      # most of the weight on one token
+        x = (q + 3.0 * keys[0, at].to(q.dtype)).contiguous()
+        check(c, x, *attend(c, x))
+    c.close()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "bf16", "i8"])
+def test_one_part_beside_many(fmt):
+    dtype = "bf16" if fmt == "bf16" else "f16"
+    c = make_cache(3, (8, 1), [(fmt, [40, 60_000, 3000])])
+    q = rnd(5, 3, 5, 8, 128, dtype=dtype)
+    counts = [5, 2, 1]
+    assert parts(c, 5, counts) > 64 * 2 * 8
+    check(c, q, *attend(c, q, counts), counts=counts, untouched=7.0)
+    c.close()

@@ -415,9 +415,9 @@ ttkv_status ttkv_decode_step_shared(ttkv_handle h, ttkv_cache *c, const ttkv_cac
  *           worked on as fp16 numbers: they end at 131008 (values for bf16 outputs at 65504).
  *   q       [entry][token][n_q_heads][128], F16 or BF16 (a BF16 tier needs BF16; otherwise |q| below 65504);
  *   out     the same shape, F16 or BF16: rounded once from fp32.  Softmax weights meet the values rounded to the product's type (fp16; bf16
- *           over bf16 tiers), their sums and maxima are fp32.
+ *           over bf16 tiers, where F16 results are no finer than BF16 ones for it), their sums and maxima are fp32.
  *   lse     [device] fp32 [entry][n_tokens][n_q_heads] or NULL.  Rows of out and lse behind a sequence's count stay as they were.
- *   workspace [device], ttkv_chunk_workspace_bytes (0: invalid arguments): partials, where few rows are cut along the tokens.
+ *   workspace [device], ttkv_chunk_workspace_bytes (0: invalid arguments): partials of the sequences whose few rows are cut along the tokens.
  * A score that is no number makes a NaN of its row; a value that is infinite or none leaves no finite number in its channel, in the rows that see it. */
 #define TTKV_MAX_CHUNK_TOKENS (1 << 22)
 ttkv_status ttkv_chunk_attn(ttkv_handle h, const ttkv_cache *c, int32_t seq, const ttkv_cache *prefix, const int32_t *member,

@@ -8,10 +8,12 @@
 // Outputs are 16 bits wide, so the weights are rounded once to the product's type; their sum, the maximum and the log-sum-exp stay fp32.
 // Quantized tiers are worked on in fp16 whatever the others' type, in front of them.  Their rows are decompressed on their way into LDS, keys
 // into two numbers each (22 bits: the log-sum-exp is an fp32 number), values into two where the outputs are fp16, into one where bf16 outputs
-// end far above what that rounds.
+// end far above what that rounds.  (fp16 outputs over bf16 tiers: the weights have bf16's 8 bits there too.)
 //
 // A kernel knows the formats that it meets (Q: none, one, or all of the quantized ones): with the loops of all of them in every kernel, registers end in
-// scratch (20001 int8 tokens 1423 us instead of 1193, int4 turns 106 instead of 95).
+// scratch (20001 int8 tokens 1423 us instead of 1193, int4 turns 106 instead of 95).  Where a launch's tiers have several quantized formats it takes the
+// kernels of all of them, and there 14 to 60 registers do end in scratch: 2048 new tokens of 32 / 8 fp16 heads over 10000 int8 and 10000 int4 tokens
+// 1405 us, over each of the two alone 665; 16 x 12 new ones over 4096 and 4096 142, alone 78 and 85.
 #pragma once
 #include "ttkv_chunk_dev.h"
 
@@ -438,10 +440,12 @@ __device__ __forceinline__ void each_tier(const ChunkArgs &a, const Share<RW, TW
 }
 
 // ---------------------------------------------------------------- few rows
-// Bound: memory (32 sequences of 4000 to 6000 bf16 tokens, 32 / 8 heads, 16 rows per KV head: 522 MB in 107 us, 4.9 TB/s where a large copy reaches 5.1).  A workgroup has
-// all rows of a KV head and a part of its tokens, four teams of two waves; keys of one step and values of the one before are on their way while one is computed.  The outputs are divided by the sum of the
-// weights as they were rounded: where a token or two have most of the weight, their rounding then cancels.  With quantized tiers LDS holds one step
-// only, so that a CU has two workgroups: one decompresses while the other computes (int4 histories of 8192 tokens, 48 rows: 89 us; with one workgroup of eight waves 250).
+// Bound: memory, not at its best (32 sequences of 4000 to 6000 bf16 tokens, 32 / 8 heads, 16 rows per KV head: 522 MB in 107 us, 4.9 TB/s; a decode step reads
+// such rows at 6.2, a kernel that only loads at 6.9): one step's rows are on their way at a time, through registers.  A workgroup has all rows of a KV
+// head and a part of its tokens, four teams of two waves; keys of one step and values of the one before are on their way while one is computed.  The
+// outputs are divided by the sum of the weights as they were rounded: where a token or two have most of the weight, their rounding then cancels.  With
+// quantized tiers LDS holds one step only, so that a CU has two workgroups: one decompresses while the other computes (int4 histories of 8192 tokens,
+// 48 rows: 89 us; with one workgroup of eight waves 250).
 template <bool BF, int Q, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, Q ? 2 : 1) void chunk_kernel(const ChunkArgs a) {
   constexpr int kKeys = 32 * kRowK, kValues = 32 * kRowV, kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kStep = kPartsK * kKeys + kPartsV * kValues;
@@ -561,11 +565,12 @@ __device__ __forceinline__ void interleave() {
 }
 
 // ---------------------------------------------------------------- many rows
-// Bound: the matrix cores and the power limit, then what the rows' way into LDS costs: 2048 fp16 rows of 32 / 8 heads behind 32768 tokens 1150 us, 0.98 PFLOP/s where a large
-// library product reaches 1.36; 980 without the loads, 870 with the products alone (builds for the measurement).  The steps overlap inside a wave: while the softmax of step s runs on the vector
-// unit, the matrix cores work on the values of step s - 1 and the scores of step s + 1.  One barrier per step.  fp rows come into LDS without
-// registers, three steps ahead, into four slots each of keys and values (through registers, one step ahead: 1205); codes through registers, into two.  256 rows per
-// workgroup, so that the CUs read an XCD's KV head from its L2 half as often as with 128; two workgroups of four waves per CU 1356.
+// Bound: the matrix cores and the power limit, then what the rows' way into LDS costs: 2048 new fp16 tokens (8192 rows per KV head) of 32 / 8 heads behind 32768 1085 to 1125 us, 1.0
+// PFLOP/s where a large library product reaches 1.36.  Builds for the measurement, beside this one at 1150 us (the clock goes with the card's power): 980 without the loads, 870 with the
+// products alone.  The steps overlap inside a wave: while the softmax of step s runs on the vector unit, the matrix cores work on the values of step s - 1 and
+// the scores of step s + 1.  One barrier per step.  fp rows come into LDS without registers, three steps ahead, into four slots each of keys and values
+// (through registers, one step ahead: 1205); codes through registers, into two.  256 rows per workgroup, so that the CUs read an XCD's KV head
+// from its L2 half as often as with 128; two workgroups of four waves per CU 1356 where this took 1268.
 template <bool BF, int Q, bool V2, int RW, int TW>
 __global__ __launch_bounds__(64 * RW * TW, 1) void chunk_rows_kernel(const ChunkArgs a) {
   constexpr int kPartsK = Q ? 2 : 1, kPartsV = V2 ? 2 : 1, kTeam = 8 * kSlot;

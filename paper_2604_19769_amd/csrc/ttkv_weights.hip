@@ -181,8 +181,9 @@ __device__ __forceinline__ f16v sum_steps(f16v acc, const Operands<KF> &ops, con
   return add_rows(acc, nx, cs, rn.off);
 }
 
-// Few rows (a step's, the last queries of a prompt).  Bound: memory (a step of 48 x 2000 to 4000 fp16 tokens, 32 / 8 heads: 305 MB in 57-62 us, 5 TB/s), and from some 200 rows
-// on the vector unit's exponentials (256 rows x 4 x 16384 bf16 tokens 51 us; its bytes alone 28).  All rows lie in LDS; the waves take an item's tokens 32 at a time, the
+// Few rows (a step's, the last queries of a prompt).  Bound: memory, not at its best (a step of 48 sequences of 2000 to 4000 fp16 tokens, 32 / 8 heads: 305 MB in 57-65 us, 4.7 to 5.3
+// TB/s; a decode step reads fp16 rows at 5.9), and from some 200 rows on the vector unit's exponentials (256 rows x 4 x 16384 bf16 tokens 51 us; its bytes
+// alone 28).  All rows lie in LDS; the waves take an item's tokens 32 at a time, the
 // next ones' keys on their way, and meet nobody.  Keys are loaded as whole lines and turned into operands through LDS of the wave's own (as
 // operands they are pieces of 32 bytes of 32 rows per instruction: a step of 48 x 4000 tokens of 32 / 8 heads 86 us).
 template <bool BF, int KF, int ROWS, int NW>
@@ -564,8 +565,10 @@ void weigh_shape(int64_t most_rows, int64_t tiles, int32_t Hkv, int32_t &chunk, 
   n_split = 1;
   chunk = kTile;
   const int64_t resident = 256;
-  // Up to 256 rows, all in LDS: 256 rows x 4 x 16384 tokens 54 us, 75 in the kernel for many; 256 x 4096 tokens 10.5 and 10.9.  One round of the workgroups that a CU
-  // holds: three with 64 rows (8 x 8192 tokens 24.8 us, 28.5 with 2048 items; in the kernel for 256 rows 24.9, but 48 x 4000 98 instead of 82), one with 256.
+  // Up to 256 rows, all in LDS: 256 rows x 4 x 16384 tokens 54 us, 75 in the kernel for many; 256 x 4096 tokens 10.5 and 10.9.  fp keys: one round of the workgroups that a CU
+  // holds, three with 64 rows (8 x 8192 fp16 tokens 24.8 us, 28.5 with 2048 items; in the kernel for 256 rows 24.9, but 48 x 4000 98 instead of 82), one with 256.
+  // int8 and int4 keys, in two numbers each, leave room for one workgroup per CU either way; 768 items instead of 256, us with some 6 of the timing's own: a query of
+  // 48 x 4000 tokens int8 133 and 166, int4 145 and 183; of 8 x 8192 60 and 52, 63 and 56 (fp16 88 and 101, 33 and 38); 64 queries of 4 x 16384 have 256: 100, 102 (60).
   if (most_rows <= kFewRows) {
     const int64_t want = most_rows <= 64 ? 768 : 256;
     chunk = (int32_t)(kTile * std::max<int64_t>(1, std::min<int64_t>(64, (tiles * Hkv + want - 1) / want)));
